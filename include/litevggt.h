@@ -326,6 +326,98 @@ int litevggt_layers_run(const litevggt_params *p, int n_layers, const void *imag
                         void *stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Frames as they arrive: K and V of the tokens so far are kept in a paged cache, new tokens (one,
+ * a frame, several frames) attend to them, and token sets attend to states of another length.
+ * The calls take lengths, offsets and page numbers from device memory: nothing about a
+ * batch has to be known on the host, and a captured call can be replayed with other lengths.  Every
+ * number that is read there is checked against the sizes given here; what is out of range is
+ * left out, never followed.
+ */
+enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1 };
+
+typedef struct {
+  int32_t n_seq;           /* sequences of a call, 1 .. 65535                          */
+  int32_t heads;           /* query heads, a multiple of kv_heads: query head h uses kv head
+                              h / (heads / kv_heads)                                   */
+  int32_t kv_heads;        /* heads of K and V, 1 .. 1024                              */
+  int32_t head_dim;        /* 64 or 128                                                */
+  int32_t cache_dtype;     /* LV_CACHE_BF16 or LV_CACHE_E4M3                           */
+  int32_t page_tokens;     /* positions of a page: 16, 32, .. 1024                     */
+  int32_t n_pages;         /* pages of the pool                                        */
+  int32_t max_pages;       /* columns of the page table                                */
+  int32_t frame_tokens;    /* T > 0: a query at position p sees positions below
+                              (p / T + 1) T, its own frame and those before it (T = 1: up to
+                              itself); 0: every position                               */
+  int32_t qk_norm;         /* != 0: K is RMS-normalised per head as it is written, q as it is
+                              used: x <- bf16(x / sqrt(mean(x^2) + 1e-6))              */
+  float   softmax_scale;   /* <= 0 selects 1/sqrt(head_dim)                            */
+} litevggt_cache_params;
+
+/* Caller-owned device buffers of a cache.  Position t of sequence s is row t % page_tokens of page
+ * page_table[s][t / page_tokens]; a number outside 0 .. n_pages-1 (-1): the page is not held.
+ * E4M3: value = code * 2^(scale - 127), one scale per row (token and kv head, K and V apart).  Pages
+ * may serve several sequences for reading; where two calls' or sequences' writes meet in one row, either may win. */
+typedef struct {
+  void *k, *v;                  /* [n_pages][kv_heads][page_tokens][head_dim] bf16 or E4M3 codes */
+  uint8_t *k_scale, *v_scale;   /* [n_pages][kv_heads][page_tokens]; LV_CACHE_E4M3 only          */
+  const int32_t *page_table;    /* [n_seq][max_pages]                                            */
+} litevggt_cache;
+
+/* Writes new tokens into the cache: row new_off[s] + i of k and v becomes position pos[s] + i of
+ * sequence s, for new_off[s] <= row < new_off[s+1].  Rows of no sequence and positions whose page is not held are
+ * left out; every other row of the pool keeps what it holds.  E4M3: a row's scale is the smallest power of two (at
+ * least 2^-126, 1 for a row of zeros) with max|x| <= 448 * scale over the finite values of the row; code =
+ * RNE(x / scale); infinities become +-448 * scale, NaN stays.
+ *   k, v     [device] [n_tokens, kv_heads, head_dim] bf16, rows k_stride, v_stride elements apart
+ *            (multiples of 8, at least kv_heads * head_dim, at most 2^26)
+ *   new_off  [device] [n_seq+1] ascending;  pos [device] [n_seq]
+ */
+int litevggt_cache_write(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
+                         const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                         const int32_t *new_off, const int32_t *pos, void *stream);
+
+/* Reads positions back: row off[s] + i of k and v becomes position first[s] + i of sequence s as
+ * bf16 (exact), zeros where the page is not held.  Rows of no sequence are left as they were.
+ *   k, v [device] [n_tokens, kv_heads, head_dim] bf16 out, strides as above
+ */
+int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *cache, const int32_t *first,
+                        const int32_t *off, int64_t n_tokens, void *k, int64_t k_stride, void *v,
+                        int64_t v_stride, void *stream);
+
+/* Attention of new tokens over the cache, their own K and V in it already: the rows new_off[s] ..
+ * new_off[s+1]-1 of q are the last ones of sequence s's kv_len[s] positions.  Per query head:
+ * o = softmax(q K^T * softmax_scale) V over the positions that are held and that the query sees
+ * (frame_tokens); a query that sees none gives zeros.  What lies in positions that a query does not
+ * see (infinities and NaN too) has no part in its result.  One token per sequence and whole frames go
+ * through the same call.  Rows of no sequence are left as they were.
+ *   q   [device] [n_tokens, heads, head_dim] bf16, o likewise, out; row strides in elements as above
+ *   ws  litevggt_cached_attn_ws_bytes(p, n_tokens) bytes
+ * The weights are rounded to bf16 for the second product; scores, the softmax's sums and
+ * the output's stay fp32.  Results do not depend on the order in which workgroups run.
+ */
+size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens);
+int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
+                         const void *q, int64_t q_stride, const int32_t *new_off, const int32_t *kv_len,
+                         void *o, int64_t o_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* Cross attention: the queries q_off[s] .. q_off[s+1]-1 attend to the states kv_begin[s] ..
+ * kv_end[s]-1, rows of another set of another length (ranges may overlap: several query sets over the
+ * same states; a padded batch gives the rows that are there).  An empty range gives zeros.
+ * Otherwise as litevggt_cached_attn; qk_norm normalises q and k in the call.
+ *   q, o   [device] [n_q, heads, head_dim] bf16;  k, v [device] [n_kv, kv_heads, head_dim] bf16
+ *   ws     litevggt_cross_attn_ws_bytes(p, n_q, n_kv) bytes
+ */
+typedef struct {
+  int32_t n_seq, heads, kv_heads, head_dim, qk_norm;   /* as in litevggt_cache_params */
+  float   softmax_scale;
+} litevggt_cross_params;
+size_t litevggt_cross_attn_ws_bytes(const litevggt_cross_params *p, int64_t n_q, int64_t n_kv);
+int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void *q, int64_t q_stride,
+                        const int32_t *q_off, int64_t n_kv, const void *k, int64_t k_stride, const void *v,
+                        int64_t v_stride, const int32_t *kv_begin, const int32_t *kv_end, void *o,
+                        int64_t o_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
  * Measurement aids (no part of the method): what this GPU sustains on the two resources the
  * kernels' rooflines are quoted against, with nothing else in the way.  A benchmark runs them
  * next to the hot path and times them with events on `stream`.

@@ -21,6 +21,7 @@ LINEAR_BF16, LINEAR_FP8_E4M3 = 0, 1
 FP8_CURRENT, FP8_DELAYED = 0, 1
 FP8_HISTORY = 80
 FP8_STATE_BYTES = 4 * (FP8_HISTORY + 2) * 4
+CACHE_BF16, CACHE_E4M3 = 0, 1
 ROLE_PROTECTED, ROLE_DST, ROLE_SRC = 0, 1, 2
 
 STATIC_SCORE_MAX = 2 * 1024 * 1024
@@ -29,6 +30,8 @@ EXPORTS = ["litevggt_strerror", "litevggt_plan", "litevggt_attn_ws_bytes", "lite
            "litevggt_select_anchors", "litevggt_match", "litevggt_merge", "litevggt_global_attn",
            "litevggt_unmerge", "litevggt_frame_attn_ws_bytes", "litevggt_frame_attn",
            "litevggt_global_block_ws_bytes", "litevggt_global_block",
+           "litevggt_cache_write", "litevggt_cache_read", "litevggt_cached_attn_ws_bytes",
+           "litevggt_cached_attn", "litevggt_cross_attn_ws_bytes", "litevggt_cross_attn",
            "litevggt_layers_run", "litevggt_probe_mfma", "litevggt_probe_stream",
            "litevggt_probe_mfma_flop", "litevggt_probe_gather"]
 
@@ -69,6 +72,34 @@ class Index(C.Structure):
     _fields_ = [("role", C.c_void_p), ("kept_idx", C.c_void_p), ("dst_idx", C.c_void_p),
                 ("src_idx", C.c_void_p), ("anchor_of", C.c_void_p), ("slot_of", C.c_void_p),
                 ("group_off", C.c_void_p), ("group_mem", C.c_void_p)]
+
+
+class CacheParams(C.Structure):
+    """Mirror of ``litevggt_cache_params``."""
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "heads", "kv_heads", "head_dim", "cache_dtype", "page_tokens",
+                                         "n_pages", "max_pages", "frame_tokens", "qk_norm")] + [
+        ("softmax_scale", C.c_float)]
+
+
+class Cache(C.Structure):
+    """Mirror of ``litevggt_cache`` (device pointers)."""
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")]
+
+
+class CrossParams(C.Structure):
+    """Mirror of ``litevggt_cross_params``."""
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "heads", "kv_heads", "head_dim", "qk_norm")] + [
+        ("softmax_scale", C.c_float)]
+
+
+def make_cache_params(n_seq, heads, head_dim, *, kv_heads=None, cache_dtype=CACHE_BF16, page_tokens=64,
+                      n_pages, max_pages, frame_tokens=0, qk_norm=0, softmax_scale=0.0) -> CacheParams:
+    return CacheParams(n_seq, heads, heads if kv_heads is None else kv_heads, head_dim, cache_dtype,
+                       page_tokens, n_pages, max_pages, frame_tokens, qk_norm, softmax_scale)
+
+
+def make_cross_params(n_seq, heads, head_dim, *, kv_heads=None, qk_norm=0, softmax_scale=0.0) -> CrossParams:
+    return CrossParams(n_seq, heads, heads if kv_heads is None else kv_heads, head_dim, qk_norm, softmax_scale)
 
 
 def make_params(frames, grid_h, grid_w, dim, heads, *, head_dim=64, n_special=5, patch=14,
@@ -113,6 +144,15 @@ def lib() -> C.CDLL:
         L.litevggt_frame_attn_ws_bytes.restype = sz
         L.litevggt_frame_attn_ws_bytes.argtypes = [PP]
         L.litevggt_frame_attn.argtypes = [PP, vp, vp, vp, vp, vp, vp, sz, vp]
+        CP, CC, XP = C.POINTER(CacheParams), C.POINTER(Cache), C.POINTER(CrossParams)
+        L.litevggt_cache_write.argtypes = [CP, CC, i64, vp, i64, vp, i64, vp, vp, vp]
+        L.litevggt_cache_read.argtypes = [CP, CC, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.litevggt_cached_attn_ws_bytes.restype = sz
+        L.litevggt_cached_attn_ws_bytes.argtypes = [CP, i64]
+        L.litevggt_cached_attn.argtypes = [CP, CC, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+        L.litevggt_cross_attn_ws_bytes.restype = sz
+        L.litevggt_cross_attn_ws_bytes.argtypes = [XP, i64, i64]
+        L.litevggt_cross_attn.argtypes = [XP, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
         L.litevggt_layers_run.argtypes = [PP, i32, vp, vp, C.POINTER(Index), vp, vp,
                                           C.POINTER(C.c_int32), C.POINTER(C.c_void_p), vp, sz, vp]
         L.litevggt_probe_mfma.argtypes = [i32, vp, i32, vp, vp]
@@ -270,6 +310,100 @@ def litevggt_global_block(p: Params, n_tokens: int, z, weights: BlockWeights, de
     wp, wn = _ws_args(ws)
     _check(lib().litevggt_global_block(C.byref(p), n_tokens, _ptr(z), C.byref(weights), _ptr(delta),
                                        wp, wn, _stream()), "litevggt_global_block")
+
+
+# ------------------------------------------------------------------ frames as they arrive
+@dataclass
+class CacheBuffers:
+    """Device tensors of a cache (owned by the caller).  ``k``, ``v``: [n_pages, kv_heads, page_tokens, head_dim]
+    bf16 or uint8 codes; ``k_scale``, ``v_scale``: uint8 [n_pages, kv_heads, page_tokens] (None for a bf16
+    cache); ``page_table``: int32 [n_seq, max_pages], -1 where no page is held."""
+    k: "object"
+    v: "object"
+    k_scale: "object"
+    v_scale: "object"
+    page_table: "object"
+
+    def struct(self) -> Cache:
+        return Cache(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), _ptr(self.page_table))
+
+
+def alloc_cache(p: CacheParams, device="cuda") -> CacheBuffers:
+    """An empty cache: no sequence holds a page.  (Pages need not be cleared before they are handed out.)"""
+    import torch
+    shape = (p.n_pages, p.kv_heads, p.page_tokens)
+    e4m3 = p.cache_dtype == CACHE_E4M3
+    rows = [torch.empty(*shape, p.head_dim, dtype=torch.uint8 if e4m3 else torch.bfloat16, device=device) for _ in range(2)]
+    scales = [torch.empty(shape, dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2)]
+    return CacheBuffers(*rows, *scales, torch.full((p.n_seq, p.max_pages), -1, dtype=torch.int32, device=device))
+
+
+def _rows(t, heads: int, head_dim: int, what: str):
+    """Count, pointer and row stride of a bf16 tensor [n, heads, head_dim] or [n, heads * head_dim]
+    whose rows are contiguous; rows may be apart (slices of a joint projection)."""
+    import torch
+    if t is None:
+        return 0, None, heads * head_dim
+    ok = t.dtype == torch.bfloat16 and t.dim() in (2, 3) and t.shape[1:].numel() == heads * head_dim and t.stride(-1) == 1
+    if ok and t.dim() == 3:
+        ok = t.shape[2] == head_dim and (heads == 1 or t.stride(1) == head_dim)
+    if not ok:
+        raise LiteVGGTError(f"{what}: bf16 rows of {heads} x {head_dim} contiguous values wanted, got "
+                            f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
+    return t.shape[0], t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * head_dim)
+
+
+def litevggt_cache_write(p: CacheParams, cache: CacheBuffers, k, v, new_off, pos) -> None:
+    n, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
+    m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
+    _same(n, m, "k and v")
+    c = cache.struct()
+    _check(lib().litevggt_cache_write(C.byref(p), C.byref(c), n, kp, ks, vp, vs, _ptr(new_off), _ptr(pos), _stream()),
+           "litevggt_cache_write")
+
+
+def litevggt_cache_read(p: CacheParams, cache: CacheBuffers, first, off, k, v) -> None:
+    n, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
+    m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
+    _same(n, m, "k and v")
+    c = cache.struct()
+    _check(lib().litevggt_cache_read(C.byref(p), C.byref(c), _ptr(first), _ptr(off), n, kp, ks, vp, vs, _stream()),
+           "litevggt_cache_read")
+
+
+def litevggt_cached_attn_ws_bytes(p: CacheParams, n_tokens: int) -> int:
+    return int(lib().litevggt_cached_attn_ws_bytes(C.byref(p), n_tokens))
+
+
+def litevggt_cached_attn(p: CacheParams, cache: CacheBuffers, q, new_off, kv_len, o, ws) -> None:
+    n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
+    m, op, os_ = _rows(o, p.heads, p.head_dim, "o")
+    _same(n, m, "q and o")
+    c = cache.struct()
+    wp, wn = _ws_args(ws)
+    _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, _ptr(new_off), _ptr(kv_len), op, os_, wp, wn,
+                                      _stream()), "litevggt_cached_attn")
+
+
+def litevggt_cross_attn_ws_bytes(p: CrossParams, n_q: int, n_kv: int) -> int:
+    return int(lib().litevggt_cross_attn_ws_bytes(C.byref(p), n_q, n_kv))
+
+
+def litevggt_cross_attn(p: CrossParams, q, q_off, k, v, kv_begin, kv_end, o, ws) -> None:
+    n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
+    m, op, os_ = _rows(o, p.heads, p.head_dim, "o")
+    _same(n, m, "q and o")
+    n_kv, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
+    m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
+    _same(n_kv, m, "k and v")
+    wp, wn = _ws_args(ws)
+    _check(lib().litevggt_cross_attn(C.byref(p), n, qp, qs, _ptr(q_off), n_kv, kp, ks, vp, vs, _ptr(kv_begin),
+                                     _ptr(kv_end), op, os_, wp, wn, _stream()), "litevggt_cross_attn")
+
+
+def _same(a: int, b: int, what: str) -> None:
+    if a != b:
+        raise LiteVGGTError(f"{what}: {a} and {b} rows")
 
 
 EVENTS_PER_LAYER = 10

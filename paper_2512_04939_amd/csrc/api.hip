@@ -113,6 +113,49 @@ float scale_of(const litevggt_params *p) {
   return p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
 }
 
+// ---- the paged cache and attention over keys of another set
+constexpr int64_t kMostStride = (int64_t)1 << 26;   // elements: 16 rows' bytes stay below 2^31
+
+int check_heads(int n_seq, int heads, int kv_heads, int head_dim, float softmax_scale) {
+  if (n_seq < 1 || n_seq > 65535) return LV_ERR_SHAPE;
+  if (kv_heads < 1 || heads < kv_heads || heads > 1024 || heads % kv_heads != 0) return LV_ERR_SHAPE;
+  if (head_dim != 64 && head_dim != 128) return LV_ERR_SHAPE;
+  if (!isfinite(softmax_scale)) return LV_ERR_PARAM;
+  return LV_OK;
+}
+int check_cache(const litevggt_cache_params *p, CacheView *cv) {
+  if (!p) return LV_ERR_NULL;
+  const int rc = check_heads(p->n_seq, p->heads, p->kv_heads, p->head_dim, p->softmax_scale);
+  if (rc) return rc;
+  if (p->cache_dtype != LV_CACHE_BF16 && p->cache_dtype != LV_CACHE_E4M3) return LV_ERR_DTYPE;
+  int shift = 4;
+  while (shift < 10 && (1 << shift) < p->page_tokens) ++shift;
+  if ((1 << shift) != p->page_tokens || p->n_pages < 1 || p->max_pages < 1) return LV_ERR_SHAPE;
+  if (((int64_t)p->max_pages << shift) >= ((int64_t)1 << 31)) return LV_ERR_SHAPE;
+  if (p->frame_tokens < 0) return LV_ERR_PARAM;
+  cv->n_seq = p->n_seq;
+  cv->kv_heads = p->kv_heads;
+  cv->head_dim = p->head_dim;
+  cv->page_shift = shift;
+  cv->n_pages = p->n_pages;
+  cv->max_pages = p->max_pages;
+  cv->e4m3 = p->cache_dtype == LV_CACHE_E4M3;
+  cv->table = nullptr;
+  return LV_OK;
+}
+int check_cache_buffers(const litevggt_cache *c, CacheView *cv) {
+  if (!c || !c->k || !c->v || !c->page_table) return LV_ERR_NULL;
+  if (cv->e4m3 && (!c->k_scale || !c->v_scale)) return LV_ERR_NULL;
+  if (((uintptr_t)c->k | (uintptr_t)c->v) & 15u) return LV_ERR_SHAPE;
+  cv->table = c->page_table;
+  return LV_OK;
+}
+// rows of `heads` heads: pointer and stride of n of them
+bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
+  return ((uintptr_t)p & 15u) == 0 && stride % 8 == 0 && stride >= width && stride <= kMostStride && n >= 0;
+}
+bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n * heads < ((int64_t)1 << 31) && n < ((int64_t)1 << 31); }
+
 }  // namespace
 
 extern "C" {
@@ -386,6 +429,129 @@ int litevggt_layers_run(const litevggt_params *p, int n_layers, const void *imag
     if ((rc = mark(LV_EV_FRAME_ATTN_END))) return rc;
   }
   return LV_OK;
+}
+
+int litevggt_cache_write(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
+                         const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                         const int32_t *new_off, const int32_t *pos, void *stream) {
+  CacheView cv;
+  int rc = check_cache(p, &cv);
+  if (rc) return rc;
+  if ((rc = check_cache_buffers(cache, &cv))) return rc;
+  if (!new_off || !pos || (n_tokens > 0 && (!k || !v))) return LV_ERR_NULL;
+  const int64_t width = (int64_t)p->kv_heads * p->head_dim;
+  if (!count_ok(n_tokens, p->kv_heads) || !rows_ok(k, k_stride, n_tokens, width) || !rows_ok(v, v_stride, n_tokens, width)) return LV_ERR_SHAPE;
+  if (n_tokens == 0) return LV_OK;
+  return launch_cache_write(cv, *cache, (const uint16_t *)k, k_stride, (const uint16_t *)v, v_stride, new_off, pos, (int)n_tokens,
+                            p->qk_norm, (hipStream_t)stream);
+}
+
+int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *cache, const int32_t *first,
+                        const int32_t *off, int64_t n_tokens, void *k, int64_t k_stride, void *v,
+                        int64_t v_stride, void *stream) {
+  CacheView cv;
+  int rc = check_cache(p, &cv);
+  if (rc) return rc;
+  if ((rc = check_cache_buffers(cache, &cv))) return rc;
+  if (!first || !off || (n_tokens > 0 && (!k || !v))) return LV_ERR_NULL;
+  const int64_t width = (int64_t)p->kv_heads * p->head_dim;
+  if (!count_ok(n_tokens, p->kv_heads) || !rows_ok(k, k_stride, n_tokens, width) || !rows_ok(v, v_stride, n_tokens, width)) return LV_ERR_SHAPE;
+  if (n_tokens == 0) return LV_OK;
+  return launch_cache_read(cv, *cache, first, off, (uint16_t *)k, k_stride, (uint16_t *)v, v_stride, (int)n_tokens, (hipStream_t)stream);
+}
+
+size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
+  CacheView cv;
+  if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
+  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, (int64_t)p->max_pages << cv.page_shift);
+}
+
+int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
+                         const void *q, int64_t q_stride, const int32_t *new_off, const int32_t *kv_len,
+                         void *o, int64_t o_stride, void *ws, size_t ws_bytes, void *stream) {
+  KvAttnArgs a = {};
+  int rc = check_cache(p, &a.cv);
+  if (rc) return rc;
+  if ((rc = check_cache_buffers(cache, &a.cv))) return rc;
+  if (!new_off || !kv_len || (n_tokens > 0 && (!q || !o))) return LV_ERR_NULL;
+  const int64_t width = (int64_t)p->heads * p->head_dim;
+  if (!count_ok(n_tokens, p->heads) || !rows_ok(q, q_stride, n_tokens, width) || !rows_ok(o, o_stride, n_tokens, width)) return LV_ERR_SHAPE;
+  if (n_tokens == 0) return LV_OK;
+  if (!ws_ok(ws, ws_bytes, litevggt_cached_attn_ws_bytes(p, n_tokens))) return LV_ERR_WORKSPACE;
+  a.q = (const uint16_t *)q;
+  a.o = (uint16_t *)o;
+  a.q_stride = q_stride;
+  a.o_stride = o_stride;
+  a.q_off = new_off;
+  a.n_q = (int)n_tokens;
+  a.n_seq = p->n_seq;
+  a.heads = p->heads;
+  a.kv_heads = p->kv_heads;
+  a.head_dim = p->head_dim;
+  a.scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
+  a.qk_norm = p->qk_norm;
+  a.frame = p->frame_tokens;
+  a.paged = true;
+  a.k = cache->k;
+  a.v = cache->v;
+  a.k_scale = cache->k_scale;
+  a.v_scale = cache->v_scale;
+  a.k_end = kv_len;
+  return launch_kv_attn(a, ws, (hipStream_t)stream);
+}
+
+static int check_cross(const litevggt_cross_params *p) {
+  if (!p) return LV_ERR_NULL;
+  return check_heads(p->n_seq, p->heads, p->kv_heads, p->head_dim, p->softmax_scale);
+}
+// scratch: the sums of the pieces, then K normalised
+size_t litevggt_cross_attn_ws_bytes(const litevggt_cross_params *p, int64_t n_q, int64_t n_kv) {
+  if (check_cross(p) || n_q < 1 || !count_ok(n_q, p->heads) || !count_ok(n_kv, p->kv_heads)) return 0;
+  const size_t norm = p->qk_norm ? align_up((size_t)n_kv * p->kv_heads * p->head_dim * 2, 256) : 0;
+  return kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, n_kv) + norm;
+}
+
+int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void *q, int64_t q_stride,
+                        const int32_t *q_off, int64_t n_kv, const void *k, int64_t k_stride, const void *v,
+                        int64_t v_stride, const int32_t *kv_begin, const int32_t *kv_end, void *o,
+                        int64_t o_stride, void *ws, size_t ws_bytes, void *stream) {
+  int rc = check_cross(p);
+  if (rc) return rc;
+  if (!q_off || !kv_begin || !kv_end || (n_q > 0 && (!q || !o)) || (n_kv > 0 && (!k || !v))) return LV_ERR_NULL;
+  const int64_t width = (int64_t)p->heads * p->head_dim, kw = (int64_t)p->kv_heads * p->head_dim;
+  if (!count_ok(n_q, p->heads) || !count_ok(n_kv, p->kv_heads)) return LV_ERR_SHAPE;
+  if (!rows_ok(q, q_stride, n_q, width) || !rows_ok(o, o_stride, n_q, width)) return LV_ERR_SHAPE;
+  if (n_kv > 0 && (!rows_ok(k, k_stride, n_kv, kw) || !rows_ok(v, v_stride, n_kv, kw))) return LV_ERR_SHAPE;
+  if (n_q == 0) return LV_OK;
+  if (!ws_ok(ws, ws_bytes, litevggt_cross_attn_ws_bytes(p, n_q, n_kv))) return LV_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  KvAttnArgs a = {};
+  a.k = k;
+  a.k_stride = k_stride;
+  if (p->qk_norm && n_kv > 0) {
+    uint16_t *kn = (uint16_t *)((char *)ws + kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, n_kv));
+    if ((rc = launch_norm_rows((const uint16_t *)k, k_stride, (int)n_kv, p->kv_heads, p->head_dim, kn, st))) return rc;
+    a.k = kn;
+    a.k_stride = kw;
+  }
+  a.q = (const uint16_t *)q;
+  a.o = (uint16_t *)o;
+  a.q_stride = q_stride;
+  a.o_stride = o_stride;
+  a.q_off = q_off;
+  a.n_q = (int)n_q;
+  a.n_seq = p->n_seq;
+  a.heads = p->heads;
+  a.kv_heads = p->kv_heads;
+  a.head_dim = p->head_dim;
+  a.scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
+  a.qk_norm = p->qk_norm;
+  a.v = v;
+  a.v_stride = v_stride;
+  a.k_begin = kv_begin;
+  a.k_end = kv_end;
+  a.n_kv = (int)n_kv;
+  return launch_kv_attn(a, ws, st);
 }
 
 }  // extern "C"

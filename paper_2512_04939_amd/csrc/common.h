@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace lv {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
@@ -171,6 +173,13 @@ __device__ __forceinline__ u32x2 quant8(const u32x4 w, float r) {
                         clamp448(bf16_lo(w.y) * r), clamp448(bf16_hi(w.y) * r)),
                cvt4_fp8(clamp448(bf16_lo(w.z) * r), clamp448(bf16_hi(w.z) * r),
                         clamp448(bf16_lo(w.w) * r), clamp448(bf16_hi(w.w) * r))};
+}
+// 8 fp8 bytes times a power of two as 8 bf16 values (v_cvt_scalef32_pk_bf16_fp8 takes the scale's exponent; exact)
+__device__ __forceinline__ u32x4 dequant8(const u32x2 w, float scale) {
+  auto two = [&](uint32_t x, auto hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, decltype(hi)::value));
+  };
+  return u32x4{two(w.x, std::false_type{}), two(w.x, std::true_type{}), two(w.y, std::false_type{}), two(w.y, std::true_type{})};
 }
 __device__ __forceinline__ float absmax8(const u32x4 w) {
   const float a = fmaxf(fmaxf(fabsf(bf16_lo(w.x)), fabsf(bf16_hi(w.x))), fmaxf(fabsf(bf16_lo(w.y)), fabsf(bf16_hi(w.y))));

@@ -124,4 +124,41 @@ int launch_attn(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_
                 const uint16_t *res = nullptr, AttnOperand *operand = nullptr,
                 const AttnKV *ready = nullptr);
 
+// cache.hip
+// The pages of a cache as its kernels see them (validated: see check_cache in api.hip)
+struct CacheView {
+  int n_seq, kv_heads, head_dim, page_shift, n_pages, max_pages;
+  bool e4m3;
+  const int32_t *table;   // [n_seq][max_pages]
+};
+int launch_cache_write(const CacheView &cv, const litevggt_cache &c, const uint16_t *k, int64_t k_stride, const uint16_t *v,
+                       int64_t v_stride, const int32_t *off, const int32_t *pos, int n, int qk_norm, hipStream_t st);
+int launch_cache_read(const CacheView &cv, const litevggt_cache &c, const int32_t *first, const int32_t *off, uint16_t *k,
+                      int64_t k_stride, uint16_t *v, int64_t v_stride, int n, hipStream_t st);
+
+// attn_kv.hip
+// Attention of rows of one set over keys of another.  Strides in elements.
+struct KvAttnArgs {
+  const uint16_t *q;
+  uint16_t *o;
+  int64_t q_stride, o_stride;
+  const int32_t *q_off;         // [n_seq + 1]
+  int n_q, n_seq, heads, kv_heads, head_dim;
+  float scale;
+  int qk_norm;                  // of q
+  int frame;                    // > 0: a query sees the keys up to the end of its frame
+  // keys of sequence s: rows k_begin[s] .. k_end[s] - 1 of k and v or, with pages, positions 0 .. k_end[s] - 1 of the cache
+  const void *k, *v;
+  int64_t k_stride, v_stride;
+  const int32_t *k_begin, *k_end;
+  int n_kv;                     // rows of k and v
+  bool paged;
+  CacheView cv;
+  const uint8_t *k_scale, *v_scale;
+};
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys);
+int launch_kv_attn(const KvAttnArgs &a, void *ws, hipStream_t st);
+// k normalised per head (row stride in elements) into rows of kv_heads * head_dim
+int launch_norm_rows(const uint16_t *k, int64_t k_stride, int n, int kv_heads, int head_dim, uint16_t *out, hipStream_t st);
+
 }  // namespace lv
