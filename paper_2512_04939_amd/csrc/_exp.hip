@@ -1,0 +1,1125 @@
+// Attention of the rows of one set over the keys of another: new tokens over a paged cache, queries over an encoder's states.
+//
+//   o_r = sum_t w_rt v_t / sum_t w_rt,   w_rt = exp2(c q_r.k_t - R_r),   c = scale * log2(e)
+//
+// for any reference R_r, in one pass over the keys: the reference of a row is raised, and what has been summed so far is
+// scaled, when a sum passes 2^40 (a score lies 40 binades above the reference).  Sums and references are per row and fp32.
+//
+// A row is a (query token, head) pair; the heads that share a kv head are rows of one block, so K and V are read once for
+// all of them.  Two kernels: k_kv_attn_few has blocks of 32 rows whose four waves take every fourth tile of 32 keys
+// each (a few rows over many keys: bound by reading K and V); k_kv_attn_many has 32 or 64 rows per wave and 64-key stages of K and V in
+// LDS that all four waves read (bound by MFMA and VALU issue).  In both a long key axis is cut into pieces
+// that different workgroups take; k_kv_attn_join puts their sums together.
+//
+// Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
+// weights already lie as the B operand of O^T += V^T P^T.  K and V lie in LDS as rows; V's fragments come out by transposing reads.
+#include "internal.h"
+#include "common.h"
+
+namespace lv {
+
+namespace {
+
+constexpr int kGrp = 16;                 // rows of K or V that are fetched together; a page holds a multiple of it
+constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
+constexpr float kRowRaise = 1.0995116e12f;   // 2^40
+constexpr int kSlotsAll = 512;           // workgroups resident on the chip: 256 CUs, 2 each
+constexpr int kRounds = 3;               // a call's pieces fill these slots at most so often
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+enum class Kv { ROWS, PAGES, E4M3 };
+
+// What a kernel needs of the call, by value
+struct Call {
+  const uint16_t *q;
+  uint16_t *o;
+  int64_t q_stride, o_stride;
+  const int32_t *q_off, *k_begin, *k_end;
+  int n_q, n_seq, heads, kv_heads, group, qk_norm, frame, n_kv;
+  float c;
+  const char *k, *v;
+  int64_t k_stride, v_stride;            // bytes
+  const uint8_t *k_scale, *v_scale;
+  const int32_t *table;
+  int page_shift, n_pages, max_pages;
+  int rows_per_block, tile;              // rows of a block, keys of a tile (the unit of cutting): powers of two
+  int block_shift, tile_shift;
+  int target;                            // pieces to aim at; 0: nothing is cut
+  float *part;                           // [slot][rows_per_block][D] sums
+  float2 *part_ml;                       // [slot][rows_per_block] reference, sum of weights
+  int slots;
+};
+
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+struct SeqInfo {
+  int q0, nq, k0, nk;      // its queries, its keys
+  int p0;                  // position of its first query
+  int blocks, tiles;
+};
+
+__device__ __forceinline__ SeqInfo seq_info(const Call &a, int s) {
+  SeqInfo r;
+  r.q0 = min(max(a.q_off[s], 0), a.n_q);
+  r.nq = min(max(a.q_off[s + 1], r.q0), a.n_q) - r.q0;
+  const int end = a.k_end[s];
+  if (a.table) {
+    const int64_t most = (int64_t)a.max_pages << a.page_shift;
+    r.k0 = 0;
+    r.nk = (int)min((int64_t)max(end, 0), most);
+    r.p0 = max(end, 0) - r.nq;
+  } else {
+    r.k0 = min(max(a.k_begin[s], 0), a.n_kv);
+    r.nk = min(max(end, r.k0), a.n_kv) - r.k0;
+    r.p0 = 0;
+  }
+  r.blocks = (int)(((uint32_t)(r.nq * a.group) + a.rows_per_block - 1) >> a.block_shift);
+  r.tiles = (int)(((uint32_t)r.nk + a.tile - 1) >> a.tile_shift);
+  return r;
+}
+
+// Keys that the row of query i of a sequence sees (all up to this one)
+__device__ __forceinline__ int limit_of(const Call &a, const SeqInfo &q, int i) {
+  if (a.frame <= 0) return q.nk;
+  const int p = q.p0 + i;
+  if (p < 0) return 0;
+  return (int)min((uint32_t)q.nk, ((uint32_t)p / (uint32_t)a.frame + 1u) * (uint32_t)a.frame);   // (below 2^32)
+}
+
+__device__ __forceinline__ int wave_sum_int(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// How the keys are cut: the tiles of a piece.  Every wave works it out from the lengths, the same in all of them.  A
+// candidate per lane: its pieces' number, and from that how long the call would take in tiles (rounds of the
+// chip's slots, each as long as a piece and what a workgroup costs to start and end).
+__device__ int piece_tiles(const Call &a, int lane) {
+  if (a.target == 0) return 0x7fffffff;
+  double work = 0.0;
+  int most = 0;
+  for (int b = 0; b < a.n_seq; b += 64)
+    if (b + lane < a.n_seq) {
+      const SeqInfo q = seq_info(a, b + lane);
+      work += (double)q.blocks * q.tiles * a.kv_heads;
+      most = max(most, q.blocks ? q.tiles : 0);
+    }
+  work = wave_sum(work);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+  most = __builtin_amdgcn_readfirstlane(most);
+  if (most <= 1) return 0x7fffffff;
+  // lane 63: uncut; the others: 1 .. kRounds rounds, 21 steps of 5 % less pieces in each
+  const double pieces = (double)a.target * (1 + lane / 21) / kRounds * (1.0 - 0.04 * (lane % 21));
+  int s = lane == 63 ? most : (int)fmin((double)most, fmax(1.0, ceil(work / pieces)));
+  float units = 0.f;
+  if (a.n_seq <= 16) {
+    for (int i = 0; i < a.n_seq; ++i) {
+      const SeqInfo q = seq_info(a, i);
+      units += (float)q.blocks * a.kv_heads * max((q.tiles + s - 1) / s, 1);
+    }
+  } else {
+    units = (float)(work / s) + 0.5f * a.n_seq * a.kv_heads;
+  }
+  const float cost = ceilf(units / kSlotsAll) * (min(s, most) + 3) + (s < most ? 6.f : 0.f);
+  // the least, the longer pieces of two
+  float best = cost * 4096.f - (float)min(s, 4095);
+  int arg = s;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float v = __shfl_xor(best, o, 64);
+    const int w = __shfl_xor(arg, o, 64);
+    if (v < best || (v == best && w > arg)) {
+      best = v;
+      arg = w;
+    }
+  }
+  return __builtin_amdgcn_readfirstlane(arg);
+}
+
+__device__ __forceinline__ int pieces_of(int tiles, int s) { return max((tiles + s - 1) / s, 1); }
+
+struct Work {
+  int seq, head, block, pieces;
+  int t0, t1;      // its tiles
+  int slot;
+};
+
+// Units of the sequences before `seq` (exclusive), for lane's sequence of a 64-sequence step
+__device__ __forceinline__ int wave_scan(int v, int lane, int &total) {
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  total = __shfl(x, 63, 64);
+  return x - v;
+}
+
+// The u-th piece of the call in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
+// side, and an XCD gets a range of them.
+__device__ bool find_work(const Call &a, int s, int lane, Work &w, SeqInfo &info) {
+  const int nb = gridDim.x;
+  int total = 0;
+  for (int b = 0; b < a.n_seq; b += 64) {
+    int u = 0;
+    if (b + lane < a.n_seq) {
+      const SeqInfo q = seq_info(a, b + lane);
+      u = q.blocks * a.kv_heads * pieces_of(q.tiles, s);
+    }
+    total += wave_sum_int(u);
+  }
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int per = (total + kXcd - 1) / kXcd, x = blockIdx.x % kXcd, y = blockIdx.x / kXcd;
+  const int u = __builtin_amdgcn_readfirstlane(x * per + y);
+  if (y >= per || u >= total || u >= nb) return false;
+  int before = 0;
+  for (int b = 0; b < a.n_seq; b += 64) {
+    int mine = 0;
+    if (b + lane < a.n_seq) {
+      const SeqInfo q = seq_info(a, b + lane);
+      mine = q.blocks * a.kv_heads * pieces_of(q.tiles, s);
+    }
+    int sum;
+    const int start = before + wave_scan(mine, lane, sum);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= start && u < start + mine);
+    if (hit) {
+      const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
+      w.seq = b + j;
+      const int local = u - __builtin_amdgcn_readlane(start, j);
+      info = seq_info(a, w.seq);
+      w.pieces = pieces_of(info.tiles, s);
+      const int per_head = w.pieces * info.blocks, len = (info.tiles + w.pieces - 1) / w.pieces;
+      w.head = local / per_head;
+      const int piece = (local - w.head * per_head) / info.blocks;
+      w.block = local - (w.head * w.pieces + piece) * info.blocks;
+      w.t0 = min(piece * len, info.tiles);
+      w.t1 = min(w.t0 + len, info.tiles);
+      w.slot = u;
+      // (scalars from here on, whatever they were worked out with)
+      w.seq = scalar(w.seq);
+      w.head = scalar(w.head);
+      w.block = scalar(w.block);
+      w.pieces = scalar(w.pieces);
+      w.t0 = scalar(w.t0);
+      w.t1 = scalar(w.t1);
+      info.q0 = scalar(info.q0);
+      info.nq = scalar(info.nq);
+      info.k0 = scalar(info.k0);
+      info.nk = scalar(info.nk);
+      info.p0 = scalar(info.p0);
+      return true;
+    }
+    before += sum;
+  }
+  return false;
+}
+
+// ---------------------------------------------------------------------------------------
+// Tiles in LDS: 32 keys, rows of D bf16 channels as they lie, their 16-byte pieces moved by an exclusive or with bits of
+// the row so that neither the rows that 16 lanes read K fragments from nor the four that V's transposing reads take
+// 64 bytes each from share banks.
+template <int D>
+struct Tile {
+  static constexpr int kRow = D * 2;                  // bytes
+  static constexpr int kPieces = D / 8;               // 16-byte pieces of a row
+  static constexpr int kRowsPer = 64 / kPieces;       // rows that one fetch of a wave brings (1 KB)
+  static constexpr int kFetches = kGrp / kRowsPer;    // fetches of a group of 16 rows
+  static __device__ __forceinline__ int k_xor(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int v_xor(int row) { return D == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
+};
+
+// 16-byte pieces from global memory straight into LDS at `lds` + 16 * lane.  What lies beyond the range of `rsrc` arrives
+// as zeros.  Not waited for: vmcnt.  (The wait states are for a scalar register that a VALU instruction has just written.)
+__device__ __forceinline__ void fetch_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)),
+               "v"(off), "s"(rsrc)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ u32x4 uniform_rsrc(const char *base, int bytes) {
+  const uint64_t b = (uint64_t)base;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)),
+               (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
+}
+
+// Where a group of 16 keys of one head lies: the first row of K and V, and the bytes of each that exist (0: none)
+struct Group {
+  const char *k, *v;
+  int k_bytes, v_bytes;
+  int64_t row;   // pages: rows before it
+};
+
+template <Kv KV, int D>
+__device__ __forceinline__ Group group_at(const Call &a, int head, int k0, int key, int end, int page) {
+  constexpr int row_bytes = KV == Kv::E4M3 ? D : 2 * D;
+  const int rows = min(scalar(max(end - key, 0)), kGrp);     // (in one they become a vector instruction, and all that hangs on it)
+  Group g;
+  if constexpr (KV == Kv::ROWS) {
+    g.row = (int64_t)k0 + key;
+    g.k = a.k + g.row * a.k_stride + head * row_bytes;
+    g.v = a.v + g.row * a.v_stride + head * row_bytes;
+    g.k_bytes = rows ? (int)((rows - 1) * a.k_stride) + row_bytes : 0;
+    g.v_bytes = rows ? (int)((rows - 1) * a.v_stride) + row_bytes : 0;
+  } else {
+    const int64_t id = max(page, 0);
+    g.row = ((id * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+    g.k = a.k + g.row * row_bytes;
+    g.v = a.v + g.row * row_bytes;
+    g.k_bytes = g.v_bytes = page >= 0 ? rows * row_bytes : 0;
+  }
+  return g;
+}
+
+// The page of position `key`: -1 where it is none
+__device__ __forceinline__ int page_at(const Call &a, int seq, int64_t key) {
+  if ((key >> a.page_shift) >= a.max_pages) return -1;
+  const int id = a.table[(int64_t)seq * a.max_pages + (key >> a.page_shift)];
+  return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
+}
+
+// A lane's offsets from a group's first row in its fetches, bf16
+template <int D>
+struct Offsets {
+  uint32_t k[Tile<D>::kFetches], v[Tile<D>::kFetches];
+  __device__ __forceinline__ void init(int lane, int64_t k_stride, int64_t v_stride) {
+    using T = Tile<D>;
+#pragma unroll
+    for (int j = 0; j < T::kFetches; ++j) {
+      const int row = j * T::kRowsPer + lane / T::kPieces, p = lane % T::kPieces;
+      k[j] = (uint32_t)(row * (int)k_stride + (p ^ T::k_xor(row)) * 16);
+      v[j] = (uint32_t)(row * (int)v_stride + (p ^ T::v_xor(row)) * 16);
+    }
+  }
+};
+
+// The group's rows on their way into LDS (bf16)
+template <int D>
+__device__ __forceinline__ void fetch_group(const Group &g, const Offsets<D> &off, uint32_t k_lds, uint32_t v_lds) {
+  const u32x4 rk = uniform_rsrc(g.k, g.k_bytes), rv = uniform_rsrc(g.v, g.v_bytes);
+#pragma unroll
+  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(rk, off.k[j], k_lds + j * 1024);
+#pragma unroll
+  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(rv, off.v[j], v_lds + j * 1024);
+}
+
+// E4M3: a group's codes and exponents in registers, then as bf16 in LDS.  D = 64: one load of a wave has all 16 rows.
+template <int D>
+struct Codes {
+  static constexpr int kLoads = D / 64;
+  u32x4 k[kLoads], v[kLoads];
+  uint32_t ks[kLoads], vs[kLoads];
+  __device__ __forceinline__ void load(const Call &a, const Group &g, int lane) {
+    constexpr int per = D / 16, rows = 64 / per;   // 16-byte pieces of a row, rows of a load
+    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)g.k, 0, __builtin_amdgcn_readfirstlane(g.k_bytes), 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void *)g.v, 0, __builtin_amdgcn_readfirstlane(g.v_bytes), 0x00020000);
+    const int n = __builtin_amdgcn_readfirstlane(g.k_bytes / D);
+    const __amdgpu_buffer_rsrc_t sk = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_scale + g.row), 0, n, 0x00020000);
+    const __amdgpu_buffer_rsrc_t sv = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_scale + g.row), 0, n, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int off = j * 1024 + lane * 16, row = j * rows + lane / per;
+      k[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
+      v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+      ks[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sk, row, 0, 0);
+      vs[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, row, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void store(char *k_lds, char *v_lds, int lane) const {
+    using T = Tile<D>;
+    constexpr int per = D / 16, rows = 64 / per;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int row = j * rows + lane / per, p = 2 * (lane % per);
+      const float a = __uint_as_float(ks[j] << 23), b = __uint_as_float(vs[j] << 23);
+      *(u32x4 *)(k_lds + row * T::kRow + ((p ^ T::k_xor(row)) * 16)) = dequant8(u32x2{k[j].x, k[j].y}, a);
+      *(u32x4 *)(k_lds + row * T::kRow + (((p + 1) ^ T::k_xor(row)) * 16)) = dequant8(u32x2{k[j].z, k[j].w}, a);
+      *(u32x4 *)(v_lds + row * T::kRow + ((p ^ T::v_xor(row)) * 16)) = dequant8(u32x2{v[j].x, v[j].y}, b);
+      *(u32x4 *)(v_lds + row * T::kRow + (((p + 1) ^ T::v_xor(row)) * 16)) = dequant8(u32x2{v[j].z, v[j].w}, b);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------------------
+// QB blocks of 32 rows of a wave
+template <int D, int QB>
+struct Rows {
+  bf16x8 q[QB][D / 16];
+  f32x16 o[QB][D / 32];     // O^T: a lane's row, channels 32 dt + 8 (r / 4) + 4 h + r % 4
+  float l[QB], ref[QB];     // sum of this lane half's weights, the row's reference (both halves the same)
+  int lim[QB];              // keys the row sees
+
+  // rows first .. first + 32 QB - 1 of the (sequence, kv head); those beyond n_rows repeat the last
+  __device__ __forceinline__ void load(const Call &a, const SeqInfo &s, int head, int first, int lane) {
+    const int n_rows = s.nq * a.group;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+      const int r = min(first + b * 32 + (lane & 31), n_rows - 1);
+      const int i = (int)((uint32_t)r / (uint32_t)a.group), g = r - i * a.group;
+      const uint16_t *p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D + (lane >> 5) * 8;
+      u32x4 w[D / 16];
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) w[j] = *(const u32x4 *)(p + 16 * j);
+      if (a.qk_norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) ss += sumsq8(w[j]);
+        ss += __shfl_xor(ss, 32, 64);
+        const float f = 1.0f / sqrtf(ss * (1.0f / D) + kQkEps);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) w[j] = scale8(w[j], f);
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) q[b][j] = __builtin_bit_cast(bf16x8, w[j]);
+      lim[b] = limit_of(a, s, i);
+      l[b] = 0.f;
+      ref[b] = kUnset;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[b][dt][e] = 0.f;
+    }
+  }
+
+  // one tile of 32 keys from key0 on, K and V rows at k_lds and v_lds.  shut: bit i: the i-th 16 keys are not held.
+  // MASK: some row does not see some of the keys.
+  template <bool MASK>
+  __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int shut, int lane) {
+    using T = Tile<D>;
+    const int h = lane >> 5, kr = lane & 31;
+    f32x16 s[QB];
+    {
+      bf16x8 kf[D / 16];
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        kf[j] = __builtin_bit_cast(bf16x8, *(const u32x4 *)(k_lds + kr * T::kRow + (((2 * j + h) ^ T::k_xor(kr)) * 16)));
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+        f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], q[b][j], acc, 0, 0, 0);
+        s[b] = acc;
+      }
+    }
+    // V fragments: [16 keys][32 channels], two halves of 8 keys each
+    u32x4 vf[2][D / 32];
+    {
+      const int row = 4 * h + (lane >> 2 & 3);
+      const char *p = v_lds + row * T::kRow + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const char *pd = p + ((dt * 64) ^ (T::v_xor(row) * 16));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(pd + u * 16 * T::kRow)));
+          const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(pd + u * 16 * T::kRow + 8 * T::kRow)));
+          vf[u][dt] = u32x4{x.x, x.y, y.x, y.y};
+        }
+      }
+    }
+    bool wild = false;       // MASK: some V entry is not finite
+    if constexpr (MASK) {
+#pragma unroll
+      for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = key0 + (r >> 2) * 8 + 4 * h + (r & 3);
+          if (key >= lim[b] || (shut >> (r >> 3) & 1)) s[b][r] = -INFINITY;
+        }
+      // a weight of 0 times an infinity or NaN would reach rows that do not see that key: such entries are taken out
+      // here and added below to the rows that do
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = vf[u][dt][i];
+            const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+            wild |= (lo | hi) != 0u;
+            vf[u][dt][i] = w & ~(lo | hi);
+          }
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+      uint32_t w[8];
+      float sum0, sum1;
+      auto weights = [&]() {
+        sum0 = sum1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][2 * e], c, -ref[b]));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][2 * e + 1], c, -ref[b]));
+          w[e] = pack_bf16(p0, p1);
+          sum0 += p0;
+          sum1 += p1;
+        }
+      };
+      weights();
+      if (__builtin_amdgcn_ballot_w64(!(l[b] + (sum0 + sum1) <= kRowRaise)) != 0) {
+        float top = s[b][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = fmaxf(ref[b], top * c), f = __builtin_amdgcn_exp2f(ref[b] - to);
+        ref[b] = to;
+        l[b] *= f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[b][dt][r] *= f;
+        weights();
+      }
+      l[b] += sum0 + sum1;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]});
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][dt]), p, o[b][dt], 0, 0, 0);
+      }
+    }
+    if constexpr (MASK)
+      if (__builtin_amdgcn_ballot_w64(wild) != 0) add_wild(v_lds, key0, shut, lane);
+  }
+
+  // entries of V that are not finite, to the rows that see their keys
+  __device__ __forceinline__ void add_wild(const char *v_lds, int key0, int shut, int lane) {
+    using T = Tile<D>;
+    const int h = lane >> 5;
+    for (int t = 0; t < 32; ++t) {
+      if (shut >> (t >> 4) & 1) continue;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int byte = (dt * 64 + i * 16 + h * 8) ^ (T::v_xor(t) * 16);
+          const u32x2 w = *(const u32x2 *)(v_lds + t * T::kRow + byte);
+          const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u)
+#pragma unroll
+              for (int b = 0; b < QB; ++b)
+                if (key0 + t < lim[b]) o[b][dt][4 * i + e] += x[e];
+        }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------------------
+// Few rows.  A workgroup has 32 rows of a (sequence, kv head) and a piece of its keys, in tiles of 128: wave w takes the w-th 32
+// keys of each, through LDS of its own, so nobody waits for anybody before the end.  bf16: two
+// tiles in LDS, the next one on its way while one is computed with; E4M3: the next tile's codes on their way in registers, turned
+// into bf16 in LDS.
+template <Kv KV, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_few(Call a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  using T = Tile<D>;
+  constexpr int kTile = 32 * T::kRow;          // bytes of a tile's K or V
+  constexpr int kStages = KV == Kv::E4M3 ? 1 : 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Work w;
+  SeqInfo s;
+  if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
+  const int n_rows = s.nq * a.group, row0 = w.block * 32;
+  const int last = scalar(limit_of(a, s, min(row0 + 31, n_rows - 1) / a.group));     // keys that some row sees
+  const int first = scalar(limit_of(a, s, row0 / a.group));                          // keys that every row sees
+  const int begin = w.t0 * 128 + wave * 32, end = (int)min((uint32_t)w.t1 * 128u, (uint32_t)last);
+  const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 127) / 128 : 0);     // the wave's tiles
+
+  char *const mine = lds + wave * (2 * kStages * kTile);
+  const uint32_t mine_at = __builtin_amdgcn_readfirstlane(lds_addr(mine));
+  Offsets<D> off;
+  if constexpr (KV != Kv::E4M3) off.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, KV == Kv::ROWS ? a.v_stride : T::kRow);
+  int ids[2] = {0, 0};               // lane j: the pages of the two groups of tile j of 64
+  uint64_t holes = 0;
+  auto look_up = [&](int i) {        // tiles i .. i + 63
+    if constexpr (KV != Kv::ROWS) {
+      const int64_t key = (int64_t)begin + (int64_t)(i + lane) * 128;
+      ids[0] = key < end ? page_at(a, w.seq, key) : -1;
+      ids[1] = key + kGrp < end ? page_at(a, w.seq, key + kGrp) : -1;
+      holes = __builtin_amdgcn_ballot_w64((key < end && ids[0] < 0) || (key + kGrp < end && ids[1] < 0));
+    }
+  };
+  Codes<D> codes[2];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int key = begin + i * 128 + g * kGrp;
+      const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(ids[g], i & 63);
+      const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
+      if constexpr (KV == Kv::E4M3) codes[g].load(a, at, lane);
+      else {
+        const uint32_t to = mine_at + (i % kStages) * (2 * kTile) + g * kGrp * T::kRow;
+        fetch_group<D>(at, off, to, to + kTile);
+      }
+    }
+  };
+  Rows<D, 1> rows;
+  rows.load(a, s, w.head, row0, lane);
+  if (n > 0) {
+    look_up(0);
+    fetch(0);
+    uint64_t shut_now = holes;
+    for (int i = 0; i < n; ++i) {
+      char *kt = mine + (i % kStages) * (2 * kTile);
+      int shut = 0;
+      if (KV != Kv::ROWS && (shut_now >> (i & 63) & 1))
+        shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
+      if constexpr (KV == Kv::E4M3) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) codes[g].store(kt + g * kGrp * T::kRow, kt + kTile + g * kGrp * T::kRow, lane);
+      }
+      if (i + 1 < n) {
+        if ((i + 1) % 64 == 0) look_up(i + 1);
+        fetch(i + 1);
+        if constexpr (KV != Kv::E4M3) wait_vm<4 * T::kFetches>();
+      } else if constexpr (KV != Kv::E4M3) {
+        wait_vm<0>();
+      }
+      const int key0 = begin + i * 128;
+      if (shut || key0 + 32 > first) rows.template tile<true>(kt, kt + kTile, a.c, key0, shut, lane);
+      else rows.template tile<false>(kt, kt + kTile, a.c, key0, 0, lane);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile has been read: its place may be filled again
+      shut_now = holes;
+    }
+  }
+
+  // the four waves' sums: [wave][32 rows][D] and their references and sums of weights
+  __syncthreads();
+  float *po = (float *)lds;
+  __shared__ float2 ml[4][32];
+  {
+    const float l = rows.l[0] + __shfl_xor(rows.l[0], 32, 64);
+    if (lane < 32) ml[wave][lane] = float2{rows.ref[0], l};
+    float *p = po + (wave * 32 + (lane & 31)) * D;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = dt * 32 + i * 8 + (lane >> 5) * 4;
+        *(f32x4 *)(p + (ch ^ ((lane & 15) * 4))) = f32x4{rows.o[0][dt][4 * i], rows.o[0][dt][4 * i + 1], rows.o[0][dt][4 * i + 2], rows.o[0][dt][4 * i + 3]};
+      }
+  }
+  __syncthreads();
+  for (int i = tid; i < 32 * (D / 4); i += 256) {
+    const int r = i / (D / 4), ch = i % (D / 4) * 4;
+    if (row0 + r >= n_rows) break;
+    float top = ml[0][r].x;
+#pragma unroll
+    for (int x = 1; x < 4; ++x) top = fmaxf(top, ml[x][r].x);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = __builtin_amdgcn_exp2f(ml[x][r].x - top);
+      const f32x4 y = *(const f32x4 *)(po + (x * 32 + r) * D + (ch ^ ((r & 15) * 4)));
+      l += ml[x][r].y * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+    }
+    if (w.pieces > 1) {
+      const int64_t at = (int64_t)w.slot * 32 + r;
+      *(f32x4 *)(a.part + at * D + ch) = sum;
+      if (ch == 0) a.part_ml[at] = float2{top, l};
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;     // no key seen: zeros
+      const int rr = row0 + r, tok = rr / a.group;
+      uint16_t *p = a.o + (int64_t)(s.q0 + tok) * a.o_stride + (w.head * a.group + rr - tok * a.group) * D + ch;
+      *(u32x2 *)p = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Many rows.  A workgroup has 256 rows, 64 per wave, and walks a piece of the keys in stages of 64, of which wave w fetches the
+// w-th 16 (a stage is four groups, a wave needs one page number for it).  bf16: a ring of four stages in LDS, filled
+// straight from memory; E4M3: three stages of bf16 in LDS, the codes of the next one in registers.
+//
+// A wave's two blocks of 32 rows run half a step apart, so that one's weights (VALU) are taken while the other's products (MFMA) run:
+//   A(t): scores of block 1 (tile t) | K(t + 1) is read | output of block 1 (t - 1) | V(t) is read;  weights of block 0 (t)
+//   B(t): scores of block 0 (t + 1), output of block 0 (t);                                          weights of block 1 (t)
+// K's and V's fragments are read once for both blocks, half a phase before their first use, into the registers that the products
+// before have just been issued from.
+template <Kv KV, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1))) void k_kv_attn_many(Call a) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  using T = Tile<D>;
+  constexpr int kHalf = 64 * T::kRow;                     // bytes of a stage's K or V
+  constexpr int kStages = KV == Kv::E4M3 ? 3 : 4;
+  constexpr int kFetch = 2 * T::kFetches;                 // fetches of a wave and stage
+  constexpr int KF = D / 16, DT = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Work w;
+  SeqInfo s;
+  if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
+  const int n_rows = s.nq * a.group, block0 = w.block * 256, row0 = block0 + wave * 64;
+  const int last = scalar(limit_of(a, s, min(block0 + 255, n_rows - 1) / a.group));
+  const bool live = row0 < n_rows;
+  const int first = live ? scalar(limit_of(a, s, row0 / a.group)) : 0;       // keys that every row of the wave sees
+  const int begin = w.t0 * 64, end = (int)min((uint32_t)w.t1 * 64u, (uint32_t)last);
+  const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 63) / 64 : 0);
+
+  Offsets<D> off;
+  if constexpr (KV != Kv::E4M3) off.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, KV == Kv::ROWS ? a.v_stride : T::kRow);
+  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + wave * (kGrp * T::kRow);
+  int own = 0, shuts = 0;        // lane j: stage j of 64: the page of this wave's group; bits of the groups that are not held
+  uint64_t holes = 0;
+  auto look_up = [&](int i) __attribute__((always_inline)) {
+    if constexpr (KV != Kv::ROWS) {
+      const int64_t key = (int64_t)begin + (int64_t)(i + lane) * 64;
+      shuts = 0;
+      own = -1;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const bool in = key + g * kGrp < end;
+        const int id = in ? page_at(a, w.seq, key + g * kGrp) : -1;
+        if (g == wave) own = id;
+        if (in && id < 0) shuts |= 1 << g;
+      }
+      holes = __builtin_amdgcn_ballot_w64(shuts != 0);
+    }
+  };
+  Codes<D> codes;
+  auto fetch = [&](int i) __attribute__((always_inline)) {      // beyond the last stage: nothing is read, the counts stay
+    const int key = begin + i * 64 + wave * kGrp;
+    const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i & 63);
+    const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
+    if constexpr (KV == Kv::E4M3) codes.load(a, at, lane);
+    else fetch_group<D>(at, off, base + (i % kStages) * (2 * kHalf), base + (i % kStages) * (2 * kHalf) + kHalf);
+  };
+  auto put = [&](int i) __attribute__((always_inline)) {
+    char *p = lds + (i % kStages) * (2 * kHalf) + wave * (kGrp * T::kRow);
+    codes.store(p, p + kHalf, lane);
+  };
+  uint64_t now = 0, ahead = 0;      // holes of the 64 stages that are computed with, that are fetched
+  int now_shuts = 0;
+  // this wave's part of stage i + 1 has landed; behind the barrier all of it, and nobody reads stage i - 1 any more
+  auto publish = [&](int i) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (KV == Kv::E4M3) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    else wait_vm<(kStages - 3) * kFetch>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    const int next = i + 3;
+    if constexpr (KV == Kv::E4M3) put(i + 2);
+    if (KV != Kv::ROWS && next % 64 == 0 && next < n) {
+      look_up(next);
+      ahead = holes;
+    }
+    fetch(next);
+  };
+  auto start = [&]() __attribute__((always_inline)) {
+    look_up(0);
+    ahead = now = holes;
+    now_shuts = shuts;
+    fetch(0);
+    if constexpr (KV == Kv::E4M3) {
+      put(0);
+      fetch(1);
+      put(1);
+      fetch(2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else {
+      fetch(1);
+      fetch(2);
+      wait_vm<2 * kFetch>();
+    }
+    __builtin_amdgcn_s_barrier();
+  };
+  if (!live) {      // no rows: the wave moves its share of the stages
+    if (n > 0) {
+      start();
+      for (int i = 0; i < n; ++i) publish(i);
+      wait_vm<0>();
+    }
+    return;
+  }
+  Rows<D, 2> rows;
+  rows.load(a, s, w.head, row0, lane);
+  if (n > 0) {
+    start();
+    f32x16 sacc[2];
+    uint32_t pb[2][8];
+    u32x4 fk[KF], fv[2][DT];
+    const uint32_t lds0 = lds_addr(lds);
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    const int kr = lane & 31, vr = 4 * h + (lane >> 2 & 3);
+    const uint32_t k_lane = lds0 + kr * T::kRow + ((h ^ T::k_xor(kr)) * 16);                       // piece 2 j + h: ^ 32 j
+    const uint32_t v_lane = lds0 + kHalf + vr * T::kRow + T::v_xor(vr) * 16 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;   // channels 32 dt: ^ 64 dt
+    auto tile_at = [&](int t) __attribute__((always_inline)) { return (uint32_t)(((t >> 1) % kStages) * (2 * kHalf) + (t & 1) * 32 * T::kRow); };
+    auto read_k = [&](int t) __attribute__((always_inline)) {
+      const uint32_t p = k_lane + tile_at(t);
+#pragma unroll
+      for (int j = 0; j < KF; ++j) fk[j] = *(lds_u32x4 *)(uintptr_t)(p ^ (j * 32));
+    };
+    auto read_v = [&](int t) __attribute__((always_inline)) {
+      const uint32_t p = v_lane + tile_at(t);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t q = (p ^ (dt * 64)) + u * 16 * T::kRow;
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)q));
+          const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(q + 8 * T::kRow)));
+          fv[u][dt] = u32x4{x.x, x.y, y.x, y.y};
+        }
+    };
+    auto scores = [&](int b) __attribute__((always_inline)) {
+      f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KF; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fk[j]), rows.q[b][j], acc, 0, 0, 0);
+      sacc[b] = acc;
+    };
+    auto output = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          rows.o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fv[u][dt]), p, rows.o[b][dt], 0, 0, 0);
+      }
+    };
+    float sum0, sum1;
+    auto weights = [&](int b, int half) __attribute__((always_inline)) {
+      if (half == 0) sum0 = sum1 = 0.f;
+#pragma unroll
+      for (int e = 4 * half; e < 4 * half + 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -rows.ref[b]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -rows.ref[b]));
+        pb[b][e] = pack_bf16(p0, p1);
+        sum0 += p0;
+        sum1 += p1;
+      }
+    };
+    auto recipe = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < KF; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x400, D == 64 ? 2 : 1, 0);    // exp2
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                  // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 5 : 3, 0);    // fused multiply-add, pack, add
+      }
+    };
+    // block b's weights become part of its sums, with the references raised first where a sum went past 2^40
+    auto settle = [&](int b) __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      rows.l[b] += sum0 + sum1;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto phase_a = [&](auto head, auto tail, int t) __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      scores(1);
+      weights(0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!decltype(tail)::value) read_k(t + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!decltype(head)::value) output(1);
+      weights(0, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      read_v(t);
+      settle(0);
+    };
+    auto phase_b = [&](auto tail) __attribute__((always_inline)) {
+      if constexpr (!decltype(tail)::value) scores(0);
+      weights(1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      output(0);
+      weights(1, 1);
+      settle(1);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const int plain = first > begin ? (first - begin) >> 6 : 0;     // stages of which every row of the wave sees every key
+    int i = 0;
+    {
+      // the stages from i on whose keys are all there and seen
+      int j = min(plain, n);
+      if constexpr (KV != Kv::ROWS) {
+        const uint64_t next = now >> (i & 63);
+        j = min(j, min((i | 63) + 1, next ? i + __ffsll((unsigned long long)next) - 1 : n));
+      }
+      j = __builtin_amdgcn_readfirstlane(j);
+      if (j > i) {
+        read_k(2 * i);
+        scores(0);
+        phase_a(Yes{}, No{}, 2 * i);
+#pragma unroll 1
+        for (; i < j - 1; ++i) {
+          asm volatile("" : "+v"(sacc[1]));   // (the same phase follows the loop: its instructions would be drawn before the branch)
+          phase_b(No{});
+          publish(i);
+          phase_a(No{}, No{}, 2 * i + 1);
+          phase_b(No{});
+          phase_a(No{}, No{}, 2 * i + 2);
+        }
+        phase_b(No{});
+        publish(i);
+        phase_a(No{}, Yes{}, 2 * i + 1);
+        phase_b(Yes{});
+        output(1);
+      } else {
+        const int shut = KV != Kv::ROWS ? __builtin_amdgcn_readlane(now_shuts, i & 63) : 0;
+        const char *kt = lds + (i % kStages) * (2 * kHalf);
+        publish(i);
+      }
+      if (++i % 64 == 0) {
+        now = ahead;
+        now_shuts = shuts;
+      }
+    }
+    wait_vm<0>();     // nothing may land after the workgroup ends
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int r = wave * 64 + b * 32 + (lane & 31);
+    const int rr = block0 + r, tok = rr / a.group;
+    const float l = rows.l[b] + __shfl_xor(rows.l[b], 32, 64);
+    if (rr >= n_rows) continue;
+    if (w.pieces > 1) {
+      const int64_t at = (int64_t)w.slot * 256 + r;
+      if (lane < 32) a.part_ml[at] = float2{rows.ref[b], l};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(f32x4 *)(a.part + at * D + dt * 32 + i * 8 + h * 4) =
+              f32x4{rows.o[b][dt][4 * i], rows.o[b][dt][4 * i + 1], rows.o[b][dt][4 * i + 2], rows.o[b][dt][4 * i + 3]};
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      uint16_t *p = a.o + (int64_t)(s.q0 + tok) * a.o_stride + (w.head * a.group + rr - tok * a.group) * D + h * 4;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(u32x2 *)(p + dt * 32 + i * 8) = u32x2{pack_bf16(rows.o[b][dt][4 * i] * inv, rows.o[b][dt][4 * i + 1] * inv),
+                                                  pack_bf16(rows.o[b][dt][4 * i + 2] * inv, rows.o[b][dt][4 * i + 3] * inv)};
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// The sums of a row's pieces put together, always in the same order.  A row has D / 4 lanes times SL: each of
+// these takes every SL-th piece (few rows, many pieces), and they meet in LDS.
+template <int D, int SL>
+__global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
+  constexpr int kCh = D / 4, kRowsWg = 256 / (kCh * SL);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int per_token = (a.heads + kRowsWg - 1) / kRowsWg;
+  const int tok = blockIdx.x / per_token;
+  const int piece_len = piece_tiles(a, lane);
+  // the token's sequence and the number of the first piece of it
+  int seq = -1, before = 0;
+  for (int b = 0; b < a.n_seq && seq < 0; b += 64) {
+    int units = 0;
+    bool in = false;
+    if (b + lane < a.n_seq) {
+      const SeqInfo q = seq_info(a, b + lane);
+      units = q.blocks * a.kv_heads * pieces_of(q.tiles, piece_len);
+      in = tok >= q.q0 && tok < q.q0 + q.nq;
+    }
+    int sum;
+    const int start = before + wave_scan(units, lane, sum);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(in);
+    before += sum;
+    if (hit) {
+      const int j = __ffsll((unsigned long long)hit) - 1;
+      seq = b + j;
+      before = __builtin_amdgcn_readlane(start, j);
+    }
+  }
+  if (seq < 0) return;
+  const SeqInfo s = seq_info(a, seq);
+  const int pieces = pieces_of(s.tiles, piece_len);
+  if (pieces == 1) return;          // written already
+  const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
+  const int hq = blockIdx.x % per_token * kRowsWg + in_wg;
+  const bool there = hq < a.heads;
+  const int head = (there ? hq : 0) / a.group, g = (there ? hq : 0) % a.group;
+  const int r = (tok - s.q0) * a.group + g;
+  const int block = r >> a.block_shift, in_block = r & (a.rows_per_block - 1);
+  const int64_t slot0 = before + (int64_t)head * pieces * s.blocks + block;
+  if (slot0 + (int64_t)(pieces - 1) * s.blocks >= a.slots) return;
+  auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
+  float top = kUnset;
+  for (int x = sl; x < pieces; x += SL) top = fmaxf(top, a.part_ml[at(x)].x);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int x = sl; x < pieces; x += SL) {
+    const float2 ml = a.part_ml[at(x)];
+    const float f = __builtin_amdgcn_exp2f(ml.x - top);
+    const f32x4 y = *(const f32x4 *)(a.part + at(x) * D + ch);
+    l += ml.y * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+  }
+  if constexpr (SL > 1) {
+    __shared__ float tops[kRowsWg][SL], ls[kRowsWg][SL];
+    __shared__ f32x4 sums[kRowsWg][SL][kCh];
+    if (ch == 0) {
+      tops[in_wg][sl] = top;
+      ls[in_wg][sl] = l;
+    }
+    sums[in_wg][sl][ch / 4] = sum;
+    __syncthreads();
+    if (sl) return;
+    for (int x = 1; x < SL; ++x) top = fmaxf(top, tops[in_wg][x]);
+    l = 0.f;
+    sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < SL; ++x) {
+      const float f = __builtin_amdgcn_exp2f(tops[in_wg][x] - top);
+      const f32x4 y = sums[in_wg][x][ch / 4];
+      l += ls[in_wg][x] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+    }
+  }
+  if (!there) return;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  *(u32x2 *)(a.o + (int64_t)tok * a.o_stride + hq * D + ch) =
+      u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+}
+
+// K's rows normalised per head, for cross attention with qk_norm
+template <int D>
+__global__ __launch_bounds__(256) void k_norm_rows(const uint16_t *k, int64_t stride, int64_t n_rows, int kv_heads, uint16_t *out) {
+  constexpr int L = D / 8;
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const int p = threadIdx.x % L;
+  const int64_t rr = min(r, n_rows - 1);
+  const u32x4 w = *(const u32x4 *)(k + rr / kv_heads * stride + rr % kv_heads * D + p * 8);
+  float ss = sumsq8(w);
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o, 64);
+  const u32x4 y = scale8(w, 1.0f / sqrtf(ss * (1.0f / D) + kQkEps));
+  if (r < n_rows) *(u32x4 *)(out + r * D + p * 8) = y;
+}
+
+// ---------------------------------------------------------------------------------------
+struct Form {
+  bool few;
+  int rows, tile;
+  int64_t units;     // blocks of the call at most, all heads
+  int target;        // pieces beside these at most
+};
+
+// Which kernel: by the rows that a (sequence, kv head) has on average.
+Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
+  Form f;
+  const int group = heads / kv_heads;
+  const double rows = (double)n_q * group / n_seq;
+  f.few = rows <= 64.0;
+  f.rows = f.few ? 32 : 256;
+  f.tile = f.few ? 128 : 64;
+  f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
+  const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
+  // (blocks that fill the chip several times over leave nothing to gain)
+  const int64_t target = f.units >= 4 * kSlotsAll && !f.few ? 0 : tiles <= 1 ? 0 : kRounds * kSlotsAll;
+  f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
+  return f;
+}
+int64_t slots_of(const Form &f) { return f.units + f.target + kXcd; }
+
+}  // namespace
+
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
+  const Form f = form_of(n_q, n_seq, heads, kv_heads, head_dim, most_keys);
+  if (f.target == 0) return 0;
+  return align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
+}
+
+template <typename K, size_t LDS>
+static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size_t, LDS>, const Call &c, uint32_t grid, hipStream_t st) {
+  if constexpr (LDS > 60000) {     // (a kernel has up to 1 KB beside it)
+    const int rc = allow_dynamic_lds<LDS>((const void *)kernel, done);
+    if (rc) return rc;
+  }
+  kernel<<<dim3(grid), 256, LDS, st>>>(c);
+  return LV_OK;
+}
+
+template <Kv KV, int D>
+static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t st) {
+  constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
+  static std::atomic<uint64_t> d0{0}, d1{0};
+  if (f.few) return go(k_kv_attn_few<KV, D>, d0, std::integral_constant<size_t, KV == Kv::E4M3 ? 2 * tile : 4 * tile>{}, c, grid, st);
+  return go(k_kv_attn_many<KV, D>, d1, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid, st);
+}
+
+int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
+  const int64_t most = x.paged ? (int64_t)x.cv.max_pages << x.cv.page_shift : x.n_kv;
+  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, most);
+  Call c;
+  c.q = x.q;
+  c.o = x.o;
+  c.q_stride = x.q_stride;
+  c.o_stride = x.o_stride;
+  c.q_off = x.q_off;
+  c.k_begin = x.k_begin;
+  c.k_end = x.k_end;
+  c.n_q = x.n_q;
+  c.n_seq = x.n_seq;
+  c.heads = x.heads;
+  c.kv_heads = x.kv_heads;
+  c.group = x.heads / x.kv_heads;
+  c.qk_norm = x.qk_norm;
+  c.frame = x.frame;
+  c.n_kv = x.n_kv;
+  c.c = x.scale * 1.4426950408889634f;
+  c.k = (const char *)x.k;
+  c.v = (const char *)x.v;
+  c.k_stride = x.k_stride * 2;
+  c.v_stride = x.v_stride * 2;
+  c.k_scale = x.k_scale;
+  c.v_scale = x.v_scale;
+  c.table = x.paged ? x.cv.table : nullptr;
+  c.page_shift = x.cv.page_shift;
+  c.n_pages = x.cv.n_pages;
+  c.max_pages = x.cv.max_pages;
+  c.rows_per_block = f.rows;
+  c.tile = f.tile;
+  c.block_shift = __builtin_ctz(f.rows);
+  c.tile_shift = __builtin_ctz(f.tile);
+  c.target = f.target;
+  c.slots = (int)slots_of(f);
+  c.part = (float *)ws;
+  c.part_ml = f.target ? (float2 *)((float *)ws + (size_t)c.slots * f.rows * x.head_dim) : nullptr;
+  const uint32_t grid = (uint32_t)((f.units + f.target + kXcd - 1) / kXcd * kXcd);
+  auto by_kv = [&](auto kv) {
+    constexpr Kv KV = decltype(kv)::value;
+    return x.head_dim == 64 ? launch_form<KV, 64>(f, c, grid, st) : launch_form<KV, 128>(f, c, grid, st);
+  };
+  int rc;
+  if (!x.paged) rc = by_kv(std::integral_constant<Kv, Kv::ROWS>{});
+  else if (!x.cv.e4m3) rc = by_kv(std::integral_constant<Kv, Kv::PAGES>{});
+  else rc = by_kv(std::integral_constant<Kv, Kv::E4M3>{});
+  if (rc) return rc;
+  if (f.target) {
+    auto join = [&](auto kernel, int rows) {
+      kernel<<<dim3((uint32_t)((int64_t)x.n_q * ((x.heads + rows - 1) / rows))), 256, 0, st>>>(c);
+    };
+    if (x.head_dim == 64) f.few ? join(k_kv_attn_join<64, 16>, 1) : join(k_kv_attn_join<64, 1>, 16);
+    else f.few ? join(k_kv_attn_join<128, 8>, 1) : join(k_kv_attn_join<128, 1>, 8);
+  }
+  LV_HIP_CHECK_LAUNCH();
+  return LV_OK;
+}
+
+int launch_norm_rows(const uint16_t *k, int64_t k_stride, int n, int kv_heads, int head_dim, uint16_t *out, hipStream_t st) {
+  const int64_t rows = (int64_t)n * kv_heads;
+  const uint32_t grid = (uint32_t)((rows * (head_dim / 8) + 255) / 256);
+  if (head_dim == 64) k_norm_rows<64><<<dim3(grid), 256, 0, st>>>(k, k_stride, rows, kv_heads, out);
+  else k_norm_rows<128><<<dim3(grid), 256, 0, st>>>(k, k_stride, rows, kv_heads, out);
+  LV_HIP_CHECK_LAUNCH();
+  return LV_OK;
+}
+
+}  // namespace lv

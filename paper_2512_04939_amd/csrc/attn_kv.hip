@@ -44,16 +44,19 @@ struct Call {
   const uint8_t *k_scale, *v_scale;
   const int32_t *table;
   int page_shift, n_pages, max_pages;
-  int rows_per_block, tile;              // rows of a block, keys of a tile (the unit of cutting)
+  int rows_per_block, tile;              // rows of a block, keys of a tile (the unit of cutting): powers of two
+  int block_shift, tile_shift;
   int target;                            // pieces to aim at; 0: nothing is cut
   float *part;                           // [slot][rows_per_block][D] sums
   float2 *part_ml;                       // [slot][rows_per_block] reference, sum of weights
   int slots;
 };
 
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 struct SeqInfo {
   int q0, nq, k0, nk;      // its queries, its keys
-  int64_t p0;              // position of its first query
+  int p0;                  // position of its first query
   int blocks, tiles;
 };
 
@@ -66,23 +69,23 @@ __device__ __forceinline__ SeqInfo seq_info(const Call &a, int s) {
     const int64_t most = (int64_t)a.max_pages << a.page_shift;
     r.k0 = 0;
     r.nk = (int)min((int64_t)max(end, 0), most);
-    r.p0 = (int64_t)end - r.nq;
+    r.p0 = max(end, 0) - r.nq;
   } else {
     r.k0 = min(max(a.k_begin[s], 0), a.n_kv);
     r.nk = min(max(end, r.k0), a.n_kv) - r.k0;
     r.p0 = 0;
   }
-  r.blocks = (int)(((int64_t)r.nq * a.group + a.rows_per_block - 1) / a.rows_per_block);
-  r.tiles = (int)(((int64_t)r.nk + a.tile - 1) / a.tile);
+  r.blocks = (int)(((uint32_t)(r.nq * a.group) + a.rows_per_block - 1) >> a.block_shift);
+  r.tiles = (int)(((uint32_t)r.nk + a.tile - 1) >> a.tile_shift);
   return r;
 }
 
 // Keys that the row of query i of a sequence sees (all up to this one)
 __device__ __forceinline__ int limit_of(const Call &a, const SeqInfo &q, int i) {
   if (a.frame <= 0) return q.nk;
-  const int64_t p = q.p0 + i;
+  const int p = q.p0 + i;
   if (p < 0) return 0;
-  return (int)min((int64_t)q.nk, (p / a.frame + 1) * a.frame);
+  return (int)min((uint32_t)q.nk, ((uint32_t)p / (uint32_t)a.frame + 1u) * (uint32_t)a.frame);   // (below 2^32)
 }
 
 __device__ __forceinline__ int wave_sum_int(int v) {
@@ -140,7 +143,8 @@ __device__ int piece_tiles(const Call &a, int lane) {
 __device__ __forceinline__ int pieces_of(int tiles, int s) { return max((tiles + s - 1) / s, 1); }
 
 struct Work {
-  int seq, head, block, piece, pieces;
+  int seq, head, block, pieces;
+  int t0, t1;      // its tiles
   int slot;
 };
 
@@ -184,16 +188,30 @@ __device__ bool find_work(const Call &a, int s, int lane, Work &w, SeqInfo &info
     const int start = before + wave_scan(mine, lane, sum);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= start && u < start + mine);
     if (hit) {
-      const int j = __ffsll((unsigned long long)hit) - 1;
+      const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
       w.seq = b + j;
       const int local = u - __builtin_amdgcn_readlane(start, j);
-      info = seq_info(a, __builtin_amdgcn_readfirstlane(w.seq));
+      info = seq_info(a, w.seq);
       w.pieces = pieces_of(info.tiles, s);
-      const int per_head = w.pieces * info.blocks;
+      const int per_head = w.pieces * info.blocks, len = (info.tiles + w.pieces - 1) / w.pieces;
       w.head = local / per_head;
-      w.piece = local % per_head / info.blocks;
-      w.block = local % info.blocks;
+      const int piece = (local - w.head * per_head) / info.blocks;
+      w.block = local - (w.head * w.pieces + piece) * info.blocks;
+      w.t0 = min(piece * len, info.tiles);
+      w.t1 = min(w.t0 + len, info.tiles);
       w.slot = u;
+      // (scalars from here on, whatever they were worked out with)
+      w.seq = scalar(w.seq);
+      w.head = scalar(w.head);
+      w.block = scalar(w.block);
+      w.pieces = scalar(w.pieces);
+      w.t0 = scalar(w.t0);
+      w.t1 = scalar(w.t1);
+      info.q0 = scalar(info.q0);
+      info.nq = scalar(info.nq);
+      info.k0 = scalar(info.k0);
+      info.nk = scalar(info.nk);
+      info.p0 = scalar(info.p0);
       return true;
     }
     before += sum;
@@ -218,7 +236,9 @@ struct Tile {
 // 16-byte pieces from global memory straight into LDS at `lds` + 16 * lane.  What lies beyond the range of `rsrc` arrives
 // as zeros.  Not waited for: vmcnt.  (The wait states are for a scalar register that a VALU instruction has just written.)
 __device__ __forceinline__ void fetch_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)),
+               "v"(off), "s"(rsrc)
+               : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -241,7 +261,7 @@ struct Group {
 template <Kv KV, int D>
 __device__ __forceinline__ Group group_at(const Call &a, int head, int k0, int key, int end, int page) {
   constexpr int row_bytes = KV == Kv::E4M3 ? D : 2 * D;
-  const int rows = min(max(end - key, 0), kGrp);
+  const int rows = min(scalar(max(end - key, 0)), kGrp);     // (in one they become a vector instruction, and all that hangs on it)
   Group g;
   if constexpr (KV == Kv::ROWS) {
     g.row = (int64_t)k0 + key;
@@ -299,11 +319,13 @@ struct Codes {
   uint32_t ks[kLoads], vs[kLoads];
   __device__ __forceinline__ void load(const Call &a, const Group &g, int lane) {
     constexpr int per = D / 16, rows = 64 / per;   // 16-byte pieces of a row, rows of a load
-    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)g.k, 0, __builtin_amdgcn_readfirstlane(g.k_bytes), 0x00020000);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void *)g.v, 0, __builtin_amdgcn_readfirstlane(g.v_bytes), 0x00020000);
-    const int n = __builtin_amdgcn_readfirstlane(g.k_bytes / D);
-    const __amdgpu_buffer_rsrc_t sk = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_scale + g.row), 0, n, 0x00020000);
-    const __amdgpu_buffer_rsrc_t sv = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_scale + g.row), 0, n, 0x00020000);
+    auto rsrc = [](const void *p, int bytes) {     // (scalars: a resource in vector registers is a loop over the lanes)
+      const uint64_t b = (uint64_t)p;
+      const uint64_t u = (uint32_t)scalar((int)(uint32_t)b) | (uint64_t)(uint32_t)scalar((int)(b >> 32)) << 32;
+      return __builtin_amdgcn_make_buffer_rsrc((void *)u, 0, scalar(bytes), 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t rk = rsrc(g.k, g.k_bytes), rv = rsrc(g.v, g.v_bytes);
+    const __amdgpu_buffer_rsrc_t sk = rsrc(a.k_scale + g.row, g.k_bytes / D), sv = rsrc(a.v_scale + g.row, g.k_bytes / D);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       const int off = j * 1024 + lane * 16, row = j * rows + lane / per;
@@ -338,12 +360,12 @@ struct Rows {
   int lim[QB];              // keys the row sees
 
   // rows first .. first + 32 QB - 1 of the (sequence, kv head); those beyond n_rows repeat the last
-  __device__ __forceinline__ void load(const Call &a, const SeqInfo &s, int head, int64_t first, int lane) {
-    const int64_t n_rows = (int64_t)s.nq * a.group;
+  __device__ __forceinline__ void load(const Call &a, const SeqInfo &s, int head, int first, int lane) {
+    const int n_rows = s.nq * a.group;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-      const int64_t r = min(first + b * 32 + (lane & 31), n_rows - 1);
-      const int i = (int)(r / a.group), g = (int)(r % a.group);
+      const int r = min(first + b * 32 + (lane & 31), n_rows - 1);
+      const int i = (int)((uint32_t)r / (uint32_t)a.group), g = r - i * a.group;
       const uint16_t *p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D + (lane >> 5) * 8;
       u32x4 w[D / 16];
 #pragma unroll
@@ -369,10 +391,9 @@ struct Rows {
     }
   }
 
-  // one tile of 32 keys from key0 on, K and V rows at k_lds and v_lds.  shut: bit i: the i-th 16 keys are not held.
-  // MASK: some row does not see some of the keys.
-  template <bool MASK>
-  __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int shut, int lane) {
+  // one tile of 32 keys from key0 on, K and V rows at k_lds and v_lds.  shut: bit i: the i-th 16 keys are not held (their rows
+  // are zeros).  cut: some row does not see some of the keys.
+  __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int shut, bool cut, int lane) {
     using T = Tile<D>;
     const int h = lane >> 5, kr = lane & 31;
     f32x16 s[QB];
@@ -405,40 +426,52 @@ struct Rows {
         }
       }
     }
-    bool wild = false;       // MASK: some V entry is not finite
-    if constexpr (MASK) {
+    if (cut || shut) {
 #pragma unroll
-      for (int b = 0; b < QB; ++b)
+      for (int b = 0; b < QB; ++b) {
+        const int to = lim[b] - key0 - 4 * h;       // the lane's keys below this one count
+        const int t0 = shut & 1 ? -32 : to, t1 = shut & 2 ? -32 : to;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = key0 + (r >> 2) * 8 + 4 * h + (r & 3);
-          if (key >= lim[b] || (shut >> (r >> 3) & 1)) s[b][r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          if ((r >> 2) * 8 + (r & 3) >= (r < 8 ? t0 : t1)) s[b][r] = -INFINITY;
+      }
+    }
+    if (cut) {
       // a weight of 0 times an infinity or NaN would reach rows that do not see that key: such entries are taken out
-      // here and added below to the rows that do
+      // here and added to the rows that do
+      typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+      u16x2 top = {0, 0};
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w = vf[u][dt][i];
-            const uint32_t lo = (w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-            wild |= (lo | hi) != 0u;
-            vf[u][dt][i] = w & ~(lo | hi);
-          }
+          for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[u][dt][i] & 0x7fff7fffu));
+      if (__builtin_amdgcn_ballot_w64(top.x >= 0x7f80 || top.y >= 0x7f80) != 0) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t w = vf[u][dt][i];
+              vf[u][dt][i] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+            }
+        add_wild(v_lds, key0, shut, lane);
+      }
     }
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
       uint32_t w[8];
       float sum0, sum1;
-      auto weights = [&]() {
+      auto weights = [&]() __attribute__((always_inline)) {
         sum0 = sum1 = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][2 * e], c, -ref[b]));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][2 * e + 1], c, -ref[b]));
           w[e] = pack_bf16(p0, p1);
+          asm("" : "+v"(w[e]));      // (where paths meet the pair would be carried unpacked, in twice the registers)
           sum0 += p0;
           sum1 += p1;
         }
@@ -467,8 +500,6 @@ struct Rows {
           o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[u][dt]), p, o[b][dt], 0, 0, 0);
       }
     }
-    if constexpr (MASK)
-      if (__builtin_amdgcn_ballot_w64(wild) != 0) add_wild(v_lds, key0, shut, lane);
   }
 
   // entries of V that are not finite, to the rows that see their keys
@@ -510,12 +541,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   Work w;
   SeqInfo s;
   if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
-  const int64_t n_rows = (int64_t)s.nq * a.group, row0 = (int64_t)w.block * 32;
-  const int last = limit_of(a, s, (int)(min(row0 + 31, n_rows - 1) / a.group));     // keys that some row sees
-  const int first = limit_of(a, s, (int)(row0 / a.group));                          // keys that every row sees
-  const int t0 = (int)((int64_t)s.tiles * w.piece / w.pieces), t1 = (int)((int64_t)s.tiles * (w.piece + 1) / w.pieces);
-  const int begin = t0 * 128 + wave * 32, end = (int)min((int64_t)t1 * 128, (int64_t)last);
-  const int n = end > begin ? (end - begin + 127) / 128 : 0;     // the wave's tiles
+  const int n_rows = s.nq * a.group, row0 = w.block * 32;
+  const int last = scalar(limit_of(a, s, min(row0 + 31, n_rows - 1) / a.group));     // keys that some row sees
+  const int first = scalar(limit_of(a, s, row0 / a.group));                          // keys that every row sees
+  const int begin = w.t0 * 128 + wave * 32, end = (int)min((uint32_t)w.t1 * 128u, (uint32_t)last);
+  const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 127) / 128 : 0);     // the wave's tiles
 
   char *const mine = lds + wave * (2 * kStages * kTile);
   const uint32_t mine_at = __builtin_amdgcn_readfirstlane(lds_addr(mine));
@@ -568,8 +598,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         wait_vm<0>();
       }
       const int key0 = begin + i * 128;
-      if (shut || key0 + 32 > first) rows.template tile<true>(kt, kt + kTile, a.c, key0, shut, lane);
-      else rows.template tile<false>(kt, kt + kTile, a.c, key0, 0, lane);
+      if (shut != 3) rows.tile(kt, kt + kTile, a.c, key0, shut, key0 + 32 > first, lane);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile has been read: its place may be filled again
       shut_now = holes;
     }
@@ -614,42 +643,48 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       if (ch == 0) a.part_ml[at] = float2{top, l};
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;     // no key seen: zeros
-      const int64_t rr = row0 + r;
-      uint16_t *p = a.o + (int64_t)(s.q0 + rr / a.group) * a.o_stride + (w.head * a.group + rr % a.group) * D + ch;
+      const int rr = row0 + r, tok = rr / a.group;
+      uint16_t *p = a.o + (int64_t)(s.q0 + tok) * a.o_stride + (w.head * a.group + rr - tok * a.group) * D + ch;
       *(u32x2 *)p = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
     }
   }
 }
 
 // ---------------------------------------------------------------------------------------
-// Many rows.  A workgroup has 128 QB rows and walks a piece of the keys in stages of 64, which wave w fetches the w-th 16 of
-// (so a stage is four groups, and a wave needs one page number for it).  bf16: a ring of stages in LDS, filled
-// straight from memory; E4M3: two stages in LDS, the one after the next in registers.
-template <Kv KV, int D, int QB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_many(Call a) {
+// Many rows.  A workgroup has 256 rows, 64 per wave, and walks a piece of the keys in stages of 64, of which wave w fetches the
+// w-th 16 (a stage is four groups, a wave needs one page number for it).  bf16: a ring of four stages in LDS, filled
+// straight from memory; E4M3: three stages of bf16 in LDS, the codes of the next one in registers.
+//
+// A wave's two blocks of 32 rows run half a step apart, so that one's weights (VALU) are taken while the other's products (MFMA) run:
+//   A(t): scores of block 1 (tile t) | K(t + 1) is read | output of block 1 (t - 1) | V(t) is read;  weights of block 0 (t)
+//   B(t): scores of block 0 (t + 1), output of block 0 (t);                                          weights of block 1 (t)
+// K's and V's fragments are read once for both blocks, half a phase before their first use, into the registers that the products
+// before have just been issued from.
+template <Kv KV, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1))) void k_kv_attn_many(Call a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using T = Tile<D>;
   constexpr int kHalf = 64 * T::kRow;                     // bytes of a stage's K or V
-  constexpr int kStages = KV == Kv::E4M3 || D == 128 ? 2 : 4;
+  constexpr int kStages = KV == Kv::E4M3 ? 3 : 4;
   constexpr int kFetch = 2 * T::kFetches;                 // fetches of a wave and stage
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int KF = D / 16, DT = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
   if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
-  const int64_t n_rows = (int64_t)s.nq * a.group, block0 = (int64_t)w.block * (128 * QB), row0 = block0 + wave * (32 * QB);
-  const int last = limit_of(a, s, (int)(min(block0 + 128 * QB - 1, n_rows - 1) / a.group));
+  const int n_rows = s.nq * a.group, block0 = w.block * 256, row0 = block0 + wave * 64;
+  const int last = scalar(limit_of(a, s, min(block0 + 255, n_rows - 1) / a.group));
   const bool live = row0 < n_rows;
-  const int first = live ? limit_of(a, s, (int)(row0 / a.group)) : 0;       // keys that every row of the wave sees
-  const int t0 = (int)((int64_t)s.tiles * w.piece / w.pieces), t1 = (int)((int64_t)s.tiles * (w.piece + 1) / w.pieces);
-  const int begin = t0 * 64, end = (int)min((int64_t)t1 * 64, (int64_t)last);
-  const int n = end > begin ? (end - begin + 63) / 64 : 0;
+  const int first = live ? scalar(limit_of(a, s, row0 / a.group)) : 0;       // keys that every row of the wave sees
+  const int begin = w.t0 * 64, end = (int)min((uint32_t)w.t1 * 64u, (uint32_t)last);
+  const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 63) / 64 : 0);
 
   Offsets<D> off;
   if constexpr (KV != Kv::E4M3) off.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, KV == Kv::ROWS ? a.v_stride : T::kRow);
   const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + wave * (kGrp * T::kRow);
   int own = 0, shuts = 0;        // lane j: stage j of 64: the page of this wave's group; bits of the groups that are not held
   uint64_t holes = 0;
-  auto look_up = [&](int i) {
+  auto look_up = [&](int i) __attribute__((always_inline)) {
     if constexpr (KV != Kv::ROWS) {
       const int64_t key = (int64_t)begin + (int64_t)(i + lane) * 64;
       shuts = 0;
@@ -665,84 +700,240 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
   };
   Codes<D> codes;
-  auto fetch = [&](int i) {      // beyond the last stage: nothing is read, the counts stay
+  auto fetch = [&](int i) __attribute__((always_inline)) {      // beyond the last stage: nothing is read, the counts stay
     const int key = begin + i * 64 + wave * kGrp;
     const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i & 63);
     const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
     if constexpr (KV == Kv::E4M3) codes.load(a, at, lane);
     else fetch_group<D>(at, off, base + (i % kStages) * (2 * kHalf), base + (i % kStages) * (2 * kHalf) + kHalf);
   };
-  auto put = [&](int i) {
+  auto put = [&](int i) __attribute__((always_inline)) {
     char *p = lds + (i % kStages) * (2 * kHalf) + wave * (kGrp * T::kRow);
     codes.store(p, p + kHalf, lane);
   };
-  Rows<D, QB> rows;
-  if (live) rows.load(a, s, w.head, row0, lane);
-  if (n > 0) {
-    uint64_t ahead = 0, now = 0;      // holes of the 64 stages being fetched, being computed with
-    int now_shuts = 0;
+  uint64_t now = 0, ahead = 0;      // holes of the 64 stages that are computed with, that are fetched
+  int now_shuts = 0;
+  // this wave's part of stage i + 1 has landed; behind the barrier all of it, and nobody reads stage i - 1 any more
+  auto publish = [&](int i) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (KV == Kv::E4M3) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    else wait_vm<(kStages - 3) * kFetch>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    const int next = i + 3;
+    if constexpr (KV == Kv::E4M3) put(i + 2);
+    if (KV != Kv::ROWS && next % 64 == 0 && next < n) {
+      look_up(next);
+      ahead = holes;
+    }
+    fetch(next);
+  };
+  auto start = [&]() __attribute__((always_inline)) {
     look_up(0);
     ahead = now = holes;
     now_shuts = shuts;
+    fetch(0);
     if constexpr (KV == Kv::E4M3) {
-      fetch(0);
       put(0);
       fetch(1);
+      put(1);
+      fetch(2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     } else {
-      for (int i = 0; i < kStages - 1; ++i) fetch(i);
+      fetch(1);
+      fetch(2);
+      wait_vm<2 * kFetch>();
     }
-    for (int i = 0; i < n; ++i) {
-      if (i && i % 64 == 0) {
+    __builtin_amdgcn_s_barrier();
+  };
+  if (!live) {      // no rows: the wave moves its share of the stages
+    if (n > 0) {
+      start();
+      for (int i = 0; i < n; ++i) publish(i);
+      wait_vm<0>();
+    }
+    return;
+  }
+  Rows<D, 2> rows;
+  rows.load(a, s, w.head, row0, lane);
+  if (n > 0) {
+    start();
+    f32x16 sacc[2];
+    uint32_t pb[2][8];
+    u32x4 fk[KF], fv[2][DT];
+    const uint32_t lds0 = lds_addr(lds);
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    const int kr = lane & 31, vr = 4 * h + (lane >> 2 & 3);
+    const uint32_t k_lane = lds0 + kr * T::kRow + ((h ^ T::k_xor(kr)) * 16);                       // piece 2 j + h: ^ 32 j
+    const uint32_t v_lane = lds0 + kHalf + vr * T::kRow + T::v_xor(vr) * 16 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;   // channels 32 dt: ^ 64 dt
+    auto tile_at = [&](int t) __attribute__((always_inline)) { return (uint32_t)(((t >> 1) % kStages) * (2 * kHalf) + (t & 1) * 32 * T::kRow); };
+    auto read_k = [&](int t) __attribute__((always_inline)) {
+      const uint32_t p = k_lane + tile_at(t);
+#pragma unroll
+      for (int j = 0; j < KF; ++j) fk[j] = *(lds_u32x4 *)(uintptr_t)(p ^ (j * 32));
+    };
+    auto read_v = [&](int t) __attribute__((always_inline)) {
+      const uint32_t p = v_lane + tile_at(t);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t q = (p ^ (dt * 64)) + u * 16 * T::kRow;
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)q));
+          const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(q + 8 * T::kRow)));
+          fv[u][dt] = u32x4{x.x, x.y, y.x, y.y};
+        }
+    };
+    auto scores = [&](int b) __attribute__((always_inline)) {
+      f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KF; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fk[j]), rows.q[b][j], acc, 0, 0, 0);
+      sacc[b] = acc;
+    };
+    auto output = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          rows.o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fv[u][dt]), p, rows.o[b][dt], 0, 0, 0);
+      }
+    };
+    float sum0, sum1;
+    auto weights = [&](int b, int half) __attribute__((always_inline)) {
+      if (half == 0) sum0 = sum1 = 0.f;
+#pragma unroll
+      for (int e = 4 * half; e < 4 * half + 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -rows.ref[b]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -rows.ref[b]));
+        pb[b][e] = pack_bf16(p0, p1);
+        asm("" : "+v"(pb[b][e]));      // (where paths meet the pair would be carried unpacked, in twice the registers)
+        sum0 += p0;
+        sum1 += p1;
+      }
+    };
+    auto recipe = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < KF; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x400, D == 64 ? 2 : 1, 0);    // exp2
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                  // MFMA
+        __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 5 : 3, 0);    // fused multiply-add, pack, add
+      }
+    };
+    // block b's weights become part of its sums, with the references raised first where a sum went past 2^40
+    auto settle = [&](int b) __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rows.l[b] + (sum0 + sum1) <= kRowRaise)) != 0, 0)) {
+        float top = sacc[b][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, sacc[b][r]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = fmaxf(rows.ref[b], top * a.c), f = __builtin_amdgcn_exp2f(rows.ref[b] - to);
+        rows.ref[b] = to;
+        rows.l[b] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) rows.o[b][dt][r] *= f;
+        weights(b, 0);
+        weights(b, 1);
+      }
+      rows.l[b] += sum0 + sum1;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto phase_a = [&](auto head, auto tail, int t) __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      scores(1);
+      weights(0, 0);
+      recipe();
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!decltype(tail)::value) read_k(t + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!decltype(head)::value) output(1);
+      weights(0, 1);
+      recipe();
+      __builtin_amdgcn_sched_barrier(0);
+      read_v(t);
+      settle(0);
+    };
+    auto phase_b = [&](auto tail) __attribute__((always_inline)) {
+      if constexpr (!decltype(tail)::value) scores(0);
+      weights(1, 0);
+      recipe();
+      __builtin_amdgcn_sched_barrier(0);
+      output(0);
+      weights(1, 1);
+      recipe();
+      settle(1);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const int plain = first > begin ? (first - begin) >> 6 : 0;     // stages of which every row of the wave sees every key
+    int i = 0;
+    while (i < n) {
+      // the stages from i on whose keys are all there and seen
+      int j = min(plain, n);
+      if constexpr (KV != Kv::ROWS) {
+        const uint64_t next = now >> (i & 63);
+        j = min(j, min((i | 63) + 1, next ? i + __ffsll((unsigned long long)next) - 1 : n));
+      }
+      j = __builtin_amdgcn_readfirstlane(j);
+      if (j > i) {
+        read_k(2 * i);
+        scores(0);
+        phase_a(Yes{}, No{}, 2 * i);
+        if (i < j - 1) do {
+          asm volatile("" : "+v"(sacc[1]));   // (the same phase follows the loop: its instructions would be drawn before the branch)
+          phase_b(No{});
+          publish(i);
+          phase_a(No{}, No{}, 2 * i + 1);
+          phase_b(No{});
+          phase_a(No{}, No{}, 2 * i + 2);
+          ++i;
+        } while (i < j - 1);
+        phase_b(No{});
+        publish(i);
+        phase_a(No{}, Yes{}, 2 * i + 1);
+        phase_b(Yes{});
+        output(1);
+      } else {
+        const int shut = KV != Kv::ROWS ? __builtin_amdgcn_readlane(now_shuts, i & 63) : 0;
+        const char *kt = lds + (i % kStages) * (2 * kHalf);
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          const int sh = shut >> (2 * t) & 3;
+          const int key0 = begin + i * 64 + t * 32;
+          if (sh != 3) rows.tile(kt + t * 32 * T::kRow, kt + kHalf + t * 32 * T::kRow, a.c, key0, sh, key0 + 32 > first, lane);
+        }
+        publish(i);
+      }
+      if (++i % 64 == 0) {
         now = ahead;
         now_shuts = shuts;
       }
-      if constexpr (KV != Kv::E4M3) wait_vm<(kStages - 2) * kFetch>();
-      __syncthreads();
-      const int next = i + (KV == Kv::E4M3 ? 2 : kStages - 1);
-      if constexpr (KV == Kv::E4M3) {
-        if (i + 1 < n) put(i + 1);
-      }
-      if (next % 64 == 0 && next < n) {
-        look_up(next);
-        ahead = holes;
-      }
-      fetch(next);
-      if (live) {
-        const char *kt = lds + (i % kStages) * (2 * kHalf);
-        const int shut = KV != Kv::ROWS && (now >> (i & 63) & 1) ? __builtin_amdgcn_readlane(now_shuts, i & 63) : 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int key0 = begin + i * 64 + t * 32;
-          const int sh = shut >> (2 * t) & 3;
-          if (sh || key0 + 32 > first) rows.template tile<true>(kt + t * 32 * T::kRow, kt + kHalf + t * 32 * T::kRow, a.c, key0, sh, lane);
-          else rows.template tile<false>(kt + t * 32 * T::kRow, kt + kHalf + t * 32 * T::kRow, a.c, key0, 0, lane);
-        }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     wait_vm<0>();     // nothing may land after the workgroup ends
   }
-  if (!live) return;
 #pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    const int r = wave * (32 * QB) + b * 32 + (lane & 31);
-    const int64_t rr = block0 + r;
+  for (int b = 0; b < 2; ++b) {
+    const int r = wave * 64 + b * 32 + (lane & 31);
+    const int rr = block0 + r, tok = rr / a.group;
     const float l = rows.l[b] + __shfl_xor(rows.l[b], 32, 64);
     if (rr >= n_rows) continue;
     if (w.pieces > 1) {
-      const int64_t at = (int64_t)w.slot * (128 * QB) + r;
+      const int64_t at = (int64_t)w.slot * 256 + r;
       if (lane < 32) a.part_ml[at] = float2{rows.ref[b], l};
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *(f32x4 *)(a.part + at * D + dt * 32 + i * 8 + (lane >> 5) * 4) =
+          *(f32x4 *)(a.part + at * D + dt * 32 + i * 8 + h * 4) =
               f32x4{rows.o[b][dt][4 * i], rows.o[b][dt][4 * i + 1], rows.o[b][dt][4 * i + 2], rows.o[b][dt][4 * i + 3]};
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
-      uint16_t *p = a.o + (int64_t)(s.q0 + rr / a.group) * a.o_stride + (w.head * a.group + rr % a.group) * D + (lane >> 5) * 4;
+      uint16_t *p = a.o + (int64_t)(s.q0 + tok) * a.o_stride + (w.head * a.group + rr - tok * a.group) * D + h * 4;
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *(u32x2 *)(p + dt * 32 + i * 8) = u32x2{pack_bf16(rows.o[b][dt][4 * i] * inv, rows.o[b][dt][4 * i + 1] * inv),
@@ -789,8 +980,8 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int hq = blockIdx.x % per_token * kRowsWg + in_wg;
   const bool there = hq < a.heads;
   const int head = (there ? hq : 0) / a.group, g = (there ? hq : 0) % a.group;
-  const int64_t r = (int64_t)(tok - s.q0) * a.group + g;
-  const int block = (int)(r / a.rows_per_block), in_block = (int)(r % a.rows_per_block);
+  const int r = (tok - s.q0) * a.group + g;
+  const int block = r >> a.block_shift, in_block = r & (a.rows_per_block - 1);
   const int64_t slot0 = before + (int64_t)head * pieces * s.blocks + block;
   if (slot0 + (int64_t)(pieces - 1) * s.blocks >= a.slots) return;
   auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
@@ -851,7 +1042,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(const uint16_t *k, int64_t st
 // ---------------------------------------------------------------------------------------
 struct Form {
   bool few;
-  int qb, rows, tile;
+  int rows, tile;
   int64_t units;     // blocks of the call at most, all heads
   int target;        // pieces beside these at most
 };
@@ -861,9 +1052,8 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t 
   Form f;
   const int group = heads / kv_heads;
   const double rows = (double)n_q * group / n_seq;
-  f.few = rows <= 32.0;
-  f.qb = f.few ? 1 : rows <= 128.0 || head_dim == 128 ? 1 : 2;
-  f.rows = f.few ? 32 : 128 * f.qb;
+  f.few = rows <= 64.0;
+  f.rows = f.few ? 32 : 256;
   f.tile = f.few ? 128 : 64;
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
@@ -895,12 +1085,9 @@ static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size
 template <Kv KV, int D>
 static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t st) {
   constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
-  static std::atomic<uint64_t> d0{0}, d1{0}, d2{0};
+  static std::atomic<uint64_t> d0{0}, d1{0};
   if (f.few) return go(k_kv_attn_few<KV, D>, d0, std::integral_constant<size_t, KV == Kv::E4M3 ? 2 * tile : 4 * tile>{}, c, grid, st);
-  using Ring = std::integral_constant<size_t, KV == Kv::E4M3 || D == 128 ? 2 * tile : 4 * tile>;
-  if (f.qb == 1) return go(k_kv_attn_many<KV, D, 1>, d1, Ring{}, c, grid, st);
-  if constexpr (D == 64) return go(k_kv_attn_many<KV, D, 2>, d2, Ring{}, c, grid, st);
-  return LV_ERR_SHAPE;
+  return go(k_kv_attn_many<KV, D>, d1, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid, st);
 }
 
 int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
@@ -935,6 +1122,8 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.max_pages = x.cv.max_pages;
   c.rows_per_block = f.rows;
   c.tile = f.tile;
+  c.block_shift = __builtin_ctz(f.rows);
+  c.tile_shift = __builtin_ctz(f.tile);
   c.target = f.target;
   c.slots = (int)slots_of(f);
   c.part = (float *)ws;
