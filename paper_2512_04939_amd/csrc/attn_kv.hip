@@ -279,73 +279,65 @@ __device__ __forceinline__ Group group_at(const Call &a, int head, int k0, int k
   return g;
 }
 
-// The page of position `key`: -1 where it is none
-__device__ __forceinline__ int page_at(const Call &a, int seq, int64_t key) {
-  if ((key >> a.page_shift) >= a.max_pages) return -1;
-  const int id = a.table[(int64_t)seq * a.max_pages + (key >> a.page_shift)];
-  return (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
+// The page of position `key` (of a sequence's keys, which end before position `end`): -1 where it is none.  No branches: what is
+// beyond the end looks at the table's last column.
+__device__ __forceinline__ int page_at(const Call &a, int seq, uint32_t key, int end) {
+  const int32_t *row = a.table + (int64_t)seq * a.max_pages;
+  const int id = row[min(key >> a.page_shift, (uint32_t)a.max_pages - 1u)];
+  return key < (uint32_t)end && (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
 }
 
-// A lane's offsets from a group's first row in its fetches, bf16
+// A lane's offsets from a group's first row (of K or of V) in its fetches, bf16
 template <int D>
 struct Offsets {
-  uint32_t k[Tile<D>::kFetches], v[Tile<D>::kFetches];
-  __device__ __forceinline__ void init(int lane, int64_t k_stride, int64_t v_stride) {
+  uint32_t o[Tile<D>::kFetches];
+  __device__ __forceinline__ void init(int lane, int64_t stride, bool of_v) {
     using T = Tile<D>;
 #pragma unroll
     for (int j = 0; j < T::kFetches; ++j) {
       const int row = j * T::kRowsPer + lane / T::kPieces, p = lane % T::kPieces;
-      k[j] = (uint32_t)(row * (int)k_stride + (p ^ T::k_xor(row)) * 16);
-      v[j] = (uint32_t)(row * (int)v_stride + (p ^ T::v_xor(row)) * 16);
+      o[j] = (uint32_t)(row * (int)stride + (p ^ (of_v ? T::v_xor(row) : T::k_xor(row))) * 16);
     }
   }
 };
 
 // The group's rows on their way into LDS (bf16)
 template <int D>
-__device__ __forceinline__ void fetch_group(const Group &g, const Offsets<D> &off, uint32_t k_lds, uint32_t v_lds) {
-  const u32x4 rk = uniform_rsrc(g.k, g.k_bytes), rv = uniform_rsrc(g.v, g.v_bytes);
+__device__ __forceinline__ void fetch_group(const char *p, int bytes, const Offsets<D> &off, uint32_t lds) {
+  const u32x4 r = uniform_rsrc(p, bytes);
 #pragma unroll
-  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(rk, off.k[j], k_lds + j * 1024);
-#pragma unroll
-  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(rv, off.v[j], v_lds + j * 1024);
+  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(r, off.o[j], lds + j * 1024);
 }
 
-// E4M3: a group's codes and exponents in registers, then as bf16 in LDS.  D = 64: one load of a wave has all 16 rows.
+// A scalar buffer resource (in vector registers it becomes a loop over the lanes)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_rsrc(const void *p, int bytes) {
+  const uint64_t b = (uint64_t)p;
+  const uint64_t u = (uint32_t)scalar((int)(uint32_t)b) | (uint64_t)(uint32_t)scalar((int)(b >> 32)) << 32;
+  return __builtin_amdgcn_make_buffer_rsrc((void *)u, 0, scalar(bytes), 0x00020000);
+}
+
+// E4M3: a group's codes and exponents (of K or of V) in registers, then as bf16 in LDS.  D = 64: one load of a wave has all 16 rows.
 template <int D>
 struct Codes {
-  static constexpr int kLoads = D / 64;
-  u32x4 k[kLoads], v[kLoads];
-  uint32_t ks[kLoads], vs[kLoads];
-  __device__ __forceinline__ void load(const Call &a, const Group &g, int lane) {
-    constexpr int per = D / 16, rows = 64 / per;   // 16-byte pieces of a row, rows of a load
-    auto rsrc = [](const void *p, int bytes) {     // (scalars: a resource in vector registers is a loop over the lanes)
-      const uint64_t b = (uint64_t)p;
-      const uint64_t u = (uint32_t)scalar((int)(uint32_t)b) | (uint64_t)(uint32_t)scalar((int)(b >> 32)) << 32;
-      return __builtin_amdgcn_make_buffer_rsrc((void *)u, 0, scalar(bytes), 0x00020000);
-    };
-    const __amdgpu_buffer_rsrc_t rk = rsrc(g.k, g.k_bytes), rv = rsrc(g.v, g.v_bytes);
-    const __amdgpu_buffer_rsrc_t sk = rsrc(a.k_scale + g.row, g.k_bytes / D), sv = rsrc(a.v_scale + g.row, g.k_bytes / D);
+  static constexpr int kLoads = D / 64, kPer = D / 16, kRows = 64 / kPer;   // loads; 16-byte pieces of a row, rows of a load
+  u32x4 c[kLoads];
+  uint32_t e[kLoads];
+  __device__ __forceinline__ void load(const char *codes, const uint8_t *scales, const Group &g, int lane) {
+    const __amdgpu_buffer_rsrc_t rc = scalar_rsrc(codes, g.k_bytes), rs = scalar_rsrc(scales + g.row, g.k_bytes / D);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int off = j * 1024 + lane * 16, row = j * rows + lane / per;
-      k[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rk, off, 0, 0));
-      v[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
-      ks[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sk, row, 0, 0);
-      vs[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(sv, row, 0, 0);
+      c[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, j * 1024 + lane * 16, 0, 0));
+      e[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, j * kRows + lane / kPer, 0, 0);
     }
   }
-  __device__ __forceinline__ void store(char *k_lds, char *v_lds, int lane) const {
+  __device__ __forceinline__ void store(char *lds, bool of_v, int lane) const {
     using T = Tile<D>;
-    constexpr int per = D / 16, rows = 64 / per;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int row = j * rows + lane / per, p = 2 * (lane % per);
-      const float a = __uint_as_float(ks[j] << 23), b = __uint_as_float(vs[j] << 23);
-      *(u32x4 *)(k_lds + row * T::kRow + ((p ^ T::k_xor(row)) * 16)) = dequant8(u32x2{k[j].x, k[j].y}, a);
-      *(u32x4 *)(k_lds + row * T::kRow + (((p + 1) ^ T::k_xor(row)) * 16)) = dequant8(u32x2{k[j].z, k[j].w}, a);
-      *(u32x4 *)(v_lds + row * T::kRow + ((p ^ T::v_xor(row)) * 16)) = dequant8(u32x2{v[j].x, v[j].y}, b);
-      *(u32x4 *)(v_lds + row * T::kRow + (((p + 1) ^ T::v_xor(row)) * 16)) = dequant8(u32x2{v[j].z, v[j].w}, b);
+      const int row = j * kRows + lane / kPer, p = 2 * (lane % kPer), x = of_v ? T::v_xor(row) : T::k_xor(row);
+      const float f = __uint_as_float(e[j] << 23);
+      *(u32x4 *)(lds + row * T::kRow + ((p ^ x) * 16)) = dequant8(u32x2{c[j].x, c[j].y}, f);
+      *(u32x4 *)(lds + row * T::kRow + (((p + 1) ^ x) * 16)) = dequant8(u32x2{c[j].z, c[j].w}, f);
     }
   }
 };
@@ -507,7 +499,7 @@ struct Rows {
     using T = Tile<D>;
     const int h = lane >> 5;
     for (int t = 0; t < 32; ++t) {
-      if (shut >> (t >> 4) & 1) continue;
+      const bool held = !(shut >> (t >> 4) & 1);
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -516,11 +508,11 @@ struct Rows {
           const u32x2 w = *(const u32x2 *)(v_lds + t * T::kRow + byte);
           const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u)
+          for (int e = 0; e < 4; ++e) {
+            const float y = (__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u ? x[e] : 0.f;
 #pragma unroll
-              for (int b = 0; b < QB; ++b)
-                if (key0 + t < lim[b]) o[b][dt][4 * i + e] += x[e];
+            for (int b = 0; b < QB; ++b) o[b][dt][4 * i + e] += held && key0 + t < lim[b] ? y : 0.f;
+          }
         }
     }
   }
@@ -549,29 +541,35 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
   char *const mine = lds + wave * (2 * kStages * kTile);
   const uint32_t mine_at = __builtin_amdgcn_readfirstlane(lds_addr(mine));
-  Offsets<D> off;
-  if constexpr (KV != Kv::E4M3) off.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, KV == Kv::ROWS ? a.v_stride : T::kRow);
+  Offsets<D> ko, vo;
+  if constexpr (KV != Kv::E4M3) {
+    ko.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, false);
+    vo.init(lane, KV == Kv::ROWS ? a.v_stride : T::kRow, true);
+  }
   int ids[2] = {0, 0};               // lane j: the pages of the two groups of tile j of 64
   uint64_t holes = 0;
   auto look_up = [&](int i) {        // tiles i .. i + 63
     if constexpr (KV != Kv::ROWS) {
-      const int64_t key = (int64_t)begin + (int64_t)(i + lane) * 128;
-      ids[0] = key < end ? page_at(a, w.seq, key) : -1;
-      ids[1] = key + kGrp < end ? page_at(a, w.seq, key + kGrp) : -1;
-      holes = __builtin_amdgcn_ballot_w64((key < end && ids[0] < 0) || (key + kGrp < end && ids[1] < 0));
+      const uint32_t key = (uint32_t)begin + (uint32_t)(i + lane) * 128u;
+      ids[0] = page_at(a, w.seq, key, end);
+      ids[1] = page_at(a, w.seq, key + kGrp, end);
+      holes = __builtin_amdgcn_ballot_w64((key < (uint32_t)end && ids[0] < 0) || (key + kGrp < (uint32_t)end && ids[1] < 0));
     }
   };
-  Codes<D> codes[2];
+  Codes<D> kc[2], vc[2];
   auto fetch = [&](int i) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int key = begin + i * 128 + g * kGrp;
       const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(ids[g], i & 63);
       const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
-      if constexpr (KV == Kv::E4M3) codes[g].load(a, at, lane);
-      else {
+      if constexpr (KV == Kv::E4M3) {
+        kc[g].load(at.k, a.k_scale, at, lane);
+        vc[g].load(at.v, a.v_scale, at, lane);
+      } else {
         const uint32_t to = mine_at + (i % kStages) * (2 * kTile) + g * kGrp * T::kRow;
-        fetch_group<D>(at, off, to, to + kTile);
+        fetch_group<D>(at.k, at.k_bytes, ko, to);
+        fetch_group<D>(at.v, at.v_bytes, vo, to + kTile);
       }
     }
   };
@@ -588,7 +586,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
       if constexpr (KV == Kv::E4M3) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) codes[g].store(kt + g * kGrp * T::kRow, kt + kTile + g * kGrp * T::kRow, lane);
+        for (int g = 0; g < 2; ++g) {
+          kc[g].store(kt + g * kGrp * T::kRow, false, lane);
+          vc[g].store(kt + kTile + g * kGrp * T::kRow, true, lane);
+        }
       }
       if (i + 1 < n) {
         if ((i + 1) % 64 == 0) look_up(i + 1);
@@ -651,87 +652,104 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ---------------------------------------------------------------------------------------
-// Many rows.  A workgroup has 256 rows, 64 per wave, and walks a piece of the keys in stages of 64, of which wave w fetches the
-// w-th 16 (a stage is four groups, a wave needs one page number for it).  bf16: a ring of four stages in LDS, filled
-// straight from memory; E4M3: three stages of bf16 in LDS, the codes of the next one in registers.
+// Many rows.  A workgroup has 256 rows and walks a piece of the keys in stages of 64 (four groups of 16).  bf16: a ring of four
+// stages in LDS, filled straight from memory; E4M3: three stages of bf16 in LDS, the codes of the next one in registers.
 //
-// A wave's two blocks of 32 rows run half a step apart, so that one's weights (VALU) are taken while the other's products (MFMA) run:
+// 64 channels: four waves of 64 rows, of which wave w fetches the w-th group of a stage.  A wave's two blocks of 32 rows run half a step
+// apart, so that one's weights (VALU) are taken while the other's products (MFMA) run:
 //   A(t): scores of block 1 (tile t) | K(t + 1) is read | output of block 1 (t - 1) | V(t) is read;  weights of block 0 (t)
 //   B(t): scores of block 0 (t + 1), output of block 0 (t);                                          weights of block 1 (t)
 // K's and V's fragments are read once for both blocks, half a phase before their first use, into the registers that the products
 // before have just been issued from.
+//
+// 128 channels: a block of 32 rows fills the registers that two waves per SIMD have (64 rows and one wave per SIMD: 304 and more
+// of 512, which the compiler does not divide without copies and spills).  Eight waves of 32 rows; wave w fetches K's (w even) or V's rows of group w / 2.
+// Tiles take turns as the blocks do above:
+//   C(t): scores (t + 1) | K(t + 2) is read | output (t - 1) | V(t) is read;  weights (t)
+//
+// No register may go to scratch in the loops: reading it back waits for the fetches (three times the time).
+template <int D>
+struct Many {
+  static constexpr int QB = D == 64 ? 2 : 1, kWaves = 8 / QB, kRows = 32 * QB;
+};
 template <Kv KV, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1))) void k_kv_attn_many(Call a) {
+__global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_many(Call a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using T = Tile<D>;
+  constexpr int QB = Many<D>::QB, kWaves = Many<D>::kWaves, kRows = Many<D>::kRows;
   constexpr int kHalf = 64 * T::kRow;                     // bytes of a stage's K or V
   constexpr int kStages = KV == Kv::E4M3 ? 3 : 4;
-  constexpr int kFetch = 2 * T::kFetches;                 // fetches of a wave and stage
+  constexpr int kFetch = (kWaves == 4 ? 2 : 1) * T::kFetches;     // fetches of a wave and stage
   constexpr int KF = D / 16, DT = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
   if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
-  const int n_rows = s.nq * a.group, block0 = w.block * 256, row0 = block0 + wave * 64;
+  const int n_rows = s.nq * a.group, block0 = w.block * 256, row0 = block0 + wave * kRows;
   const int last = scalar(limit_of(a, s, min(block0 + 255, n_rows - 1) / a.group));
   const bool live = row0 < n_rows;
   const int first = live ? scalar(limit_of(a, s, row0 / a.group)) : 0;       // keys that every row of the wave sees
   const int begin = w.t0 * 64, end = (int)min((uint32_t)w.t1 * 64u, (uint32_t)last);
   const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 63) / 64 : 0);
 
-  Offsets<D> off;
-  if constexpr (KV != Kv::E4M3) off.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, KV == Kv::ROWS ? a.v_stride : T::kRow);
-  const uint32_t base = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + wave * (kGrp * T::kRow);
-  int own = 0, shuts = 0;        // lane j: stage j of 64: the page of this wave's group; bits of the groups that are not held
+  // what the wave fetches: its group, K's rows and (four waves) V's
+  const int group = kWaves == 4 ? wave : wave >> 1;
+  const bool only_v = kWaves == 8 && (wave & 1);
+  Offsets<D> off, off_v;
+  if constexpr (KV != Kv::E4M3) {
+    off.init(lane, KV != Kv::ROWS ? T::kRow : only_v ? a.v_stride : a.k_stride, only_v);
+    if constexpr (kWaves == 4) off_v.init(lane, KV != Kv::ROWS ? T::kRow : a.v_stride, true);
+  }
+  const uint32_t to = (only_v ? kHalf : 0) + group * (kGrp * T::kRow), base = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + to;
+  // lane j, of stage from + j: the page of this wave's group; bits of the groups that are not held.  Stages are fetched three
+  // ahead, so these serve the computation of stages from .. from + 60.
+  int from = 0, own = 0, shuts = 0;
   uint64_t holes = 0;
   auto look_up = [&](int i) __attribute__((always_inline)) {
     if constexpr (KV != Kv::ROWS) {
-      const int64_t key = (int64_t)begin + (int64_t)(i + lane) * 64;
+      const uint32_t key = (uint32_t)begin + (uint32_t)(i + lane) * 64u;
+      from = i;
       shuts = 0;
       own = -1;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const bool in = key + g * kGrp < end;
-        const int id = in ? page_at(a, w.seq, key + g * kGrp) : -1;
-        if (g == wave) own = id;
-        if (in && id < 0) shuts |= 1 << g;
+        const int id = page_at(a, w.seq, key + g * kGrp, end);
+        own = g == group ? id : own;
+        shuts |= (key + g * kGrp < (uint32_t)end && id < 0 ? 1 : 0) << g;
       }
       holes = __builtin_amdgcn_ballot_w64(shuts != 0);
     }
   };
-  Codes<D> codes;
+  Codes<D> codes, codes_v;
   auto fetch = [&](int i) __attribute__((always_inline)) {      // beyond the last stage: nothing is read, the counts stay
-    const int key = begin + i * 64 + wave * kGrp;
-    const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i & 63);
+    const int key = begin + i * 64 + group * kGrp;
+    const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i - from);
     const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
-    if constexpr (KV == Kv::E4M3) codes.load(a, at, lane);
-    else fetch_group<D>(at, off, base + (i % kStages) * (2 * kHalf), base + (i % kStages) * (2 * kHalf) + kHalf);
+    if constexpr (KV == Kv::E4M3) {
+      codes.load(only_v ? at.v : at.k, only_v ? a.v_scale : a.k_scale, at, lane);
+      if constexpr (kWaves == 4) codes_v.load(at.v, a.v_scale, at, lane);
+    } else {
+      fetch_group<D>(only_v ? at.v : at.k, only_v ? at.v_bytes : at.k_bytes, off, base + (i % kStages) * (2 * kHalf));
+      if constexpr (kWaves == 4) fetch_group<D>(at.v, at.v_bytes, off_v, base + (i % kStages) * (2 * kHalf) + kHalf);
+    }
   };
   auto put = [&](int i) __attribute__((always_inline)) {
-    char *p = lds + (i % kStages) * (2 * kHalf) + wave * (kGrp * T::kRow);
-    codes.store(p, p + kHalf, lane);
+    char *p = lds + (i % kStages) * (2 * kHalf) + to;
+    codes.store(p, only_v, lane);
+    if constexpr (kWaves == 4) codes_v.store(p + kHalf, true, lane);
   };
-  uint64_t now = 0, ahead = 0;      // holes of the 64 stages that are computed with, that are fetched
-  int now_shuts = 0;
   // this wave's part of stage i + 1 has landed; behind the barrier all of it, and nobody reads stage i - 1 any more
   auto publish = [&](int i) __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KV == Kv::E4M3) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    else wait_vm<(kStages - 3) * kFetch>();
+    if constexpr (KV != Kv::E4M3) wait_vm<(kStages - 3) * kFetch>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    const int next = i + 3;
     if constexpr (KV == Kv::E4M3) put(i + 2);
-    if (KV != Kv::ROWS && next % 64 == 0 && next < n) {
-      look_up(next);
-      ahead = holes;
-    }
-    fetch(next);
+    fetch(i + 3);
   };
   auto start = [&]() __attribute__((always_inline)) {
     look_up(0);
-    ahead = now = holes;
-    now_shuts = shuts;
     fetch(0);
     if constexpr (KV == Kv::E4M3) {
       put(0);
@@ -749,18 +767,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
   if (!live) {      // no rows: the wave moves its share of the stages
     if (n > 0) {
       start();
-      for (int i = 0; i < n; ++i) publish(i);
+      for (int i = 0; i < n; ++i) {
+        if (KV != Kv::ROWS && i - from > 60) look_up(i);
+        publish(i);
+      }
       wait_vm<0>();
     }
     return;
   }
-  Rows<D, 2> rows;
+  Rows<D, QB> rows;
   rows.load(a, s, w.head, row0, lane);
   if (n > 0) {
     start();
-    f32x16 sacc[2];
+    f32x16 sacc[2];              // scores: of the two blocks, or of even and odd tiles
     uint32_t pb[2][8];
-    u32x4 fk[KF], fv[2][DT];
+    u32x4 fk[KF], fv[2][DT];     // 64 channels
     const uint32_t lds0 = lds_addr(lds);
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     const int kr = lane & 31, vr = 4 * h + (lane >> 2 & 3);
@@ -787,7 +808,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
     auto scores = [&](int b) __attribute__((always_inline)) {
       f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < KF; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fk[j]), rows.q[b][j], acc, 0, 0, 0);
+      for (int j = 0; j < KF; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fk[j]), rows.q[QB == 2 ? b : 0][j], acc, 0, 0, 0);
       sacc[b] = acc;
     };
     auto output = [&](int b) __attribute__((always_inline)) {
@@ -796,21 +817,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
         const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          rows.o[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fv[u][dt]), p, rows.o[b][dt], 0, 0, 0);
+          rows.o[QB == 2 ? b : 0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fv[u][dt]), p, rows.o[QB == 2 ? b : 0][dt], 0, 0, 0);
       }
     };
     float sum0, sum1;
+    auto weight = [&](int b, int e) __attribute__((always_inline)) {
+      const float ref = rows.ref[QB == 2 ? b : 0];
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -ref));
+      pb[b][e] = pack_bf16(p0, p1);
+      asm("" : "+v"(pb[b][e]));      // (where paths meet the pair would be carried unpacked, in twice the registers)
+      sum0 += p0;
+      sum1 += p1;
+    };
     auto weights = [&](int b, int half) __attribute__((always_inline)) {
       if (half == 0) sum0 = sum1 = 0.f;
 #pragma unroll
-      for (int e = 4 * half; e < 4 * half + 4; ++e) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -rows.ref[b]));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -rows.ref[b]));
-        pb[b][e] = pack_bf16(p0, p1);
-        asm("" : "+v"(pb[b][e]));      // (where paths meet the pair would be carried unpacked, in twice the registers)
-        sum0 += p0;
-        sum1 += p1;
-      }
+      for (int e = 4 * half; e < 4 * half + 4; ++e) weight(b, e);
+    };
+    auto weights2 = [&](int b, int q) __attribute__((always_inline)) {
+      if (q == 0) sum0 = sum1 = 0.f;
+#pragma unroll
+      for (int e = 2 * q; e < 2 * q + 2; ++e) weight(b, e);
     };
     auto recipe = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -822,23 +850,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
     };
     // block b's weights become part of its sums, with the references raised first where a sum went past 2^40
     auto settle = [&](int b) __attribute__((always_inline)) {
+      constexpr int kOne = QB == 2 ? 1 : 0;
+      const int r = b * kOne;
       __builtin_amdgcn_sched_barrier(0);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rows.l[b] + (sum0 + sum1) <= kRowRaise)) != 0, 0)) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(rows.l[r] + (sum0 + sum1) <= kRowRaise)) != 0, 0)) {
         float top = sacc[b][0];
 #pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, sacc[b][r]);
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, sacc[b][e]);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float to = fmaxf(rows.ref[b], top * a.c), f = __builtin_amdgcn_exp2f(rows.ref[b] - to);
-        rows.ref[b] = to;
-        rows.l[b] *= f;
+        const float to = fmaxf(rows.ref[r], top * a.c), f = __builtin_amdgcn_exp2f(rows.ref[r] - to);
+        rows.ref[r] = to;
+        rows.l[r] *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) rows.o[b][dt][r] *= f;
+          for (int e = 0; e < 16; ++e) rows.o[r][dt][e] *= f;
         weights(b, 0);
         weights(b, 1);
       }
-      rows.l[b] += sum0 + sum1;
+      rows.l[r] += sum0 + sum1;
       __builtin_amdgcn_sched_barrier(0);
     };
     auto phase_a = [&](auto head, auto tail, int t) __attribute__((always_inline)) {
@@ -866,6 +896,72 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
       recipe();
       settle(1);
     };
+    // 128 channels: C(t) in quarters, of four products each
+    u32x4 f0[QB == 1 ? 4 : 1], f1[QB == 1 ? 4 : 1];
+    auto read_k4 = [&](int t, int half, u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
+      const uint32_t p = k_lane + tile_at(t);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = *(lds_u32x4 *)(uintptr_t)(p ^ ((4 * half + j) * 32));
+    };
+    auto read_v4 = [&](int t, int u, u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
+      const uint32_t p = v_lane + tile_at(t) + u * 16 * T::kRow;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        const uint32_t q = p ^ (dt * 64);
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)q));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(q + 8 * T::kRow)));
+        f[dt] = u32x4{x.x, x.y, y.x, y.y};
+      }
+    };
+    auto scores4 = [&](int b, int half, const u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
+      f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (half) acc = sacc[b];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[j]), rows.q[0][4 * half + j], acc, 0, 0, 0);
+      sacc[b] = acc;
+    };
+    auto output4 = [&](int b, int u, const u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
+      const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+        rows.o[0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[dt]), p, rows.o[0][dt], 0, 0, 0);
+    };
+    auto quarter = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // head: nothing of a tile before; tail: no tile after; pub: stage t / 2 + 1 is needed and t / 2 - 1 no more
+    auto phase_c = [&](auto head, auto tail, auto pub, int b, int t) __attribute__((always_inline)) {
+      constexpr bool kHead = decltype(head)::value, kTail = decltype(tail)::value, kPub = decltype(pub)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!kTail) scores4(b ^ 1, 0, f0);
+      weights2(b, 0);
+      quarter();
+      if constexpr (!kHead) read_v4(t - 1, 0, f0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!kTail) scores4(b ^ 1, 1, f1);
+      weights2(b, 1);
+      quarter();
+      if constexpr (!kHead) read_v4(t - 1, 1, f1);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!kHead) output4(b ^ 1, 0, f0);
+      weights2(b, 2);
+      quarter();
+      if constexpr (kPub) publish(t >> 1);
+      if constexpr (!kTail) read_k4(t + 2, 0, f0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!kHead) output4(b ^ 1, 1, f1);
+      weights2(b, 3);
+      quarter();
+      if constexpr (!kTail) read_k4(t + 2, 1, f1);
+      settle(b);
+    };
     using Yes = std::true_type;
     using No = std::false_type;
     const int plain = first > begin ? (first - begin) >> 6 : 0;     // stages of which every row of the wave sees every key
@@ -874,30 +970,60 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
       // the stages from i on whose keys are all there and seen
       int j = min(plain, n);
       if constexpr (KV != Kv::ROWS) {
-        const uint64_t next = now >> (i & 63);
-        j = min(j, min((i | 63) + 1, next ? i + __ffsll((unsigned long long)next) - 1 : n));
+        if (i - from > 60) look_up(i);
+        const uint64_t next = holes >> (i - from);
+        j = min(j, min(from + 61, next ? i + __ffsll((unsigned long long)next) - 1 : n));
       }
       j = __builtin_amdgcn_readfirstlane(j);
       if (j > i) {
-        read_k(2 * i);
-        scores(0);
-        phase_a(Yes{}, No{}, 2 * i);
-        if (i < j - 1) do {
-          asm volatile("" : "+v"(sacc[1]));   // (the same phase follows the loop: its instructions would be drawn before the branch)
+        if constexpr (QB == 2) {
+          read_k(2 * i);
+          scores(0);
+          phase_a(Yes{}, No{}, 2 * i);
+          if (i < j - 1) do {
+            asm volatile("" : "+v"(sacc[1]));   // (the same phase follows the loop: its instructions would be drawn before the branch)
+            phase_b(No{});
+            publish(i);
+            phase_a(No{}, No{}, 2 * i + 1);
+            phase_b(No{});
+            phase_a(No{}, No{}, 2 * i + 2);
+            ++i;
+          } while (i < j - 1);
           phase_b(No{});
           publish(i);
-          phase_a(No{}, No{}, 2 * i + 1);
-          phase_b(No{});
-          phase_a(No{}, No{}, 2 * i + 2);
-          ++i;
-        } while (i < j - 1);
-        phase_b(No{});
-        publish(i);
-        phase_a(No{}, Yes{}, 2 * i + 1);
-        phase_b(Yes{});
-        output(1);
+          phase_a(No{}, Yes{}, 2 * i + 1);
+          phase_b(Yes{});
+          output(1);
+        } else {
+          read_k4(2 * i, 0, f0);
+          read_k4(2 * i, 1, f1);
+          scores4(0, 0, f0);
+          scores4(0, 1, f1);
+          read_k4(2 * i + 1, 0, f0);
+          read_k4(2 * i + 1, 1, f1);
+          if (i < j - 1) {
+            phase_c(Yes{}, No{}, Yes{}, 0, 2 * i);
+            phase_c(No{}, No{}, No{}, 1, 2 * i + 1);
+            ++i;
+            if (i < j - 1) do {
+              asm volatile("" : "+v"(sacc[0]));
+              phase_c(No{}, No{}, Yes{}, 0, 2 * i);
+              phase_c(No{}, No{}, No{}, 1, 2 * i + 1);
+              ++i;
+            } while (i < j - 1);
+            phase_c(No{}, No{}, Yes{}, 0, 2 * i);      // (its reads of a tile beyond the run are of a stage that is there or arriving, and not used)
+          } else {
+            phase_c(Yes{}, No{}, Yes{}, 0, 2 * i);
+          }
+          phase_c(No{}, Yes{}, No{}, 1, 2 * i + 1);
+          read_v4(2 * i + 1, 0, f0);
+          output4(1, 0, f0);
+          read_v4(2 * i + 1, 1, f1);
+          output4(1, 1, f1);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
       } else {
-        const int shut = KV != Kv::ROWS ? __builtin_amdgcn_readlane(now_shuts, i & 63) : 0;
+        const int shut = KV != Kv::ROWS ? __builtin_amdgcn_readlane(shuts, i - from) : 0;
         const char *kt = lds + (i % kStages) * (2 * kHalf);
 #pragma unroll 1
         for (int t = 0; t < 2; ++t) {
@@ -907,16 +1033,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2
         }
         publish(i);
       }
-      if (++i % 64 == 0) {
-        now = ahead;
-        now_shuts = shuts;
-      }
+      ++i;
     }
     wait_vm<0>();     // nothing may land after the workgroup ends
   }
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int r = wave * 64 + b * 32 + (lane & 31);
+  for (int b = 0; b < QB; ++b) {
+    const int r = wave * kRows + b * 32 + (lane & 31);
     const int rr = block0 + r, tok = rr / a.group;
     const float l = rows.l[b] + __shfl_xor(rows.l[b], 32, 64);
     if (rr >= n_rows) continue;
@@ -1073,12 +1196,12 @@ size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_di
 }
 
 template <typename K, size_t LDS>
-static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size_t, LDS>, const Call &c, uint32_t grid, hipStream_t st) {
+static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size_t, LDS>, const Call &c, uint32_t grid, int threads, hipStream_t st) {
   if constexpr (LDS > 60000) {     // (a kernel has up to 1 KB beside it)
     const int rc = allow_dynamic_lds<LDS>((const void *)kernel, done);
     if (rc) return rc;
   }
-  kernel<<<dim3(grid), 256, LDS, st>>>(c);
+  kernel<<<dim3(grid), threads, LDS, st>>>(c);
   return LV_OK;
 }
 
@@ -1086,8 +1209,9 @@ template <Kv KV, int D>
 static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t st) {
   constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
   static std::atomic<uint64_t> d0{0}, d1{0};
-  if (f.few) return go(k_kv_attn_few<KV, D>, d0, std::integral_constant<size_t, KV == Kv::E4M3 ? 2 * tile : 4 * tile>{}, c, grid, st);
-  return go(k_kv_attn_many<KV, D>, d1, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid, st);
+  if (f.few) return go(k_kv_attn_few<KV, D>, d0, std::integral_constant<size_t, KV == Kv::E4M3 ? 2 * tile : 4 * tile>{}, c, grid, 256, st);
+  return go(k_kv_attn_many<KV, D>, d1, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid,
+            64 * Many<D>::kWaves, st);
 }
 
 int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
