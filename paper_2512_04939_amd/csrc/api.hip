@@ -115,6 +115,7 @@ float scale_of(const litevggt_params *p) {
 
 // ---- the paged cache and attention over keys of another set
 constexpr int64_t kMostStride = (int64_t)1 << 26;   // elements: 16 rows' bytes stay below 2^31
+constexpr int64_t kMostPositions = 0x7fff0000;      // of a sequence: what lies beyond stands for no position
 
 int check_heads(int n_seq, int heads, int kv_heads, int head_dim, float softmax_scale) {
   if (n_seq < 1 || n_seq > 65535) return LV_ERR_SHAPE;
@@ -131,7 +132,7 @@ int check_cache(const litevggt_cache_params *p, CacheView *cv) {
   int shift = 4;
   while (shift < 10 && (1 << shift) < p->page_tokens) ++shift;
   if ((1 << shift) != p->page_tokens || p->n_pages < 1 || p->max_pages < 1) return LV_ERR_SHAPE;
-  if (((int64_t)p->max_pages << shift) >= ((int64_t)1 << 31)) return LV_ERR_SHAPE;
+  if (((int64_t)p->max_pages << shift) > kMostPositions) return LV_ERR_SHAPE;
   if (p->frame_tokens < 0) return LV_ERR_PARAM;
   cv->n_seq = p->n_seq;
   cv->kv_heads = p->kv_heads;

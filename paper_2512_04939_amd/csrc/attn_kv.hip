@@ -21,6 +21,7 @@ namespace lv {
 namespace {
 
 constexpr int kGrp = 16;                 // rows of K or V that are fetched together; a page holds a multiple of it
+constexpr int kNoKey = 0x7fff0000;       // beyond every position that rows see
 constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
 constexpr float kRowRaise = 1.0995116e12f;   // 2^40
 constexpr int kSlotsAll = 512;           // workgroups resident on the chip: 256 CUs, 2 each
@@ -287,17 +288,20 @@ __device__ __forceinline__ int page_at(const Call &a, int seq, uint32_t key, int
   return key < (uint32_t)end && (uint32_t)id < (uint32_t)a.n_pages ? id : -1;
 }
 
-// A lane's offsets from a group's first row (of K or of V) in its fetches, bf16
+// A lane's offsets from a group's first row (of K or of V) in its fetches, bf16: fetch j brings rows kRowsPer j .. and piece p ^ x(row), where
+// x(row) = x(lane's row of fetch 0) ^ turn j.  They are worked out where they are used: kept, they cost the registers that 128
+// channels have not got.
 template <int D>
 struct Offsets {
-  uint32_t o[Tile<D>::kFetches];
+  uint32_t row, piece;     // bytes
+  int step, turn;
   __device__ __forceinline__ void init(int lane, int64_t stride, bool of_v) {
     using T = Tile<D>;
-#pragma unroll
-    for (int j = 0; j < T::kFetches; ++j) {
-      const int row = j * T::kRowsPer + lane / T::kPieces, p = lane % T::kPieces;
-      o[j] = (uint32_t)(row * (int)stride + (p ^ (of_v ? T::v_xor(row) : T::k_xor(row))) * 16);
-    }
+    const int r = lane / T::kPieces, p = lane % T::kPieces;
+    row = (uint32_t)(r * (int)stride);
+    piece = (uint32_t)(p ^ (of_v ? T::v_xor(r) : T::k_xor(r))) * 16u;
+    step = T::kRowsPer * (int)stride;
+    turn = of_v ? 0 : 64;
   }
 };
 
@@ -305,8 +309,10 @@ struct Offsets {
 template <int D>
 __device__ __forceinline__ void fetch_group(const char *p, int bytes, const Offsets<D> &off, uint32_t lds) {
   const u32x4 r = uniform_rsrc(p, bytes);
+  uint32_t piece = off.piece;
+  asm volatile("" : "+v"(piece));
 #pragma unroll
-  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(r, off.o[j], lds + j * 1024);
+  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(r, off.row + (uint32_t)(j * off.step) + (piece ^ (uint32_t)(j * off.turn)), lds + j * 1024);
 }
 
 // A scalar buffer resource (in vector registers it becomes a loop over the lanes)
@@ -383,9 +389,9 @@ struct Rows {
     }
   }
 
-  // one tile of 32 keys from key0 on, K and V rows at k_lds and v_lds.  shut: bit i: the i-th 16 keys are not held (their rows
-  // are zeros).  cut: some row does not see some of the keys.
-  __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int shut, bool cut, int lane) {
+  // one tile of 32 keys, 16 from key0 and 16 from key1 on, K and V rows at k_lds and v_lds; what is not held is zeros, its
+  // keys are kNoKey.  cut: some row does not see some of the keys.
+  __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int key1, bool cut, int lane) {
     using T = Tile<D>;
     const int h = lane >> 5, kr = lane & 31;
     f32x16 s[QB];
@@ -418,17 +424,14 @@ struct Rows {
         }
       }
     }
-    if (cut || shut) {
+    if (cut) {
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
-        const int to = lim[b] - key0 - 4 * h;       // the lane's keys below this one count
-        const int t0 = shut & 1 ? -32 : to, t1 = shut & 2 ? -32 : to;
+        const int t0 = lim[b] - key0 - 4 * h, t1 = lim[b] - key1 - 4 * h;       // the lane's keys below these count
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if ((r >> 2) * 8 + (r & 3) >= (r < 8 ? t0 : t1)) s[b][r] = -INFINITY;
+          if ((r >> 2 & 1) * 8 + (r & 3) >= (r < 8 ? t0 : t1)) s[b][r] = -INFINITY;
       }
-    }
-    if (cut) {
       // a weight of 0 times an infinity or NaN would reach rows that do not see that key: such entries are taken out
       // here and added to the rows that do
       typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
@@ -449,7 +452,7 @@ struct Rows {
               const uint32_t w = vf[u][dt][i];
               vf[u][dt][i] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
             }
-        add_wild(v_lds, key0, shut, lane);
+        add_wild(v_lds, key0, key1, lane);
       }
     }
 #pragma unroll
@@ -495,11 +498,11 @@ struct Rows {
   }
 
   // entries of V that are not finite, to the rows that see their keys
-  __device__ __forceinline__ void add_wild(const char *v_lds, int key0, int shut, int lane) {
+  __device__ __forceinline__ void add_wild(const char *v_lds, int key0, int key1, int lane) {
     using T = Tile<D>;
     const int h = lane >> 5;
     for (int t = 0; t < 32; ++t) {
-      const bool held = !(shut >> (t >> 4) & 1);
+      const int key = t < 16 ? key0 + t : key1 + t - 16;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -511,7 +514,7 @@ struct Rows {
           for (int e = 0; e < 4; ++e) {
             const float y = (__float_as_uint(x[e]) & 0x7f800000u) == 0x7f800000u ? x[e] : 0.f;
 #pragma unroll
-            for (int b = 0; b < QB; ++b) o[b][dt][4 * i + e] += held && key0 + t < lim[b] ? y : 0.f;
+            for (int b = 0; b < QB; ++b) o[b][dt][4 * i + e] += key < lim[b] ? y : 0.f;
           }
         }
     }
@@ -599,7 +602,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         wait_vm<0>();
       }
       const int key0 = begin + i * 128;
-      if (shut != 3) rows.tile(kt, kt + kTile, a.c, key0, shut, key0 + 32 > first, lane);
+      if (shut != 3)
+        rows.tile(kt, kt + kTile, a.c, shut & 1 ? kNoKey : key0, shut & 2 ? kNoKey : key0 + kGrp, shut || key0 + 32 > first, lane);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile has been read: its place may be filled again
       shut_now = holes;
     }
@@ -690,7 +694,6 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   const bool live = row0 < n_rows;
   const int first = live ? scalar(limit_of(a, s, row0 / a.group)) : 0;       // keys that every row of the wave sees
   const int begin = w.t0 * 64, end = (int)min((uint32_t)w.t1 * 64u, (uint32_t)last);
-  const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 63) / 64 : 0);
 
   // what the wave fetches: its group, K's rows and (four waves) V's
   const int group = kWaves == 4 ? wave : wave >> 1;
@@ -701,40 +704,63 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     if constexpr (kWaves == 4) off_v.init(lane, KV != Kv::ROWS ? T::kRow : a.v_stride, true);
   }
   const uint32_t to = (only_v ? kHalf : 0) + group * (kGrp * T::kRow), base = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + to;
-  // lane j, of stage from + j: the page of this wave's group; bits of the groups that are not held.  Stages are fetched three
-  // ahead, so these serve the computation of stages from .. from + 60.
-  int from = 0, own = 0, shuts = 0;
-  uint64_t holes = 0;
+  // Pages: stages are made of the groups that are held.  The numbers and pages of 256 of them, 64 stages, are listed at a time, and
+  // stages are fetched three ahead: a list serves the computation of stages from .. from + 60.  Lane j, of stage from + j: group and page
+  // that this wave fetches.
+  __shared__ int list[KV == Kv::ROWS ? 1 : kWaves][2][KV == Kv::ROWS ? 1 : 256];
+  int n = KV == Kv::ROWS ? scalar(end > begin ? (end - begin + 63) / 64 : 0) : 0x7fffffff;    // stages (pages: once it is known)
+  int from = 0, listed = 0, own = 0, own_key = 0;
+  int plain = KV == Kv::ROWS ? (first > begin ? (first - begin) >> 6 : 0) : 0;     // stages up to this one hold 64 keys that every row sees
   auto look_up = [&](int i) __attribute__((always_inline)) {
     if constexpr (KV != Kv::ROWS) {
-      const uint32_t key = (uint32_t)begin + (uint32_t)(i + lane) * 64u;
+      int *const ids = list[wave][0], *const groups = list[wave][1];
+      int at = i ? scalar(groups[4 * (i - from)]) : begin >> 4, count = 0;
+      const int last_group = (end + kGrp - 1) >> 4;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       from = i;
-      shuts = 0;
-      own = -1;
+#pragma unroll 1
+      do {
+        int id[4];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int id = page_at(a, w.seq, key + g * kGrp, end);
-        own = g == group ? id : own;
-        shuts |= (key + g * kGrp < (uint32_t)end && id < 0 ? 1 : 0) << g;
-      }
-      holes = __builtin_amdgcn_ballot_w64(shuts != 0);
+        for (int p = 0; p < 4; ++p) id[p] = page_at(a, w.seq, (uint32_t)(at + p * 64 + lane) * kGrp, end);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const uint64_t held = __builtin_amdgcn_ballot_w64(id[p] >= 0);
+          const int to = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(held >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)held, 0u));
+          if (id[p] >= 0 && to < 256) {
+            ids[to] = id[p];
+            groups[to] = at + p * 64 + lane;
+          }
+          count += scalar(__popcll(held));
+        }
+        at += 256;
+      } while (count < 256 && at < last_group);
+      if (count <= 256 && at >= last_group) n = i + (count + 3) / 4;
+      listed = min(count, 256);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const bool there = 4 * lane + group < count;
+      own = there ? ids[4 * lane + group] : -1;
+      own_key = there ? groups[4 * lane + group] * kGrp : kNoKey;
+      const bool whole = 4 * lane + 3 < count && groups[4 * lane + 3] * kGrp + kGrp <= first;
+      const uint64_t ragged = __builtin_amdgcn_ballot_w64(!whole);
+      plain = i + (ragged ? __ffsll((unsigned long long)ragged) - 1 : 64);
     }
   };
   Codes<D> codes, codes_v;
   auto fetch = [&](int i) __attribute__((always_inline)) {      // beyond the last stage: nothing is read, the counts stay
-    const int key = begin + i * 64 + group * kGrp;
+    const int key = KV == Kv::ROWS ? begin + i * 64 + group * kGrp : __builtin_amdgcn_readlane(own_key, i - from);
     const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i - from);
     const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
     if constexpr (KV == Kv::E4M3) {
       codes.load(only_v ? at.v : at.k, only_v ? a.v_scale : a.k_scale, at, lane);
       if constexpr (kWaves == 4) codes_v.load(at.v, a.v_scale, at, lane);
     } else {
-      fetch_group<D>(only_v ? at.v : at.k, only_v ? at.v_bytes : at.k_bytes, off, base + (i % kStages) * (2 * kHalf));
-      if constexpr (kWaves == 4) fetch_group<D>(at.v, at.v_bytes, off_v, base + (i % kStages) * (2 * kHalf) + kHalf);
+      fetch_group<D>(only_v ? at.v : at.k, only_v ? at.v_bytes : at.k_bytes, off, base + ((uint32_t)i % kStages) * (2 * kHalf));
+      if constexpr (kWaves == 4) fetch_group<D>(at.v, at.v_bytes, off_v, base + ((uint32_t)i % kStages) * (2 * kHalf) + kHalf);
     }
   };
   auto put = [&](int i) __attribute__((always_inline)) {
-    char *p = lds + (i % kStages) * (2 * kHalf) + to;
+    char *p = lds + ((uint32_t)i % kStages) * (2 * kHalf) + to;
     codes.store(p, only_v, lane);
     if constexpr (kWaves == 4) codes_v.store(p + kHalf, true, lane);
   };
@@ -749,7 +775,6 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     fetch(i + 3);
   };
   auto start = [&]() __attribute__((always_inline)) {
-    look_up(0);
     fetch(0);
     if constexpr (KV == Kv::E4M3) {
       put(0);
@@ -764,11 +789,16 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     }
     __builtin_amdgcn_s_barrier();
   };
+  if (end > begin) look_up(0);
+  else n = 0;
   if (!live) {      // no rows: the wave moves its share of the stages
     if (n > 0) {
       start();
       for (int i = 0; i < n; ++i) {
-        if (KV != Kv::ROWS && i - from > 60) look_up(i);
+        if (KV != Kv::ROWS && i - from > 60) {
+          look_up(i);
+          if (i >= n) break;
+        }
         publish(i);
       }
       wait_vm<0>();
@@ -782,19 +812,32 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     f32x16 sacc[2];              // scores: of the two blocks, or of even and odd tiles
     uint32_t pb[2][8];
     u32x4 fk[KF], fv[2][DT];     // 64 channels
+    constexpr int kF4 = QB == 1 ? 4 : 1;
+    u32x4 f0[kF4], f1[kF4];      // 128 channels
     const uint32_t lds0 = lds_addr(lds);
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     const int kr = lane & 31, vr = 4 * h + (lane >> 2 & 3);
-    const uint32_t k_lane = lds0 + kr * T::kRow + ((h ^ T::k_xor(kr)) * 16);                       // piece 2 j + h: ^ 32 j
-    const uint32_t v_lane = lds0 + kHalf + vr * T::kRow + T::v_xor(vr) * 16 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;   // channels 32 dt: ^ 64 dt
-    auto tile_at = [&](int t) __attribute__((always_inline)) { return (uint32_t)(((t >> 1) % kStages) * (2 * kHalf) + (t & 1) * 32 * T::kRow); };
+    auto tile_at = [&](int t) __attribute__((always_inline)) { return ((uint32_t)(t >> 1) % kStages) * (2 * kHalf) + (uint32_t)(t & 1) * (32 * T::kRow); };
+    const uint32_t k_lane = kr * T::kRow + ((h ^ T::k_xor(kr)) * 16);                       // piece 2 j + h: ^ 32 j
+    const uint32_t v_lane = kHalf + vr * T::kRow + T::v_xor(vr) * 16 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;   // channels 32 dt: ^ 64 dt
+    uint32_t lanes = k_lane | v_lane << 16;      // (128 channels: in one register)
+    auto k_at = [&](int t) __attribute__((always_inline)) {
+      if constexpr (QB == 2) return k_lane + (lds0 + tile_at(t));
+      asm volatile("" : "+v"(lanes));
+      return (lanes & 0xffffu) + (lds0 + tile_at(t));
+    };
+    auto v_at = [&](int t) __attribute__((always_inline)) {
+      if constexpr (QB == 2) return v_lane + (lds0 + tile_at(t));
+      asm volatile("" : "+v"(lanes));
+      return (lanes >> 16) + (lds0 + tile_at(t));
+    };
     auto read_k = [&](int t) __attribute__((always_inline)) {
-      const uint32_t p = k_lane + tile_at(t);
+      const uint32_t p = k_at(t);
 #pragma unroll
       for (int j = 0; j < KF; ++j) fk[j] = *(lds_u32x4 *)(uintptr_t)(p ^ (j * 32));
     };
     auto read_v = [&](int t) __attribute__((always_inline)) {
-      const uint32_t p = v_lane + tile_at(t);
+      const uint32_t p = v_at(t);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -805,48 +848,87 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
           fv[u][dt] = u32x4{x.x, x.y, y.x, y.y};
         }
     };
-    auto scores = [&](int b) __attribute__((always_inline)) {
-      f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // 128 channels: four fragments at a time
+    auto read_k4 = [&](int t, int half, u32x4(&f)[kF4]) __attribute__((always_inline)) {
+      const uint32_t p = k_at(t);
 #pragma unroll
-      for (int j = 0; j < KF; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fk[j]), rows.q[QB == 2 ? b : 0][j], acc, 0, 0, 0);
-      sacc[b] = acc;
+      for (int j = 0; j < 4; ++j) f[j] = *(lds_u32x4 *)(uintptr_t)(p ^ ((4 * half + j) * 32));
     };
-    auto output = [&](int b) __attribute__((always_inline)) {
+    auto read_v4 = [&](int t, int u, u32x4(&f)[kF4]) __attribute__((always_inline)) {
+      const uint32_t p = v_at(t) + u * 16 * T::kRow;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          rows.o[QB == 2 ? b : 0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fv[u][dt]), p, rows.o[QB == 2 ? b : 0][dt], 0, 0, 0);
+      for (int dt = 0; dt < 4; ++dt) {
+        const uint32_t q = p ^ (dt * 64);
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)q));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(q + 8 * T::kRow)));
+        f[dt] = u32x4{x.x, x.y, y.x, y.y};
+      }
+    };
+    // product number m of a phase: scores of bs (the first half), output of bo
+    auto product = [&](auto scores, auto output, int m, int bs, int bo) __attribute__((always_inline)) {
+      if (m < KF) {
+        if constexpr (decltype(scores)::value) {
+          const u32x4 f = QB == 2 ? fk[m % KF] : m < 4 ? f0[m % kF4] : f1[m % kF4];
+          f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          if (m) acc = sacc[bs];
+          sacc[bs] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), rows.q[QB == 2 ? bs : 0][m], acc, 0, 0, 0);
+        }
+      } else if constexpr (decltype(output)::value) {
+        const int u = (m - KF) / DT, dt = (m - KF) % DT;
+        const u32x4 f = QB == 2 ? fv[u][dt] : u == 0 ? f0[dt % kF4] : f1[dt % kF4];
+        const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pb[bo][4 * u], pb[bo][4 * u + 1], pb[bo][4 * u + 2], pb[bo][4 * u + 3]});
+        f32x16 &o = rows.o[QB == 2 ? bo : 0][dt];
+        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), w, o, 0, 0, 0);
       }
     };
     float sum0, sum1;
-    auto weight = [&](int b, int e) __attribute__((always_inline)) {
-      const float ref = rows.ref[QB == 2 ? b : 0];
-      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -ref));
-      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -ref));
+    auto weight = [&](int b, int e, float p0, float p1) __attribute__((always_inline)) {
       pb[b][e] = pack_bf16(p0, p1);
       asm("" : "+v"(pb[b][e]));      // (where paths meet the pair would be carried unpacked, in twice the registers)
       sum0 += p0;
       sum1 += p1;
     };
-    auto weights = [&](int b, int half) __attribute__((always_inline)) {
-      if (half == 0) sum0 = sum1 = 0.f;
+    auto weights = [&](int b) __attribute__((always_inline)) {
+      const float ref = rows.ref[QB == 2 ? b : 0];
+      sum0 = sum1 = 0.f;
 #pragma unroll
-      for (int e = 4 * half; e < 4 * half + 4; ++e) weight(b, e);
+      for (int e = 0; e < 8; ++e)
+        weight(b, e, __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e], a.c, -ref)), __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[b][2 * e + 1], a.c, -ref)));
     };
-    auto weights2 = [&](int b, int q) __attribute__((always_inline)) {
-      if (q == 0) sum0 = sum1 = 0.f;
+    // A phase: 2 KF products, and the weights of block bw among them, a pair of them to one or two products, each in three
+    // steps that stand next to the other pairs' (the exponent of the next, exp2 of this, sum and rounding of the last).  `then` follows
+    // product m (reads of fragments).
+    auto phase = [&](auto scores, auto output, int bw, int bs, int bo, auto &&then) __attribute__((always_inline)) {
+      constexpr int kPer = 2 * KF / 8;
+      const float ref = rows.ref[QB == 2 ? bw : 0];
+      sum0 = sum1 = 0.f;
+      float x0 = __builtin_fmaf(sacc[bw][0], a.c, -ref), x1 = __builtin_fmaf(sacc[bw][1], a.c, -ref), y0 = 0.f, y1 = 0.f;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int e = 2 * q; e < 2 * q + 2; ++e) weight(b, e);
-    };
-    auto recipe = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < KF; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x400, D == 64 ? 2 : 1, 0);    // exp2
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                  // MFMA
-        __builtin_amdgcn_sched_group_barrier(0x002, D == 64 ? 5 : 3, 0);    // fused multiply-add, pack, add
+      for (int m = 0; m < 2 * KF; ++m) {
+        product(scores, output, m, bs, bo);
+        const int e = m / kPer;
+        if (m % kPer == 0) {
+          const float z0 = y0, z1 = y1;
+          y0 = __builtin_amdgcn_exp2f(x0);
+          y1 = __builtin_amdgcn_exp2f(x1);
+          if (kPer == 1 && e) weight(bw, e - 1, z0, z1);
+          if (kPer == 1 && e < 7) {
+            x0 = __builtin_fmaf(sacc[bw][2 * e + 2], a.c, -ref);
+            x1 = __builtin_fmaf(sacc[bw][2 * e + 3], a.c, -ref);
+          }
+        } else {
+          weight(bw, e, y0, y1);
+          if (e < 7) {
+            x0 = __builtin_fmaf(sacc[bw][2 * e + 2], a.c, -ref);
+            x1 = __builtin_fmaf(sacc[bw][2 * e + 3], a.c, -ref);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        then(m);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if (kPer == 1) weight(bw, 7, y0, y1);
     };
     // block b's weights become part of its sums, with the references raised first where a sum went past 2^40
     auto settle = [&](int b) __attribute__((always_inline)) {
@@ -865,120 +947,51 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int e = 0; e < 16; ++e) rows.o[r][dt][e] *= f;
-        weights(b, 0);
-        weights(b, 1);
+        weights(b);
       }
       rows.l[r] += sum0 + sum1;
       __builtin_amdgcn_sched_barrier(0);
     };
+    using Yes = std::true_type;
+    using No = std::false_type;
     auto phase_a = [&](auto head, auto tail, int t) __attribute__((always_inline)) {
-      __builtin_amdgcn_sched_barrier(0);
-      scores(1);
-      weights(0, 0);
-      recipe();
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!decltype(tail)::value) read_k(t + 1);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!decltype(head)::value) output(1);
-      weights(0, 1);
-      recipe();
-      __builtin_amdgcn_sched_barrier(0);
-      read_v(t);
+      phase(Yes{}, std::bool_constant<!decltype(head)::value>{}, 0, 1, 1, [&](int m) __attribute__((always_inline)) {
+        if (m == KF - 1 && !decltype(tail)::value) read_k(t + 1);
+        if (m == 2 * KF - 1) read_v(t);
+      });
       settle(0);
     };
     auto phase_b = [&](auto tail) __attribute__((always_inline)) {
-      if constexpr (!decltype(tail)::value) scores(0);
-      weights(1, 0);
-      recipe();
-      __builtin_amdgcn_sched_barrier(0);
-      output(0);
-      weights(1, 1);
-      recipe();
+      phase(std::bool_constant<!decltype(tail)::value>{}, Yes{}, 1, 0, 0, [](int) {});
       settle(1);
-    };
-    // 128 channels: C(t) in quarters, of four products each
-    u32x4 f0[QB == 1 ? 4 : 1], f1[QB == 1 ? 4 : 1];
-    auto read_k4 = [&](int t, int half, u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
-      const uint32_t p = k_lane + tile_at(t);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[j] = *(lds_u32x4 *)(uintptr_t)(p ^ ((4 * half + j) * 32));
-    };
-    auto read_v4 = [&](int t, int u, u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
-      const uint32_t p = v_lane + tile_at(t) + u * 16 * T::kRow;
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt) {
-        const uint32_t q = p ^ (dt * 64);
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)q));
-        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(q + 8 * T::kRow)));
-        f[dt] = u32x4{x.x, x.y, y.x, y.y};
-      }
-    };
-    auto scores4 = [&](int b, int half, const u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
-      f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (half) acc = sacc[b];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[j]), rows.q[0][4 * half + j], acc, 0, 0, 0);
-      sacc[b] = acc;
-    };
-    auto output4 = [&](int b, int u, const u32x4(&f)[QB == 1 ? 4 : 1]) __attribute__((always_inline)) {
-      const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pb[b][4 * u], pb[b][4 * u + 1], pb[b][4 * u + 2], pb[b][4 * u + 3]});
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        rows.o[0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[dt]), p, rows.o[0][dt], 0, 0, 0);
-    };
-    auto quarter = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
     };
     // head: nothing of a tile before; tail: no tile after; pub: stage t / 2 + 1 is needed and t / 2 - 1 no more
     auto phase_c = [&](auto head, auto tail, auto pub, int b, int t) __attribute__((always_inline)) {
-      constexpr bool kHead = decltype(head)::value, kTail = decltype(tail)::value, kPub = decltype(pub)::value;
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!kTail) scores4(b ^ 1, 0, f0);
-      weights2(b, 0);
-      quarter();
-      if constexpr (!kHead) read_v4(t - 1, 0, f0);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!kTail) scores4(b ^ 1, 1, f1);
-      weights2(b, 1);
-      quarter();
-      if constexpr (!kHead) read_v4(t - 1, 1, f1);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!kHead) output4(b ^ 1, 0, f0);
-      weights2(b, 2);
-      quarter();
-      if constexpr (kPub) publish(t >> 1);
-      if constexpr (!kTail) read_k4(t + 2, 0, f0);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!kHead) output4(b ^ 1, 1, f1);
-      weights2(b, 3);
-      quarter();
-      if constexpr (!kTail) read_k4(t + 2, 1, f1);
+      constexpr bool kHead = decltype(head)::value, kTail = decltype(tail)::value;
+      phase(std::bool_constant<!kTail>{}, std::bool_constant<!kHead>{}, b, b ^ 1, b ^ 1, [&](int m) __attribute__((always_inline)) {
+        if (m == 3 && !kHead) read_v4(t - 1, 0, f0);
+        if (m == 7 && !kHead) read_v4(t - 1, 1, f1);
+        if (m == 11) {
+          if constexpr (decltype(pub)::value) publish(t >> 1);
+          if (!kTail) read_k4(t + 2, 0, f0);
+        }
+        if (m == 15 && !kTail) read_k4(t + 2, 1, f1);
+      });
       settle(b);
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    const int plain = first > begin ? (first - begin) >> 6 : 0;     // stages of which every row of the wave sees every key
     int i = 0;
     while (i < n) {
       // the stages from i on whose keys are all there and seen
-      int j = min(plain, n);
-      if constexpr (KV != Kv::ROWS) {
-        if (i - from > 60) look_up(i);
-        const uint64_t next = holes >> (i - from);
-        j = min(j, min(from + 61, next ? i + __ffsll((unsigned long long)next) - 1 : n));
+      if (KV != Kv::ROWS && i - from > 60) {
+        look_up(i);
+        if (i >= n) break;
       }
-      j = __builtin_amdgcn_readfirstlane(j);
+      const int j = scalar(min(plain, KV == Kv::ROWS ? n : min(n, from + 61)));
       if (j > i) {
         if constexpr (QB == 2) {
           read_k(2 * i);
-          scores(0);
+#pragma unroll
+          for (int m = 0; m < KF; ++m) product(Yes{}, No{}, m, 0, 0);
           phase_a(Yes{}, No{}, 2 * i);
           if (i < j - 1) do {
             asm volatile("" : "+v"(sacc[1]));   // (the same phase follows the loop: its instructions would be drawn before the branch)
@@ -993,12 +1006,13 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
           publish(i);
           phase_a(No{}, Yes{}, 2 * i + 1);
           phase_b(Yes{});
-          output(1);
+#pragma unroll
+          for (int m = KF; m < 2 * KF; ++m) product(No{}, Yes{}, m, 1, 1);
         } else {
           read_k4(2 * i, 0, f0);
           read_k4(2 * i, 1, f1);
-          scores4(0, 0, f0);
-          scores4(0, 1, f1);
+#pragma unroll
+          for (int m = 0; m < KF; ++m) product(Yes{}, No{}, m, 0, 0);
           read_k4(2 * i + 1, 0, f0);
           read_k4(2 * i + 1, 1, f1);
           if (i < j - 1) {
@@ -1017,19 +1031,24 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
           }
           phase_c(No{}, Yes{}, No{}, 1, 2 * i + 1);
           read_v4(2 * i + 1, 0, f0);
-          output4(1, 0, f0);
           read_v4(2 * i + 1, 1, f1);
-          output4(1, 1, f1);
+#pragma unroll
+          for (int m = KF; m < 2 * KF; ++m) product(No{}, Yes{}, m, 1, 1);
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
       } else {
-        const int shut = KV != Kv::ROWS ? __builtin_amdgcn_readlane(shuts, i - from) : 0;
-        const char *kt = lds + (i % kStages) * (2 * kHalf);
+        const char *kt = lds + ((uint32_t)i % kStages) * (2 * kHalf);
 #pragma unroll 1
         for (int t = 0; t < 2; ++t) {
-          const int sh = shut >> (2 * t) & 3;
-          const int key0 = begin + i * 64 + t * 32;
-          if (sh != 3) rows.tile(kt + t * 32 * T::kRow, kt + kHalf + t * 32 * T::kRow, a.c, key0, sh, key0 + 32 > first, lane);
+          int key0 = begin + i * 64 + t * 32, key1 = key0 + kGrp;
+          if constexpr (KV != Kv::ROWS) {
+            const int *const groups = list[wave][1] + 4 * (i - from) + 2 * t;
+            const int known = 4 * (i - from) + 2 * t;
+            key0 = known < listed ? scalar(groups[0]) * kGrp : kNoKey;
+            key1 = known + 1 < listed ? scalar(groups[1]) * kGrp : kNoKey;
+          }
+          if (key0 < end)
+            rows.tile(kt + t * 32 * T::kRow, kt + kHalf + t * 32 * T::kRow, a.c, key0, key1, key1 + kGrp > first, lane);
         }
         publish(i);
       }
