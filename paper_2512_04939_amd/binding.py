@@ -7,6 +7,7 @@ missing library raises at import of the symbols, a failing call raises ``LiteVGG
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -177,8 +178,15 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream() -> int:
+    torch = _torch()
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+@functools.lru_cache(maxsize=None)
+def _torch():
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    torch.cuda.current_stream()      # (initialises the device: the calls after this one only ask for the handle)
+    return torch
 
 
 def litevggt_strerror(code: int) -> str:
@@ -341,16 +349,24 @@ def alloc_cache(p: CacheParams, device="cuda") -> CacheBuffers:
 def _rows(t, heads: int, head_dim: int, what: str):
     """Count, pointer and row stride of a bf16 tensor [n, heads, head_dim] or [n, heads * head_dim]
     whose rows are contiguous; rows may be apart (slices of a joint projection)."""
-    import torch
+    width = heads * head_dim
     if t is None:
-        return 0, None, heads * head_dim
-    ok = t.dtype == torch.bfloat16 and t.dim() in (2, 3) and t.shape[1:].numel() == heads * head_dim and t.stride(-1) == 1
-    if ok and t.dim() == 3:
-        ok = t.shape[2] == head_dim and (heads == 1 or t.stride(1) == head_dim)
-    if not ok:
+        return 0, None, width
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        ok = shape[1] == heads and shape[2] == head_dim and stride[2] == 1 and (stride[1] == head_dim or heads == 1)
+    else:
+        ok = len(shape) == 2 and shape[1] == width and stride[1] == 1
+    if not ok or t.dtype is not _bf16():
         raise LiteVGGTError(f"{what}: bf16 rows of {heads} x {head_dim} contiguous values wanted, got "
-                            f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
-    return t.shape[0], t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * head_dim)
+                            f"{tuple(shape)} {t.dtype} with strides {stride}")
+    return shape[0], t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], width)
+
+
+@functools.lru_cache(maxsize=None)
+def _bf16():
+    import torch
+    return torch.bfloat16
 
 
 def litevggt_cache_write(p: CacheParams, cache: CacheBuffers, k, v, new_off, pos) -> None:

@@ -21,10 +21,12 @@ namespace lv {
 namespace {
 
 constexpr int kGrp = 16;                 // rows of K or V that are fetched together; a page holds a multiple of it
+constexpr int kUncut = 0x7fffffff;       // tiles of a piece where nothing is cut
 constexpr int kNoKey = 0x7fff0000;       // beyond every position that rows see
 constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
 constexpr float kRowRaise = 1.0995116e12f;   // 2^40
 constexpr int kSlotsAll = 512;           // workgroups resident on the chip: 256 CUs, 2 each
+constexpr int kWholeTiles = 8;           // no call is cut whose sequences have no more tiles (what joining costs)
 constexpr int kRounds = 3;               // a call's pieces fill these slots at most so often
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -48,6 +50,7 @@ struct Call {
   int rows_per_block, tile;              // rows of a block, keys of a tile (the unit of cutting): powers of two
   int block_shift, tile_shift;
   int target;                            // pieces to aim at; 0: nothing is cut
+  int *chosen;                           // tiles of a piece, for the kernel that joins them
   float *part;                           // [slot][rows_per_block][D] sums
   float2 *part_ml;                       // [slot][rows_per_block] reference, sum of weights
   int slots;
@@ -95,37 +98,51 @@ __device__ __forceinline__ int wave_sum_int(int v) {
   return v;
 }
 
-// How the keys are cut: the tiles of a piece.  Every wave works it out from the lengths, the same in all of them.  A
+// The sequence of the call that this lane looks at (step b of 64)
+__device__ __forceinline__ SeqInfo lane_seq(const Call &a, int b, int lane) {
+  SeqInfo q = {0, 0, 0, 0, 0, 0, 0};
+  if (b + lane < a.n_seq) q = seq_info(a, b + lane);
+  return q;
+}
+
+// How the keys are cut: the tiles of a piece.  Every wave works it out from the lengths, the same in all of them; `me`: lane_seq(0).  A
 // candidate per lane: its pieces' number, and from that how long the call would take in tiles (rounds of the
 // chip's slots, each as long as a piece and what a workgroup costs to start and end).
-__device__ int piece_tiles(const Call &a, int lane) {
-  if (a.target == 0) return 0x7fffffff;
-  double work = 0.0;
-  int most = 0;
-  for (int b = 0; b < a.n_seq; b += 64)
-    if (b + lane < a.n_seq) {
-      const SeqInfo q = seq_info(a, b + lane);
-      work += (double)q.blocks * q.tiles * a.kv_heads;
-      most = max(most, q.blocks ? q.tiles : 0);
-    }
-  work = wave_sum(work);
+__device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInfo &me) {
+  if (a.target == 0) return kUncut;
+  float work = (float)me.blocks * (float)me.tiles;
+  int most = me.blocks ? me.tiles : 0;
+  for (int b = 64; b < a.n_seq; b += 64) {
+    const SeqInfo q = lane_seq(a, b, lane);
+    work += (float)q.blocks * (float)q.tiles;
+    most = max(most, q.blocks ? q.tiles : 0);
+  }
+  if (a.n_seq > 1) {
+    work = wave_sum(work);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
-  most = __builtin_amdgcn_readfirstlane(most);
-  if (most <= 1) return 0x7fffffff;
-  // lane 63: uncut; the others: 1 .. kRounds rounds, 21 steps of 5 % less pieces in each
-  const double pieces = (double)a.target * (1 + lane / 21) / kRounds * (1.0 - 0.04 * (lane % 21));
-  int s = lane == 63 ? most : (int)fmin((double)most, fmax(1.0, ceil(work / pieces)));
+    for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+  } else {
+    work = __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, work)));
+  }
+  work *= (float)a.kv_heads;
+  most = scalar(most);
+  if (most <= 1) return kUncut;
+  // lane 63: uncut; the others: 1 .. kRounds rounds, 21 steps of 4 % less pieces in each.  (A hair longer than the quotient: the
+  // pieces are at most as many as were aimed at and one for each block, whatever the roundings.)
+  const float pieces = (float)a.target * (float)(1 + lane / 21) / kRounds * (1.0f - 0.04f * (float)(lane % 21));
+  const int s = lane == 63 ? most : (int)fminf((float)most, fmaxf(1.0f, ceilf(work / pieces * 1.0001f)));
   float units = 0.f;
+  const float inv = 1.0f / (float)s;
   if (a.n_seq <= 16) {
     for (int i = 0; i < a.n_seq; ++i) {
-      const SeqInfo q = seq_info(a, i);
-      units += (float)q.blocks * a.kv_heads * max((q.tiles + s - 1) / s, 1);
+      const int tiles = __builtin_amdgcn_readlane(me.tiles, i);
+      units += (float)__builtin_amdgcn_readlane(me.blocks, i) * fmaxf(ceilf((float)tiles * inv - 1e-4f), 1.0f);
     }
+    units *= (float)a.kv_heads;
   } else {
-    units = (float)(work / s) + 0.5f * a.n_seq * a.kv_heads;
+    units = work * inv + 0.5f * (float)a.n_seq * (float)a.kv_heads;
   }
-  const float cost = ceilf(units / kSlotsAll) * (min(s, most) + 3) + (s < most ? 6.f : 0.f);
+  const float cost = ceilf(units * (1.0f / kSlotsAll)) * (float)(min(s, most) + 3) + (s < most ? 6.f : 0.f);
   // the least, the longer pieces of two
   float best = cost * 4096.f - (float)min(s, 4095);
   int arg = s;
@@ -138,10 +155,11 @@ __device__ int piece_tiles(const Call &a, int lane) {
       arg = w;
     }
   }
-  return __builtin_amdgcn_readfirstlane(arg);
+  return scalar(arg);
 }
 
-__device__ __forceinline__ int pieces_of(int tiles, int s) { return max((tiles + s - 1) / s, 1); }
+__device__ __forceinline__ int pieces_of(int tiles, int s) { return s == kUncut ? 1 : max((int)((uint32_t)(tiles + s - 1) / (uint32_t)s), 1); }
+__device__ __forceinline__ int units_of(const Call &a, const SeqInfo &q, int s) { return q.blocks * a.kv_heads * pieces_of(q.tiles, s); }
 
 struct Work {
   int seq, head, block, pieces;
@@ -149,7 +167,7 @@ struct Work {
   int slot;
 };
 
-// Units of the sequences before `seq` (exclusive), for lane's sequence of a 64-sequence step
+// Sum over the lanes before this one; total: over all
 __device__ __forceinline__ int wave_scan(int v, int lane, int &total) {
   int x = v;
 #pragma unroll
@@ -161,63 +179,76 @@ __device__ __forceinline__ int wave_scan(int v, int lane, int &total) {
   return x - v;
 }
 
-// The u-th piece of the call in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
+// The workgroup's piece of the call, in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
 // side, and an XCD gets a range of them.
-__device__ bool find_work(const Call &a, int s, int lane, Work &w, SeqInfo &info) {
-  const int nb = gridDim.x;
-  int total = 0;
-  for (int b = 0; b < a.n_seq; b += 64) {
-    int u = 0;
-    if (b + lane < a.n_seq) {
-      const SeqInfo q = seq_info(a, b + lane);
-      u = q.blocks * a.kv_heads * pieces_of(q.tiles, s);
-    }
-    total += wave_sum_int(u);
+__device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
+  const SeqInfo me = lane_seq(a, 0, lane);
+  const int s = piece_tiles(a, lane, me);
+  if (a.target && blockIdx.x == 0 && threadIdx.x == 0) *a.chosen = s;
+  const int mine = units_of(a, me, s);
+  int total = scalar(mine), start = 0, seen = 0;     // of the first 64 sequences; units before the lane's
+  if (a.n_seq > 1) {
+    start = wave_scan(mine, lane, seen);
+    total = scalar(seen);
   }
-  total = __builtin_amdgcn_readfirstlane(total);
-  const int per = (total + kXcd - 1) / kXcd, x = blockIdx.x % kXcd, y = blockIdx.x / kXcd;
-  const int u = __builtin_amdgcn_readfirstlane(x * per + y);
-  if (y >= per || u >= total || u >= nb) return false;
-  int before = 0;
-  for (int b = 0; b < a.n_seq; b += 64) {
-    int mine = 0;
-    if (b + lane < a.n_seq) {
-      const SeqInfo q = seq_info(a, b + lane);
-      mine = q.blocks * a.kv_heads * pieces_of(q.tiles, s);
-    }
-    int sum;
-    const int start = before + wave_scan(mine, lane, sum);
+  const int first64 = total;
+  for (int b = 64; b < a.n_seq; b += 64) total += scalar(wave_sum_int(units_of(a, lane_seq(a, b, lane), s)));
+  const int per = (total + kXcd - 1) / kXcd, y = blockIdx.x / kXcd, u = (int)(blockIdx.x % kXcd) * per + y;
+  if (y >= per || u >= total || u >= (int)gridDim.x) return false;
+  int local = u, j = 0;
+  w.seq = 0;
+  if (a.n_seq > 1 && u < first64) {
     const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= start && u < start + mine);
-    if (hit) {
-      const int j = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)hit) - 1);
-      w.seq = b + j;
-      const int local = u - __builtin_amdgcn_readlane(start, j);
-      info = seq_info(a, w.seq);
-      w.pieces = pieces_of(info.tiles, s);
-      const int per_head = w.pieces * info.blocks, len = (info.tiles + w.pieces - 1) / w.pieces;
-      w.head = local / per_head;
-      const int piece = (local - w.head * per_head) / info.blocks;
-      w.block = local - (w.head * w.pieces + piece) * info.blocks;
-      w.t0 = min(piece * len, info.tiles);
-      w.t1 = min(w.t0 + len, info.tiles);
-      w.slot = u;
-      // (scalars from here on, whatever they were worked out with)
-      w.seq = scalar(w.seq);
-      w.head = scalar(w.head);
-      w.block = scalar(w.block);
-      w.pieces = scalar(w.pieces);
-      w.t0 = scalar(w.t0);
-      w.t1 = scalar(w.t1);
-      info.q0 = scalar(info.q0);
-      info.nq = scalar(info.nq);
-      info.k0 = scalar(info.k0);
-      info.nk = scalar(info.nk);
-      info.p0 = scalar(info.p0);
-      return true;
-    }
-    before += sum;
+    j = scalar(__ffsll((unsigned long long)hit) - 1);
+    w.seq = j;
+    local = u - __builtin_amdgcn_readlane(start, j);
   }
-  return false;
+  if (u < first64) {
+    info.q0 = __builtin_amdgcn_readlane(me.q0, j);
+    info.nq = __builtin_amdgcn_readlane(me.nq, j);
+    info.k0 = __builtin_amdgcn_readlane(me.k0, j);
+    info.nk = __builtin_amdgcn_readlane(me.nk, j);
+    info.p0 = __builtin_amdgcn_readlane(me.p0, j);
+    info.blocks = __builtin_amdgcn_readlane(me.blocks, j);
+    info.tiles = __builtin_amdgcn_readlane(me.tiles, j);
+  } else {
+    int before = first64;
+    for (int b = 64;; b += 64) {
+      const SeqInfo q = lane_seq(a, b, lane);
+      const int v = units_of(a, q, s);
+      int sum;
+      const int at = before + wave_scan(v, lane, sum);
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= at && u < at + v);
+      if (hit) {
+        j = scalar(__ffsll((unsigned long long)hit) - 1);
+        w.seq = b + j;
+        local = u - __builtin_amdgcn_readlane(at, j);
+        info = seq_info(a, w.seq);
+        break;
+      }
+      before += scalar(sum);
+      if (b + 64 >= a.n_seq) return false;      // (lengths that changed meanwhile)
+    }
+  }
+  // (scalars from here on, whatever they were worked out with)
+  info.q0 = scalar(info.q0);
+  info.nq = scalar(info.nq);
+  info.k0 = scalar(info.k0);
+  info.nk = scalar(info.nk);
+  info.p0 = scalar(info.p0);
+  info.blocks = scalar(info.blocks);
+  info.tiles = scalar(info.tiles);
+  w.seq = scalar(w.seq);
+  w.pieces = scalar(pieces_of(info.tiles, s));
+  const int len = w.pieces == 1 ? info.tiles : (int)((uint32_t)(info.tiles + w.pieces - 1) / (uint32_t)w.pieces);
+  const int hp = (int)((uint32_t)local / (uint32_t)info.blocks);      // head and piece
+  w.block = scalar(local - hp * info.blocks);
+  const int head = w.pieces == 1 ? hp : (int)((uint32_t)hp / (uint32_t)w.pieces), piece = hp - head * w.pieces;
+  w.head = scalar(head);
+  w.t0 = scalar(min(piece * len, info.tiles));
+  w.t1 = min(w.t0 + scalar(len), info.tiles);
+  w.slot = u;
+  return true;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -535,7 +566,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
-  if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
+  if (!find_work(a, lane, w, s)) return;
   const int n_rows = s.nq * a.group, row0 = w.block * 32;
   const int last = scalar(limit_of(a, s, min(row0 + 31, n_rows - 1) / a.group));     // keys that some row sees
   const int first = scalar(limit_of(a, s, row0 / a.group));                          // keys that every row sees
@@ -688,7 +719,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
-  if (!find_work(a, piece_tiles(a, lane), lane, w, s)) return;
+  if (!find_work(a, lane, w, s)) return;
   const int n_rows = s.nq * a.group, block0 = w.block * 256, row0 = block0 + wave * kRows;
   const int last = scalar(limit_of(a, s, min(block0 + 255, n_rows - 1) / a.group));
   const bool live = row0 < n_rows;
@@ -1093,23 +1124,22 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int per_token = (a.heads + kRowsWg - 1) / kRowsWg;
   const int tok = blockIdx.x / per_token;
-  const int piece_len = piece_tiles(a, lane);
+  const int piece_len = *a.chosen;
+  if (piece_len == kUncut) return;
   // the token's sequence and the number of the first piece of it
   int seq = -1, before = 0;
   for (int b = 0; b < a.n_seq && seq < 0; b += 64) {
-    int units = 0;
-    bool in = false;
-    if (b + lane < a.n_seq) {
-      const SeqInfo q = seq_info(a, b + lane);
-      units = q.blocks * a.kv_heads * pieces_of(q.tiles, piece_len);
-      in = tok >= q.q0 && tok < q.q0 + q.nq;
+    const SeqInfo q = lane_seq(a, b, lane);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(tok >= q.q0 && tok < q.q0 + q.nq);
+    if (a.n_seq == 1) {
+      seq = hit ? 0 : -1;
+      break;
     }
     int sum;
-    const int start = before + wave_scan(units, lane, sum);
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(in);
+    const int start = before + wave_scan(units_of(a, q, piece_len), lane, sum);
     before += sum;
     if (hit) {
-      const int j = __ffsll((unsigned long long)hit) - 1;
+      const int j = scalar(__ffsll((unsigned long long)hit) - 1);
       seq = b + j;
       before = __builtin_amdgcn_readlane(start, j);
     }
@@ -1200,7 +1230,7 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t 
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (blocks that fill the chip several times over leave nothing to gain)
-  const int64_t target = f.units >= 4 * kSlotsAll && !f.few ? 0 : tiles <= 1 ? 0 : kRounds * kSlotsAll;
+  const int64_t target = f.units >= 4 * kSlotsAll && !f.few ? 0 : tiles <= kWholeTiles ? 0 : kRounds * kSlotsAll;
   f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
   return f;
 }
@@ -1211,7 +1241,7 @@ int64_t slots_of(const Form &f) { return f.units + f.target + kXcd; }
 size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
   const Form f = form_of(n_q, n_seq, heads, kv_heads, head_dim, most_keys);
   if (f.target == 0) return 0;
-  return align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
+  return 256 + align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
 }
 
 template <typename K, size_t LDS>
@@ -1269,8 +1299,9 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.tile_shift = __builtin_ctz(f.tile);
   c.target = f.target;
   c.slots = (int)slots_of(f);
-  c.part = (float *)ws;
-  c.part_ml = f.target ? (float2 *)((float *)ws + (size_t)c.slots * f.rows * x.head_dim) : nullptr;
+  c.chosen = (int *)ws;
+  c.part = f.target ? (float *)((char *)ws + 256) : nullptr;
+  c.part_ml = f.target ? (float2 *)(c.part + (size_t)c.slots * f.rows * x.head_dim) : nullptr;
   const uint32_t grid = (uint32_t)((f.units + f.target + kXcd - 1) / kXcd * kXcd);
   auto by_kv = [&](auto kv) {
     constexpr Kv KV = decltype(kv)::value;
