@@ -464,7 +464,7 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
 size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
   CacheView cv;
   if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
-  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, (int64_t)p->max_pages << cv.page_shift);
+  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.e4m3, (int64_t)p->max_pages << cv.page_shift);
 }
 
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
@@ -509,7 +509,7 @@ static int check_cross(const litevggt_cross_params *p) {
 size_t litevggt_cross_attn_ws_bytes(const litevggt_cross_params *p, int64_t n_q, int64_t n_kv) {
   if (check_cross(p) || n_q < 1 || !count_ok(n_q, p->heads) || !count_ok(n_kv, p->kv_heads)) return 0;
   const size_t norm = p->qk_norm ? align_up((size_t)n_kv * p->kv_heads * p->head_dim * 2, 256) : 0;
-  return kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, n_kv) + norm;
+  return kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, false, n_kv) + norm;
 }
 
 int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void *q, int64_t q_stride,
@@ -530,7 +530,7 @@ int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void 
   a.k = k;
   a.k_stride = k_stride;
   if (p->qk_norm && n_kv > 0) {
-    uint16_t *kn = (uint16_t *)((char *)ws + kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, n_kv));
+    uint16_t *kn = (uint16_t *)((char *)ws + kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, false, n_kv));
     if ((rc = launch_norm_rows((const uint16_t *)k, k_stride, (int)n_kv, p->kv_heads, p->head_dim, kn, st))) return rc;
     a.k = kn;
     a.k_stride = kw;

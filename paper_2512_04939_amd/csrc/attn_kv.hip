@@ -13,6 +13,8 @@
 //
 // Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
 // weights already lie as the B operand of O^T += V^T P^T.  K and V lie in LDS as rows; V's fragments come out by transposing reads.
+#include <algorithm>
+
 #include "internal.h"
 #include "common.h"
 
@@ -25,8 +27,9 @@ constexpr int kUncut = 0x7fffffff;       // tiles of a piece where nothing is cu
 constexpr int kNoKey = 0x7fff0000;       // beyond every position that rows see
 constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
 constexpr float kRowRaise = 1.0995116e12f;   // 2^40
-constexpr int kSlotsAll = 512;           // workgroups resident on the chip: 256 CUs, 2 each
+constexpr int kCus = 256;
 constexpr int kWholeTiles = 8;           // no call is cut whose sequences have no more tiles (what joining costs)
+constexpr int kSide = 16;                // units side by side that one XCD takes, at most
 constexpr int kRounds = 3;               // a call's pieces fill these slots at most so often
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -50,6 +53,8 @@ struct Call {
   int rows_per_block, tile;              // rows of a block, keys of a tile (the unit of cutting): powers of two
   int block_shift, tile_shift;
   int target;                            // pieces to aim at; 0: nothing is cut
+  int most_units;                        // units that there is room for
+  int resident;                          // workgroups that the chip holds at once
   int *chosen;                           // tiles of a piece, for the kernel that joins them
   float *part;                           // [slot][rows_per_block][D] sums
   float2 *part_ml;                       // [slot][rows_per_block] reference, sum of weights
@@ -105,6 +110,13 @@ __device__ __forceinline__ SeqInfo lane_seq(const Call &a, int b, int lane) {
   return q;
 }
 
+// One sequence whose blocks fill the chip's slots once or more: the blocks of its first heads, as many as fill whole rounds, are not
+// cut, those of the others are, so that the last round is as full.
+__device__ __forceinline__ int whole_heads(const Call &a, int blocks) {
+  if (a.n_seq > 1 || blocks == 0 || a.target == 0) return 0;
+  return min((int)((uint32_t)(blocks * a.kv_heads / a.resident * a.resident) / (uint32_t)blocks), a.kv_heads);
+}
+
 // How the keys are cut: the tiles of a piece.  Every wave works it out from the lengths, the same in all of them; `me`: lane_seq(0).  A
 // candidate per lane: its pieces' number, and from that how long the call would take in tiles (rounds of the
 // chip's slots, each as long as a piece and what a workgroup costs to start and end).
@@ -124,9 +136,11 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
   } else {
     work = __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, work)));
   }
-  work *= (float)a.kv_heads;
+  const int heads = a.kv_heads - whole_heads(a, me.blocks);     // (of one sequence: every lane that has one)
+  work *= (float)(a.n_seq > 1 ? a.kv_heads : scalar(heads));
   most = scalar(most);
-  if (most <= 1) return kUncut;
+  if (most <= 1 || work == 0.f) return kUncut;
+  static_assert(kRounds == 3, "candidates");
   // lane 63: uncut; the others: 1 .. kRounds rounds, 21 steps of 4 % less pieces in each.  (A hair longer than the quotient: the
   // pieces are at most as many as were aimed at and one for each block, whatever the roundings.)
   const float pieces = (float)a.target * (float)(1 + lane / 21) / kRounds * (1.0f - 0.04f * (float)(lane % 21));
@@ -138,11 +152,12 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
       const int tiles = __builtin_amdgcn_readlane(me.tiles, i);
       units += (float)__builtin_amdgcn_readlane(me.blocks, i) * fmaxf(ceilf((float)tiles * inv - 1e-4f), 1.0f);
     }
-    units *= (float)a.kv_heads;
+    units *= (float)(a.n_seq > 1 ? a.kv_heads : scalar(heads));
   } else {
     units = work * inv + 0.5f * (float)a.n_seq * (float)a.kv_heads;
   }
-  const float cost = ceilf(units * (1.0f / kSlotsAll)) * (float)(min(s, most) + 3) + (s < most ? 6.f : 0.f);
+  // (a piece's sums are written and read: 8 stages of many rows' time for the slots' 512 of 64 KB)
+  const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 32 ? 11 : 3)) + (s < most ? 6.f : 0.f);
   // the least, the longer pieces of two
   float best = cost * 4096.f - (float)min(s, 4095);
   int arg = s;
@@ -185,7 +200,8 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   const SeqInfo me = lane_seq(a, 0, lane);
   const int s = piece_tiles(a, lane, me);
   if (a.target && blockIdx.x == 0 && threadIdx.x == 0) *a.chosen = s;
-  const int mine = units_of(a, me, s);
+  const int whole = scalar(whole_heads(a, me.blocks)) * scalar(me.blocks);     // units that are not cut, ahead of the others
+  const int mine = a.n_seq > 1 ? units_of(a, me, s) : whole + (me.blocks * a.kv_heads - whole) * pieces_of(me.tiles, s);
   int total = scalar(mine), start = 0, seen = 0;     // of the first 64 sequences; units before the lane's
   if (a.n_seq > 1) {
     start = wave_scan(mine, lane, seen);
@@ -193,8 +209,11 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   }
   const int first64 = total;
   for (int b = 64; b < a.n_seq; b += 64) total += scalar(wave_sum_int(units_of(a, lane_seq(a, b, lane), s)));
-  const int per = (total + kXcd - 1) / kXcd, y = blockIdx.x / kXcd, u = (int)(blockIdx.x % kXcd) * per + y;
-  if (y >= per || u >= total || u >= (int)gridDim.x) return false;
+  // XCDs take turns with a few units that stand side by side
+  const int side = a.rows_per_block == 32 ? 1 : a.n_seq > 1 ? 8 : min(max(scalar(me.blocks), 1), kSide);
+  const uint32_t y = blockIdx.x / kXcd, turn = y / (uint32_t)side;
+  const int u = (int)((turn * kXcd + blockIdx.x % kXcd) * side + (y - turn * side));
+  if (u >= total || u >= a.most_units) return false;
   int local = u, j = 0;
   w.seq = 0;
   if (a.n_seq > 1 && u < first64) {
@@ -239,15 +258,17 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   info.blocks = scalar(info.blocks);
   info.tiles = scalar(info.tiles);
   w.seq = scalar(w.seq);
-  w.pieces = scalar(pieces_of(info.tiles, s));
+  w.pieces = u < whole ? 1 : scalar(pieces_of(info.tiles, s));
+  w.slot = u - whole;
+  const int skip = u < whole ? 0 : whole / info.blocks;     // heads
+  local -= skip * info.blocks;
   const int len = w.pieces == 1 ? info.tiles : (int)((uint32_t)(info.tiles + w.pieces - 1) / (uint32_t)w.pieces);
   const int hp = (int)((uint32_t)local / (uint32_t)info.blocks);      // head and piece
   w.block = scalar(local - hp * info.blocks);
   const int head = w.pieces == 1 ? hp : (int)((uint32_t)hp / (uint32_t)w.pieces), piece = hp - head * w.pieces;
-  w.head = scalar(head);
+  w.head = skip + scalar(head);
   w.t0 = scalar(min(piece * len, info.tiles));
   w.t1 = min(w.t0 + scalar(len), info.tiles);
-  w.slot = u;
   return true;
 }
 
@@ -740,7 +761,9 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   // that this wave fetches.
   __shared__ int list[KV == Kv::ROWS ? 1 : kWaves][2][KV == Kv::ROWS ? 1 : 256];
   int n = KV == Kv::ROWS ? scalar(end > begin ? (end - begin + 63) / 64 : 0) : 0x7fffffff;    // stages (pages: once it is known)
-  int from = 0, listed = 0, own = 0, own_key = 0;
+  // Of a group: rows before it in the pool, and how many of its 16 exist, in the bits from 24 of the upper word on.
+  int from = 0, listed = 0;
+  uint32_t own = 0, own_hi = 0;
   int plain = KV == Kv::ROWS ? (first > begin ? (first - begin) >> 6 : 0) : 0;     // stages up to this one hold 64 keys that every row sees
   auto look_up = [&](int i) __attribute__((always_inline)) {
     if constexpr (KV != Kv::ROWS) {
@@ -770,25 +793,52 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
       listed = min(count, 256);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       const bool there = 4 * lane + group < count;
-      own = there ? ids[4 * lane + group] : -1;
-      own_key = there ? groups[4 * lane + group] * kGrp : kNoKey;
+      const int key = there ? groups[4 * lane + group] * kGrp : 0, id = there ? ids[4 * lane + group] : 0;
+      const int64_t row = (((int64_t)id * a.kv_heads + w.head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+      own = (uint32_t)row;
+      own_hi = (uint32_t)(row >> 32) | (there ? (uint32_t)min(end - key, kGrp) << 24 : 0u);
       const bool whole = 4 * lane + 3 < count && groups[4 * lane + 3] * kGrp + kGrp <= first;
       const uint64_t ragged = __builtin_amdgcn_ballot_w64(!whole);
       plain = i + (ragged ? __ffsll((unsigned long long)ragged) - 1 : 64);
     }
   };
   Codes<D> codes, codes_v;
-  auto fetch = [&](int i) __attribute__((always_inline)) {      // beyond the last stage: nothing is read, the counts stay
-    const int key = KV == Kv::ROWS ? begin + i * 64 + group * kGrp : __builtin_amdgcn_readlane(own_key, i - from);
-    const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(own, i - from);
-    const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
-    if constexpr (KV == Kv::E4M3) {
-      codes.load(only_v ? at.v : at.k, only_v ? a.v_scale : a.k_scale, at, lane);
-      if constexpr (kWaves == 4) codes_v.load(at.v, a.v_scale, at, lane);
+  // Rows: what the next fetch brings, and the rows that are left of it on
+  const int64_t row_first = (int64_t)s.k0 + begin + group * kGrp;
+  const char *next_k = a.k + row_first * a.k_stride + w.head * T::kRow, *next_v = a.v + row_first * a.v_stride + w.head * T::kRow;
+  if (only_v) next_k = next_v;
+  const int64_t step_k = 64 * (only_v ? a.v_stride : a.k_stride), step_v = 64 * a.v_stride;
+  const int stride_k = (int)(only_v ? a.v_stride : a.k_stride), stride_v = (int)a.v_stride;
+  int left = end - begin - group * kGrp;
+  uint32_t ring = base;          // where it goes
+  // the stages in their order; beyond the last one nothing is read, the counts stay
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    if constexpr (KV == Kv::ROWS) {
+      int bytes_k = (kGrp - 1) * stride_k + T::kRow, bytes_v = (kGrp - 1) * stride_v + T::kRow;
+      if (__builtin_expect(left < kGrp, 0)) {
+        bytes_k = left > 0 ? (left - 1) * stride_k + T::kRow : 0;
+        bytes_v = left > 0 ? (left - 1) * stride_v + T::kRow : 0;
+      }
+      fetch_group<D>(next_k, bytes_k, off, ring);
+      if constexpr (kWaves == 4) fetch_group<D>(next_v, bytes_v, off_v, ring + kHalf);
+      next_k += step_k;
+      next_v += step_v;
+      left -= 64;
     } else {
-      fetch_group<D>(only_v ? at.v : at.k, only_v ? at.v_bytes : at.k_bytes, off, base + ((uint32_t)i % kStages) * (2 * kHalf));
-      if constexpr (kWaves == 4) fetch_group<D>(at.v, at.v_bytes, off_v, base + ((uint32_t)i % kStages) * (2 * kHalf) + kHalf);
+      constexpr int kBytes = KV == Kv::E4M3 ? D : 2 * D;
+      const uint32_t lo = __builtin_amdgcn_readlane(own, i - from), hi = __builtin_amdgcn_readlane(own_hi, i - from);
+      Group at;
+      at.row = (int64_t)((uint64_t)(hi & 0xffffffu) << 32 | lo);
+      at.k_bytes = at.v_bytes = (int)(hi >> 24) * kBytes;
+      if constexpr (KV == Kv::E4M3) {
+        codes.load((only_v ? a.v : a.k) + at.row * kBytes, only_v ? a.v_scale : a.k_scale, at, lane);
+        if constexpr (kWaves == 4) codes_v.load(a.v + at.row * kBytes, a.v_scale, at, lane);
+      } else {
+        fetch_group<D>((only_v ? a.v : a.k) + at.row * kBytes, at.k_bytes, off, ring);
+        if constexpr (kWaves == 4) fetch_group<D>(a.v + at.row * kBytes, at.k_bytes, off_v, ring + kHalf);
+      }
     }
+    if constexpr (KV != Kv::E4M3) ring = ring == base + (kStages - 1) * (2 * kHalf) ? base : ring + 2 * kHalf;
   };
   auto put = [&](int i) __attribute__((always_inline)) {
     char *p = lds + ((uint32_t)i % kStages) * (2 * kHalf) + to;
@@ -1146,7 +1196,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   }
   if (seq < 0) return;
   const SeqInfo s = seq_info(a, seq);
-  const int pieces = pieces_of(s.tiles, piece_len);
+  const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
   if (pieces == 1) return;          // written already
   const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
   const int hq = blockIdx.x % per_token * kRowsWg + in_wg;
@@ -1154,7 +1204,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int head = (there ? hq : 0) / a.group, g = (there ? hq : 0) % a.group;
   const int r = (tok - s.q0) * a.group + g;
   const int block = r >> a.block_shift, in_block = r & (a.rows_per_block - 1);
-  const int64_t slot0 = before + (int64_t)head * pieces * s.blocks + block;
+  const int64_t slot0 = before + (int64_t)max(head - whole, 0) * pieces * s.blocks + block;
   if (slot0 + (int64_t)(pieces - 1) * s.blocks >= a.slots) return;
   auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
   float top = kUnset;
@@ -1190,7 +1240,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
       for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
     }
   }
-  if (!there) return;
+  if (!there || head < whole) return;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   *(u32x2 *)(a.o + (int64_t)tok * a.o_stride + hq * D + ch) =
       u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
@@ -1215,33 +1265,39 @@ __global__ __launch_bounds__(256) void k_norm_rows(const uint16_t *k, int64_t st
 struct Form {
   bool few;
   int rows, tile;
+  int resident;      // workgroups that the chip holds at once
   int64_t units;     // blocks of the call at most, all heads
   int target;        // pieces beside these at most
 };
 
 // Which kernel: by the rows that a (sequence, kv head) has on average.
-Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
+Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
   Form f;
   const int group = heads / kv_heads;
   const double rows = (double)n_q * group / n_seq;
   f.few = rows <= 64.0;
   f.rows = f.few ? 32 : 256;
   f.tile = f.few ? 128 : 64;
+  f.resident = kCus * (head_dim == 64 || (f.few && e4m3) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (blocks that fill the chip several times over leave nothing to gain)
-  const int64_t target = f.units >= 4 * kSlotsAll && !f.few ? 0 : tiles <= kWholeTiles ? 0 : kRounds * kSlotsAll;
+  const int64_t target = f.units >= 4 * f.resident && !f.few && n_seq > 1 ? 0 : tiles <= kWholeTiles ? 0 : kRounds * f.resident;
   f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
   return f;
 }
-int64_t slots_of(const Form &f) { return f.units + f.target + kXcd; }
+// (one sequence: beyond the heads that fill whole rounds)
+int64_t slots_of(const Form &f, int n_seq, int kv_heads) {
+  const int64_t blocks = f.units / kv_heads;
+  return (n_seq > 1 || f.units < f.resident ? f.units : std::min(f.units, f.resident + 2 * blocks)) + f.target;
+}
 
 }  // namespace
 
-size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
-  const Form f = form_of(n_q, n_seq, heads, kv_heads, head_dim, most_keys);
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
+  const Form f = form_of(n_q, n_seq, heads, kv_heads, head_dim, e4m3, most_keys);
   if (f.target == 0) return 0;
-  return 256 + align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
+  return 256 + align_up((size_t)slots_of(f, n_seq, kv_heads) * f.rows * (head_dim + 2) * sizeof(float), 256);
 }
 
 template <typename K, size_t LDS>
@@ -1265,7 +1321,7 @@ static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t 
 
 int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   const int64_t most = x.paged ? (int64_t)x.cv.max_pages << x.cv.page_shift : x.n_kv;
-  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, most);
+  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, x.paged && x.cv.e4m3, most);
   Call c;
   c.q = x.q;
   c.o = x.o;
@@ -1298,11 +1354,14 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.block_shift = __builtin_ctz(f.rows);
   c.tile_shift = __builtin_ctz(f.tile);
   c.target = f.target;
-  c.slots = (int)slots_of(f);
+  c.slots = (int)slots_of(f, x.n_seq, x.kv_heads);
+  c.resident = f.resident;
+  c.most_units = (int)(f.units + f.target);
   c.chosen = (int *)ws;
   c.part = f.target ? (float *)((char *)ws + 256) : nullptr;
   c.part_ml = f.target ? (float2 *)(c.part + (size_t)c.slots * f.rows * x.head_dim) : nullptr;
-  const uint32_t grid = (uint32_t)((f.units + f.target + kXcd - 1) / kXcd * kXcd);
+  const int side = f.few ? 1 : x.n_seq > 1 ? 8 : kSide;
+  const uint32_t grid = (uint32_t)((f.units + f.target) / kXcd * kXcd + kXcd * (side + 1));     // (whole turns of units side by side)
   auto by_kv = [&](auto kv) {
     constexpr Kv KV = decltype(kv)::value;
     return x.head_dim == 64 ? launch_form<KV, 64>(f, c, grid, st) : launch_form<KV, 128>(f, c, grid, st);
