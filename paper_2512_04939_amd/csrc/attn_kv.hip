@@ -345,15 +345,14 @@ __device__ __forceinline__ int page_at(const Call &a, int seq, uint32_t key, int
 // channels have not got.
 template <int D>
 struct Offsets {
-  uint32_t row, piece;     // bytes
+  uint32_t at;             // the row's bytes (a multiple of 16), and the number of the piece in the lowest four bits
   int step, turn;
   __device__ __forceinline__ void init(int lane, int64_t stride, bool of_v) {
     using T = Tile<D>;
     const int r = lane / T::kPieces, p = lane % T::kPieces;
-    row = (uint32_t)(r * (int)stride);
-    piece = (uint32_t)(p ^ (of_v ? T::v_xor(r) : T::k_xor(r))) * 16u;
+    at = (uint32_t)(r * (int)stride) | (uint32_t)(p ^ (of_v ? T::v_xor(r) : T::k_xor(r)));
     step = T::kRowsPer * (int)stride;
-    turn = of_v ? 0 : 64;
+    turn = of_v ? 0 : 4;
   }
 };
 
@@ -361,10 +360,11 @@ struct Offsets {
 template <int D>
 __device__ __forceinline__ void fetch_group(const char *p, int bytes, const Offsets<D> &off, uint32_t lds) {
   const u32x4 r = uniform_rsrc(p, bytes);
-  uint32_t piece = off.piece;
-  asm volatile("" : "+v"(piece));
+  uint32_t at = off.at;
+  asm volatile("" : "+v"(at));
+  const uint32_t row = at & ~15u, piece = at & 15u;
 #pragma unroll
-  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(r, off.row + (uint32_t)(j * off.step) + (piece ^ (uint32_t)(j * off.turn)), lds + j * 1024);
+  for (int j = 0; j < Tile<D>::kFetches; ++j) fetch_lds(r, row + (uint32_t)(j * off.step) + (piece ^ (uint32_t)(j * off.turn)) * 16u, lds + j * 1024);
 }
 
 // A scalar buffer resource (in vector registers it becomes a loop over the lanes)
@@ -894,7 +894,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     uint32_t pb[2][8];
     u32x4 fk[KF], fv[2][DT];     // 64 channels
     constexpr int kF4 = QB == 1 ? 4 : 1;
-    u32x4 f0[kF4], f1[kF4];      // 128 channels
+    u32x4 f0[kF4], f1[kF4], g0[kF4], g1[kF4];      // 128 channels: K's and V's fragments
     const uint32_t lds0 = lds_addr(lds);
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     const int kr = lane & 31, vr = 4 * h + (lane >> 2 & 3);
@@ -956,7 +956,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
         }
       } else if constexpr (decltype(output)::value) {
         const int u = (m - KF) / DT, dt = (m - KF) % DT;
-        const u32x4 f = QB == 2 ? fv[u][dt] : u == 0 ? f0[dt % kF4] : f1[dt % kF4];
+        const u32x4 f = QB == 2 ? fv[u][dt] : u == 0 ? g0[dt % kF4] : g1[dt % kF4];
         const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pb[bo][4 * u], pb[bo][4 * u + 1], pb[bo][4 * u + 2], pb[bo][4 * u + 3]});
         f32x16 &o = rows.o[QB == 2 ? bo : 0][dt];
         o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), w, o, 0, 0, 0);
@@ -1050,13 +1050,17 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     auto phase_c = [&](auto head, auto tail, auto pub, int b, int t) __attribute__((always_inline)) {
       constexpr bool kHead = decltype(head)::value, kTail = decltype(tail)::value;
       phase(std::bool_constant<!kTail>{}, std::bool_constant<!kHead>{}, b, b ^ 1, b ^ 1, [&](int m) __attribute__((always_inline)) {
-        if (m == 3 && !kHead) read_v4(t - 1, 0, f0);
-        if (m == 7 && !kHead) read_v4(t - 1, 1, f1);
-        if (m == 11) {
+        if (m == 7) {
           if constexpr (decltype(pub)::value) publish(t >> 1);
-          if (!kTail) read_k4(t + 2, 0, f0);
+          if (!kTail) {
+            read_k4(t + 2, 0, f0);
+            read_k4(t + 2, 1, f1);
+          }
         }
-        if (m == 15 && !kTail) read_k4(t + 2, 1, f1);
+        if (m == 15) {
+          read_v4(t, 0, g0);
+          read_v4(t, 1, g1);
+        }
       });
       settle(b);
     };
@@ -1111,8 +1115,6 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
             phase_c(Yes{}, No{}, Yes{}, 0, 2 * i);
           }
           phase_c(No{}, Yes{}, No{}, 1, 2 * i + 1);
-          read_v4(2 * i + 1, 0, f0);
-          read_v4(2 * i + 1, 1, f1);
 #pragma unroll
           for (int m = KF; m < 2 * KF; ++m) product(No{}, Yes{}, m, 1, 1);
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
