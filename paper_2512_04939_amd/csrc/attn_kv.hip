@@ -157,7 +157,7 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
     units = work * inv + 0.5f * (float)a.n_seq * (float)a.kv_heads;
   }
   // (a piece's sums are written and read: 8 stages of many rows' time for the slots' 512 of 64 KB)
-  const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 32 ? 11 : 3)) + (s < most ? 6.f : 0.f);
+  const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 64 ? 11 : 3)) + (s < most ? 6.f : 0.f);
   // the least, the longer pieces of two
   float best = cost * 4096.f - (float)min(s, 4095);
   int arg = s;
@@ -210,7 +210,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   const int first64 = total;
   for (int b = 64; b < a.n_seq; b += 64) total += scalar(wave_sum_int(units_of(a, lane_seq(a, b, lane), s)));
   // XCDs take turns with a few units that stand side by side
-  const int side = a.rows_per_block == 32 ? 1 : a.n_seq > 1 ? 8 : min(max(scalar(me.blocks), 1), kSide);
+  const int side = a.rows_per_block <= 64 ? 1 : a.n_seq > 1 ? 8 : min(max(scalar(me.blocks), 1), kSide);
   const uint32_t y = blockIdx.x / kXcd, turn = y / (uint32_t)side;
   const int u = (int)((turn * kXcd + blockIdx.x % kXcd) * side + (y - turn * side));
   if (u >= total || u >= a.most_units) return false;
@@ -574,22 +574,23 @@ struct Rows {
 };
 
 // ---------------------------------------------------------------------------------------
-// Few rows.  A workgroup has 32 rows of a (sequence, kv head) and a piece of its keys, in tiles of 128: wave w takes the w-th 32
+// Few rows.  A workgroup has 32 or 64 rows of a (sequence, kv head) and a piece of its keys, in tiles of 128: wave w takes the w-th 32
 // keys of each, through LDS of its own, so nobody waits for anybody before the end.  bf16: two
 // tiles in LDS, the next one on its way while one is computed with; E4M3: the next tile's codes on their way in registers, turned
 // into bf16 in LDS.
-template <Kv KV, int D>
+template <Kv KV, int D, int QB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_few(Call a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using T = Tile<D>;
+  constexpr int kRows = 32 * QB;
   constexpr int kTile = 32 * T::kRow;          // bytes of a tile's K or V
   constexpr int kStages = KV == Kv::E4M3 ? 1 : 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
   if (!find_work(a, lane, w, s)) return;
-  const int n_rows = s.nq * a.group, row0 = w.block * 32;
-  const int last = scalar(limit_of(a, s, min(row0 + 31, n_rows - 1) / a.group));     // keys that some row sees
+  const int n_rows = s.nq * a.group, row0 = w.block * kRows;
+  const int last = scalar(limit_of(a, s, min(row0 + kRows - 1, n_rows - 1) / a.group));     // keys that some row sees
   const int first = scalar(limit_of(a, s, row0 / a.group));                          // keys that every row sees
   const int begin = w.t0 * 128 + wave * 32, end = (int)min((uint32_t)w.t1 * 128u, (uint32_t)last);
   const int n = __builtin_amdgcn_readfirstlane(end > begin ? (end - begin + 127) / 128 : 0);     // the wave's tiles
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
     }
   };
-  Rows<D, 1> rows;
+  Rows<D, QB> rows;
   rows.load(a, s, w.head, row0, lane);
   if (n > 0) {
     look_up(0);
@@ -661,24 +662,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
   }
 
-  // the four waves' sums: [wave][32 rows][D] and their references and sums of weights
+  // the four waves' sums: [wave][row][D] and their references and sums of weights
   __syncthreads();
   float *po = (float *)lds;
-  __shared__ float2 ml[4][32];
-  {
-    const float l = rows.l[0] + __shfl_xor(rows.l[0], 32, 64);
-    if (lane < 32) ml[wave][lane] = float2{rows.ref[0], l};
-    float *p = po + (wave * 32 + (lane & 31)) * D;
+  __shared__ float2 ml[4][kRows];
+#pragma unroll
+  for (int b = 0; b < QB; ++b) {
+    const int r = b * 32 + (lane & 31);
+    const float l = rows.l[b] + __shfl_xor(rows.l[b], 32, 64);
+    if (lane < 32) ml[wave][r] = float2{rows.ref[b], l};
+    float *p = po + (wave * kRows + r) * D;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int ch = dt * 32 + i * 8 + (lane >> 5) * 4;
-        *(f32x4 *)(p + (ch ^ ((lane & 15) * 4))) = f32x4{rows.o[0][dt][4 * i], rows.o[0][dt][4 * i + 1], rows.o[0][dt][4 * i + 2], rows.o[0][dt][4 * i + 3]};
+        *(f32x4 *)(p + (ch ^ ((lane & 15) * 4))) = f32x4{rows.o[b][dt][4 * i], rows.o[b][dt][4 * i + 1], rows.o[b][dt][4 * i + 2], rows.o[b][dt][4 * i + 3]};
       }
   }
   __syncthreads();
-  for (int i = tid; i < 32 * (D / 4); i += 256) {
+  for (int i = tid; i < kRows * (D / 4); i += 256) {
     const int r = i / (D / 4), ch = i % (D / 4) * 4;
     if (row0 + r >= n_rows) break;
     float top = ml[0][r].x;
@@ -689,13 +692,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const float f = __builtin_amdgcn_exp2f(ml[x][r].x - top);
-      const f32x4 y = *(const f32x4 *)(po + (x * 32 + r) * D + (ch ^ ((r & 15) * 4)));
+      const f32x4 y = *(const f32x4 *)(po + (x * kRows + r) * D + (ch ^ ((r & 15) * 4)));
       l += ml[x][r].y * f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
     }
     if (w.pieces > 1) {
-      const int64_t at = (int64_t)w.slot * 32 + r;
+      const int64_t at = (int64_t)w.slot * kRows + r;
       *(f32x4 *)(a.part + at * D + ch) = sum;
       if (ch == 0) a.part_ml[at] = float2{top, l};
     } else {
@@ -1277,8 +1280,8 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m
   Form f;
   const int group = heads / kv_heads;
   const double rows = (double)n_q * group / n_seq;
-  f.few = rows <= 64.0;
-  f.rows = f.few ? 32 : 256;
+  f.few = rows <= (head_dim == 64 ? 64.0 : 32.0);
+  f.rows = f.few ? (rows <= 32.0 ? 32 : 64) : 256;
   f.tile = f.few ? 128 : 64;
   f.resident = kCus * (head_dim == 64 || (f.few && e4m3) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
@@ -1315,9 +1318,13 @@ static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size
 template <Kv KV, int D>
 static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t st) {
   constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
-  static std::atomic<uint64_t> d0{0}, d1{0};
-  if (f.few) return go(k_kv_attn_few<KV, D>, d0, std::integral_constant<size_t, KV == Kv::E4M3 ? 2 * tile : 4 * tile>{}, c, grid, 256, st);
-  return go(k_kv_attn_many<KV, D>, d1, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid,
+  static std::atomic<uint64_t> d0{0}, d1{0}, d2{0};
+  // (the ring of four waves' tiles, and room for their sums at the end)
+  constexpr size_t ring = KV == Kv::E4M3 ? 2 * tile : 4 * tile, sums = 4 * 32 * D * sizeof(float);
+  if (f.few && f.rows == 32) return go(k_kv_attn_few<KV, D, 1>, d0, std::integral_constant<size_t, std::max(ring, sums)>{}, c, grid, 256, st);
+  if constexpr (D == 64)
+    if (f.few) return go(k_kv_attn_few<KV, D, 2>, d1, std::integral_constant<size_t, std::max(ring, 2 * sums)>{}, c, grid, 256, st);
+  return go(k_kv_attn_many<KV, D>, d2, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid,
             64 * Many<D>::kWaves, st);
 }
 
