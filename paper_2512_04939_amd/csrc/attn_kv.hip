@@ -97,11 +97,33 @@ __device__ __forceinline__ int limit_of(const Call &a, const SeqInfo &q, int i) 
   return (int)min((uint32_t)q.nk, ((uint32_t)p / (uint32_t)a.frame + 1u) * (uint32_t)a.frame);   // (below 2^32)
 }
 
-__device__ __forceinline__ int wave_sum_int(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Over the lanes by moves inside rows of 16 lanes, then from row to row: shuffles are LDS round trips, and a call's first 2 us were
+// six of them for each reduction (cross attention of 4 x 16 rows over 1000 to 1500 keys: 13.1 us with shuffles, 11.1 so)
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t old, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, kCtrl, 0xF, 0xF, false);
+}
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) {
+  v = min(v, dpp_u32<0x128>(v, v));   // row_ror:8
+  v = min(v, dpp_u32<0x124>(v, v));   // row_ror:4
+  v = min(v, dpp_u32<0x4E>(v, v));    // quad_perm [2,3,0,1]
+  v = min(v, dpp_u32<0xB1>(v, v));    // quad_perm [1,0,3,2]
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = min((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return (uint32_t)scalar((int)min((uint32_t)b[0], (uint32_t)b[1]));
+}
+// (sums up to the lane: row_shr 1, 2, 4, 8 where the lane there is one of the row; the rows' last lanes to the rows behind)
+__device__ __forceinline__ int wave_prefix(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
   return v;
 }
+__device__ __forceinline__ int wave_sum_int(int v) { return __builtin_amdgcn_readlane(wave_prefix(v), 63); }
 
 // The sequence of the call that this lane looks at (step b of 64)
 __device__ __forceinline__ SeqInfo lane_seq(const Call &a, int b, int lane) {
@@ -130,9 +152,8 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
     most = max(most, q.blocks ? q.tiles : 0);
   }
   if (a.n_seq > 1) {
-    work = wave_sum(work);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+    work = wave_sum_ordered(work);
+    most = (int)~wave_min_u32(~(uint32_t)most);
   } else {
     work = __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, work)));
   }
@@ -158,19 +179,9 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
   }
   // (a piece's sums are written and read: 8 stages of many rows' time for the slots' 512 of 64 KB)
   const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 64 ? 11 : 3)) + (s < most ? 6.f : 0.f);
-  // the least, the longer pieces of two
-  float best = cost * 4096.f - (float)min(s, 4095);
-  int arg = s;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float v = __shfl_xor(best, o, 64);
-    const int w = __shfl_xor(arg, o, 64);
-    if (v < best || (v == best && w > arg)) {
-      best = v;
-      arg = w;
-    }
-  }
-  return scalar(arg);
+  // the least, of equal ones the later (longer pieces)
+  const uint32_t key = (uint32_t)fminf(cost * 8.f, 67108863.f) << 6 | (uint32_t)(63 - lane);
+  return __builtin_amdgcn_readlane(s, 63 - (int)(wave_min_u32(key) & 63u));
 }
 
 __device__ __forceinline__ int pieces_of(int tiles, int s) { return s == kUncut ? 1 : max((int)((uint32_t)(tiles + s - 1) / (uint32_t)s), 1); }
@@ -183,14 +194,9 @@ struct Work {
 };
 
 // Sum over the lanes before this one; total: over all
-__device__ __forceinline__ int wave_scan(int v, int lane, int &total) {
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  total = __shfl(x, 63, 64);
+__device__ __forceinline__ int wave_scan(int v, int &total) {
+  const int x = wave_prefix(v);
+  total = __builtin_amdgcn_readlane(x, 63);
   return x - v;
 }
 
@@ -204,7 +210,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   const int mine = a.n_seq > 1 ? units_of(a, me, s) : whole + (me.blocks * a.kv_heads - whole) * pieces_of(me.tiles, s);
   int total = scalar(mine), start = 0, seen = 0;     // of the first 64 sequences; units before the lane's
   if (a.n_seq > 1) {
-    start = wave_scan(mine, lane, seen);
+    start = wave_scan(mine, seen);
     total = scalar(seen);
   }
   const int first64 = total;
@@ -236,7 +242,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
       const SeqInfo q = lane_seq(a, b, lane);
       const int v = units_of(a, q, s);
       int sum;
-      const int at = before + wave_scan(v, lane, sum);
+      const int at = before + wave_scan(v, sum);
       const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= at && u < at + v);
       if (hit) {
         j = scalar(__ffsll((unsigned long long)hit) - 1);
@@ -1191,7 +1197,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
       break;
     }
     int sum;
-    const int start = before + wave_scan(units_of(a, q, piece_len), lane, sum);
+    const int start = before + wave_scan(units_of(a, q, piece_len), sum);
     before += sum;
     if (hit) {
       const int j = scalar(__ffsll((unsigned long long)hit) - 1);
