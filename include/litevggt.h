@@ -331,7 +331,8 @@ int litevggt_layers_run(const litevggt_params *p, int n_layers, const void *imag
  * The calls take lengths, offsets and page numbers from device memory: nothing about a
  * batch has to be known on the host, and a captured call can be replayed with other lengths.  Every
  * number that is read there is checked against the sizes given here; what is out of range is
- * left out, never followed.
+ * left out, never followed.  A call has fewer than 2^24 tokens (queries, states), and of these times their heads
+ * fewer than 2^27.  Scratch for more tokens, all else equal, serves fewer.
  */
 enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1 };
 
@@ -339,7 +340,7 @@ typedef struct {
   int32_t n_seq;           /* sequences of a call, 1 .. 65535                          */
   int32_t heads;           /* query heads, a multiple of kv_heads: query head h uses kv head
                               h / (heads / kv_heads)                                   */
-  int32_t kv_heads;        /* heads of K and V, 1 .. 1024                              */
+  int32_t kv_heads;        /* heads of K and V, 1 .. 1024; n_seq * kv_heads at most 2^22 */
   int32_t head_dim;        /* 64 or 128                                                */
   int32_t cache_dtype;     /* LV_CACHE_BF16 or LV_CACHE_E4M3                           */
   int32_t page_tokens;     /* positions of a page: 16, 32, .. 1024                     */
@@ -355,8 +356,9 @@ typedef struct {
 
 /* Caller-owned device buffers of a cache.  Position t of sequence s is row t % page_tokens of page
  * page_table[s][t / page_tokens]; a number outside 0 .. n_pages-1 (-1): the page is not held.
- * E4M3: value = code * 2^(scale - 127), one scale per row (token and kv head, K and V apart).  Pages
- * may serve several sequences for reading; where two calls' or sequences' writes meet in one row, either may win. */
+ * E4M3: value = code * 2^(scale - 127), scale 1 .. 254, one per row (token and kv head, K and V apart).  Pages
+ * may serve several sequences for reading; a row where the writes of two sequences of a call, or of two calls at
+ * once, meet may hold parts of both. */
 typedef struct {
   void *k, *v;                  /* [n_pages][kv_heads][page_tokens][head_dim] bf16 or E4M3 codes */
   uint8_t *k_scale, *v_scale;   /* [n_pages][kv_heads][page_tokens]; LV_CACHE_E4M3 only          */
@@ -393,7 +395,8 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
  *   q   [device] [n_tokens, heads, head_dim] bf16, o likewise, out; row strides in elements as above
  *   ws  litevggt_cached_attn_ws_bytes(p, n_tokens) bytes
  * The weights are rounded to bf16 for the second product; scores, the softmax's sums and
- * the output's stay fp32.  Results do not depend on the order in which workgroups run.
+ * the output's stay fp32 (weights may reach 2^40 before they are divided by their sum: V's finite values are
+ * to lie below 2^80).  Results do not depend on the order in which workgroups run.
  */
 size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens);
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,

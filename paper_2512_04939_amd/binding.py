@@ -363,10 +363,25 @@ def _rows(t, heads: int, head_dim: int, what: str):
     return shape[0], t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], width)
 
 
+def _ints(t, n: int, what: str):
+    """Pointer of n numbers (or more) that the device reads as int32."""
+    if t is None:
+        return None
+    if t.dtype is not _int32() or t.numel() < n or not t.is_contiguous():
+        raise LiteVGGTError(f"{what}: {n} int32 numbers wanted, got {tuple(t.shape)} {t.dtype} with strides {t.stride()}")
+    return t.data_ptr()
+
+
 @functools.lru_cache(maxsize=None)
 def _bf16():
     import torch
     return torch.bfloat16
+
+
+@functools.lru_cache(maxsize=None)
+def _int32():
+    import torch
+    return torch.int32
 
 
 def litevggt_cache_write(p: CacheParams, cache: CacheBuffers, k, v, new_off, pos) -> None:
@@ -374,7 +389,8 @@ def litevggt_cache_write(p: CacheParams, cache: CacheBuffers, k, v, new_off, pos
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n, m, "k and v")
     c = cache.struct()
-    _check(lib().litevggt_cache_write(C.byref(p), C.byref(c), n, kp, ks, vp, vs, _ptr(new_off), _ptr(pos), _stream()),
+    _check(lib().litevggt_cache_write(C.byref(p), C.byref(c), n, kp, ks, vp, vs,
+                                      _ints(new_off, p.n_seq + 1, "new_off"), _ints(pos, p.n_seq, "pos"), _stream()),
            "litevggt_cache_write")
 
 
@@ -383,7 +399,8 @@ def litevggt_cache_read(p: CacheParams, cache: CacheBuffers, first, off, k, v) -
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n, m, "k and v")
     c = cache.struct()
-    _check(lib().litevggt_cache_read(C.byref(p), C.byref(c), _ptr(first), _ptr(off), n, kp, ks, vp, vs, _stream()),
+    _check(lib().litevggt_cache_read(C.byref(p), C.byref(c), _ints(first, p.n_seq, "first"),
+                                     _ints(off, p.n_seq + 1, "off"), n, kp, ks, vp, vs, _stream()),
            "litevggt_cache_read")
 
 
@@ -397,8 +414,8 @@ def litevggt_cached_attn(p: CacheParams, cache: CacheBuffers, q, new_off, kv_len
     _same(n, m, "q and o")
     c = cache.struct()
     wp, wn = _ws_args(ws)
-    _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, _ptr(new_off), _ptr(kv_len), op, os_, wp, wn,
-                                      _stream()), "litevggt_cached_attn")
+    _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, _ints(new_off, p.n_seq + 1, "new_off"),
+                                      _ints(kv_len, p.n_seq, "kv_len"), op, os_, wp, wn, _stream()), "litevggt_cached_attn")
 
 
 def litevggt_cross_attn_ws_bytes(p: CrossParams, n_q: int, n_kv: int) -> int:
@@ -413,8 +430,8 @@ def litevggt_cross_attn(p: CrossParams, q, q_off, k, v, kv_begin, kv_end, o, ws)
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n_kv, m, "k and v")
     wp, wn = _ws_args(ws)
-    _check(lib().litevggt_cross_attn(C.byref(p), n, qp, qs, _ptr(q_off), n_kv, kp, ks, vp, vs, _ptr(kv_begin),
-                                     _ptr(kv_end), op, os_, wp, wn, _stream()), "litevggt_cross_attn")
+    _check(lib().litevggt_cross_attn(C.byref(p), n, qp, qs, _ints(q_off, p.n_seq + 1, "q_off"), n_kv, kp, ks, vp, vs,
+                                     _ints(kv_begin, p.n_seq, "kv_begin"), _ints(kv_end, p.n_seq, "kv_end"), op, os_, wp, wn, _stream()), "litevggt_cross_attn")
 
 
 def _same(a: int, b: int, what: str) -> None:

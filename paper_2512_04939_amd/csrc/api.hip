@@ -120,6 +120,7 @@ constexpr int64_t kMostPositions = 0x7fff0000;      // of a sequence: what lies 
 int check_heads(int n_seq, int heads, int kv_heads, int head_dim, float softmax_scale) {
   if (n_seq < 1 || n_seq > 65535) return LV_ERR_SHAPE;
   if (kv_heads < 1 || heads < kv_heads || heads > 1024 || heads % kv_heads != 0) return LV_ERR_SHAPE;
+  if ((int64_t)n_seq * kv_heads > (int64_t)1 << 22) return LV_ERR_SHAPE;
   if (head_dim != 64 && head_dim != 128) return LV_ERR_SHAPE;
   if (!isfinite(softmax_scale)) return LV_ERR_PARAM;
   return LV_OK;
@@ -155,7 +156,8 @@ int check_cache_buffers(const litevggt_cache *c, CacheView *cv) {
 bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
   return ((uintptr_t)p & 15u) == 0 && stride % 8 == 0 && stride >= width && stride <= kMostStride && n >= 0;
 }
-bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n * heads < ((int64_t)1 << 31) && n < ((int64_t)1 << 31); }
+// tokens of a call, and of these times heads (grids of 256 threads stay below 2^32 of them in x)
+bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n < ((int64_t)1 << 24) && n * heads < ((int64_t)1 << 27); }
 
 }  // namespace
 

@@ -28,7 +28,7 @@ constexpr int kNoKey = 0x7fff0000;       // beyond every position that rows see
 constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
 constexpr float kRowRaise = 1.0995116e12f;   // 2^40
 constexpr int kCus = 256;
-constexpr int kWholeTiles = 8;           // no call is cut whose sequences have no more tiles (what joining costs)
+constexpr int kWholeTiles = 8;           // no call is cut whose sequences have fewer tiles (what joining costs)
 constexpr int kSide = 16;                // units side by side that one XCD takes, at most
 constexpr int kRounds = 3;               // a call's pieces fill these slots at most so often
 
@@ -187,6 +187,10 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
 __device__ __forceinline__ int pieces_of(int tiles, int s) { return s == kUncut ? 1 : max((int)((uint32_t)(tiles + s - 1) / (uint32_t)s), 1); }
 __device__ __forceinline__ int units_of(const Call &a, const SeqInfo &q, int s) { return q.blocks * a.kv_heads * pieces_of(q.tiles, s); }
 
+// The slots of the workspace that a sequence takes: those of its pieces, if it is cut.  They are at most twice the pieces aimed at,
+// however many sequences there are: who is cut has more tiles than a piece, so at most twice as many pieces as the quotient.
+__device__ __forceinline__ int slots_taken(const Call &a, const SeqInfo &q, int s) { return pieces_of(q.tiles, s) > 1 ? units_of(a, q, s) : 0; }
+
 struct Work {
   int seq, head, block, pieces;
   int t0, t1;      // its tiles
@@ -208,10 +212,10 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   if (a.target && blockIdx.x == 0 && threadIdx.x == 0) *a.chosen = s;
   const int whole = scalar(whole_heads(a, me.blocks)) * scalar(me.blocks);     // units that are not cut, ahead of the others
   const int mine = a.n_seq > 1 ? units_of(a, me, s) : whole + (me.blocks * a.kv_heads - whole) * pieces_of(me.tiles, s);
-  int total = scalar(mine), start = 0, seen = 0;     // of the first 64 sequences; units before the lane's
+  int total = scalar(mine), start = 0, cut = 0, taken = 0;     // of the first 64 sequences; units before the lane's, slots before them
   if (a.n_seq > 1) {
-    start = wave_scan(mine, seen);
-    total = scalar(seen);
+    start = wave_scan(mine, total);
+    if (a.target) cut = wave_scan(slots_taken(a, me, s), taken);
   }
   const int first64 = total;
   for (int b = 64; b < a.n_seq; b += 64) total += scalar(wave_sum_int(units_of(a, lane_seq(a, b, lane), s)));
@@ -222,11 +226,13 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   if (u >= total || u >= a.most_units) return false;
   int local = u, j = 0;
   w.seq = 0;
+  w.slot = u - whole;
   if (a.n_seq > 1 && u < first64) {
     const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= start && u < start + mine);
     j = scalar(__ffsll((unsigned long long)hit) - 1);
     w.seq = j;
     local = u - __builtin_amdgcn_readlane(start, j);
+    w.slot = local + __builtin_amdgcn_readlane(cut, j);
   }
   if (u < first64) {
     info.q0 = __builtin_amdgcn_readlane(me.q0, j);
@@ -241,17 +247,19 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
     for (int b = 64;; b += 64) {
       const SeqInfo q = lane_seq(a, b, lane);
       const int v = units_of(a, q, s);
-      int sum;
-      const int at = before + wave_scan(v, sum);
+      int sum, slots;
+      const int at = before + wave_scan(v, sum), slot = taken + wave_scan(slots_taken(a, q, s), slots);
       const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= at && u < at + v);
       if (hit) {
         j = scalar(__ffsll((unsigned long long)hit) - 1);
         w.seq = b + j;
         local = u - __builtin_amdgcn_readlane(at, j);
+        w.slot = local + __builtin_amdgcn_readlane(slot, j);
         info = seq_info(a, w.seq);
         break;
       }
-      before += scalar(sum);
+      before += sum;
+      taken += slots;
       if (b + 64 >= a.n_seq) return false;      // (lengths that changed meanwhile)
     }
   }
@@ -265,7 +273,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   info.tiles = scalar(info.tiles);
   w.seq = scalar(w.seq);
   w.pieces = u < whole ? 1 : scalar(pieces_of(info.tiles, s));
-  w.slot = u - whole;
+  if (w.pieces > 1 && w.slot >= a.slots) return false;      // (offsets that do not ascend)
   const int skip = u < whole ? 0 : whole / info.blocks;     // heads
   local -= skip * info.blocks;
   const int len = w.pieces == 1 ? info.tiles : (int)((uint32_t)(info.tiles + w.pieces - 1) / (uint32_t)w.pieces);
@@ -1183,8 +1191,7 @@ template <int D, int SL>
 __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   constexpr int kCh = D / 4, kRowsWg = 256 / (kCh * SL);
   const int tid = threadIdx.x, lane = tid & 63;
-  const int per_token = (a.heads + kRowsWg - 1) / kRowsWg;
-  const int tok = blockIdx.x / per_token;
+  const int tok = blockIdx.x;
   const int piece_len = *a.chosen;
   if (piece_len == kUncut) return;
   // the token's sequence and the number of the first piece of it
@@ -1197,7 +1204,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
       break;
     }
     int sum;
-    const int start = before + wave_scan(units_of(a, q, piece_len), sum);
+    const int start = before + wave_scan(slots_taken(a, q, piece_len), sum);
     before += sum;
     if (hit) {
       const int j = scalar(__ffsll((unsigned long long)hit) - 1);
@@ -1210,7 +1217,7 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
   if (pieces == 1) return;          // written already
   const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
-  const int hq = blockIdx.x % per_token * kRowsWg + in_wg;
+  const int hq = blockIdx.y * kRowsWg + in_wg;
   const bool there = hq < a.heads;
   const int head = (there ? hq : 0) / a.group, g = (there ? hq : 0) % a.group;
   const int r = (tok - s.q0) * a.group + g;
@@ -1293,22 +1300,27 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (blocks that fill the chip several times over leave nothing to gain)
-  const int64_t target = f.units >= 4 * f.resident && !f.few && n_seq > 1 ? 0 : tiles <= kWholeTiles ? 0 : kRounds * f.resident;
+  const int64_t target = f.units >= 4 * f.resident && !f.few && n_seq > 1 ? 0 : tiles < kWholeTiles ? 0 : kRounds * f.resident;
   f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
   return f;
 }
-// (one sequence: beyond the heads that fill whole rounds)
-int64_t slots_of(const Form &f, int n_seq, int kv_heads) {
-  const int64_t blocks = f.units / kv_heads;
-  return (n_seq > 1 || f.units < f.resident ? f.units : std::min(f.units, f.resident + 2 * blocks)) + f.target;
+// Blocks that are cut take a piece each beside those aimed at, and at most twice as many as were aimed at (slots_taken)
+int64_t slots_of(const Form &f) { return std::min(f.units + f.target, 2 * (int64_t)f.target); }
+size_t sums_bytes(const Form &f, int head_dim) {
+  return f.target == 0 ? 0 : 256 + align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
 }
 
 }  // namespace
 
 size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
-  const Form f = form_of(n_q, n_seq, heads, kv_heads, head_dim, e4m3, most_keys);
-  if (f.target == 0) return 0;
-  return 256 + align_up((size_t)slots_of(f, n_seq, kv_heads) * f.rows * (head_dim + 2) * sizeof(float), 256);
+  // What the call needs grows with n_q inside a form only.  The size is the largest up to n_q, so that scratch for a
+  // longer call serves the shorter ones.
+  const int group = heads / kv_heads;
+  const int64_t cut = (4 * kCus * (head_dim == 64 ? 2 : 1) - 1) / kv_heads - n_seq;     // most blocks of many rows that are cut (form_of)
+  size_t most = 0;
+  for (int64_t n : {(int64_t)n_q, (int64_t)32 * n_seq / group, (int64_t)64 * n_seq / group, (256 * cut + 255) / group})
+    if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, e4m3, most_keys), head_dim));
+  return most;
 }
 
 template <typename K, size_t LDS>
@@ -1369,7 +1381,7 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.block_shift = __builtin_ctz(f.rows);
   c.tile_shift = __builtin_ctz(f.tile);
   c.target = f.target;
-  c.slots = (int)slots_of(f, x.n_seq, x.kv_heads);
+  c.slots = (int)slots_of(f);
   c.resident = f.resident;
   c.most_units = (int)(f.units + f.target);
   c.chosen = (int *)ws;
@@ -1388,7 +1400,7 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   if (rc) return rc;
   if (f.target) {
     auto join = [&](auto kernel, int rows) {
-      kernel<<<dim3((uint32_t)((int64_t)x.n_q * ((x.heads + rows - 1) / rows))), 256, 0, st>>>(c);
+      kernel<<<dim3((uint32_t)x.n_q, (uint32_t)((x.heads + rows - 1) / rows)), 256, 0, st>>>(c);
     };
     if (x.head_dim == 64) f.few ? join(k_kv_attn_join<64, 16>, 1) : join(k_kv_attn_join<64, 1>, 16);
     else f.few ? join(k_kv_attn_join<128, 8>, 1) : join(k_kv_attn_join<128, 1>, 8);

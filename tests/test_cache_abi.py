@@ -134,3 +134,41 @@ def test_binding_refuses_what_rows_cannot_be():
     q = torch.zeros(5, 4, 64, dtype=torch.bfloat16)
     with pytest.raises(B.LiteVGGTError, match="rows"):
         B.litevggt_cached_attn(p, c, q, i, i, q[:3], None)
+
+
+def test_largest_calls():
+    assert write(n=1 << 24) == read(n=1 << 24) == cached(n=1 << 24) == cross(n=1 << 24) == cross(m=1 << 24) == SHAPE
+    wide = params(n_seq=2, heads=16, kv_heads=16)
+    assert write(wide, n=1 << 23, ks=1024, vs=1024) == cached(wide, n=1 << 23, qs=1024, os=1024) == SHAPE
+    assert B.litevggt_cached_attn_ws_bytes(wide, 1 << 23) == 0
+    many = params(n_seq=65535, heads=128, kv_heads=128)
+    assert write(many, ks=8192, vs=8192) == cached(many, qs=8192, os=8192) == SHAPE
+
+
+@pytest.mark.parametrize("n_seq,heads,kv,dim,e4m3", [(1, 16, 16, 64, False), (1, 12, 1, 128, True), (7, 16, 4, 64, True), (64, 16, 16, 64, False),
+                                                     (300, 8, 2, 128, False), (4096, 16, 16, 128, True), (65535, 4, 4, 64, False)])
+def test_scratch_for_more_tokens_serves_fewer(n_seq, heads, kv, dim, e4m3):
+    p = params(n_seq=n_seq, heads=heads, kv_heads=kv, head_dim=dim, cache_dtype=int(e4m3), max_pages=4096)
+    x = B.make_cross_params(n_seq, heads, dim, kv_heads=kv)
+    group = heads // kv
+    counts = sorted({max(1, c + e) for c in [32 * n_seq // group, 64 * n_seq // group] + [int(1.3 ** j) for j in range(56)] for e in (-1, 0, 1)})
+    for sizes in ([B.litevggt_cached_attn_ws_bytes(p, n) for n in counts], [B.litevggt_cross_attn_ws_bytes(x, n, 100000) for n in counts]):
+        assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+        assert 0 < sizes[0] and sizes[-1] < 512 << 20
+
+
+def test_binding_refuses_numbers_that_are_not_int32():
+    p = params()
+    c = B.CacheBuffers(*(torch.zeros(1) for _ in range(5)))
+    k = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    q = torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+    off, one = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    x = B.make_cross_params(2, 4, 64, kv_heads=2)
+    for bad in (off.long(), off[:1], torch.zeros(6, dtype=torch.int32)[::2], off.float()):
+        for call in (lambda a, b: B.litevggt_cache_write(p, c, k, k, a, b), lambda a, b: B.litevggt_cache_read(p, c, b, a, k, k),
+                     lambda a, b: B.litevggt_cached_attn(p, c, q, a, b, q, None),
+                     lambda a, b: B.litevggt_cross_attn(x, q, a, k, k, b, b, q, None)):
+            with pytest.raises(B.LiteVGGTError, match="int32"):
+                call(bad, one)
+            with pytest.raises(B.LiteVGGTError, match="int32"):
+                call(off, bad)
