@@ -1225,17 +1225,34 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int64_t slot0 = before + (int64_t)max(head - whole, 0) * pieces * s.blocks + block;
   if (slot0 + (int64_t)(pieces - 1) * s.blocks >= a.slots) return;
   auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
-  float top = kUnset;
-  for (int x = sl; x < pieces; x += SL) top = fmaxf(top, a.part_ml[at(x)].x);
+  // four pieces at a time: their loads are on the way together
+  float top = kUnset, l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int x = sl; x < pieces; x += SL) {
-    const float2 ml = a.part_ml[at(x)];
-    const float f = __builtin_amdgcn_exp2f(ml.x - top);
-    const f32x4 y = *(const f32x4 *)(a.part + at(x) * D + ch);
-    l += ml.y * f;
+  for (int x0 = sl; x0 < pieces; x0 += 4 * SL) {
+    float2 ml[4];
+    f32x4 y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+    for (int i = 0; i < 4; ++i) {
+      const int64_t from = at(min(x0 + i * SL, pieces - 1));
+      ml[i] = a.part_ml[from];
+      y[i] = *(const f32x4 *)(a.part + from * D + ch);
+    }
+    float to = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to = fmaxf(to, ml[i].x);
+    const float g = __builtin_amdgcn_exp2f(top - to);
+    top = to;
+    l *= g;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] *= g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (x0 + i * SL >= pieces) break;
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - to);
+      l += ml[i].y * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += y[i][e] * f;
+    }
   }
   if constexpr (SL > 1) {
     __shared__ float tops[kRowsWg][SL], ls[kRowsWg][SL];
