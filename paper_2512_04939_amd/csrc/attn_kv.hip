@@ -204,6 +204,19 @@ __device__ __forceinline__ int wave_scan(int v, int &total) {
   return x - v;
 }
 
+// A lane's sequence, in all lanes
+__device__ __forceinline__ SeqInfo from_lane(const SeqInfo &q, int j) {
+  SeqInfo r;
+  r.q0 = __builtin_amdgcn_readlane(q.q0, j);
+  r.nq = __builtin_amdgcn_readlane(q.nq, j);
+  r.k0 = __builtin_amdgcn_readlane(q.k0, j);
+  r.nk = __builtin_amdgcn_readlane(q.nk, j);
+  r.p0 = __builtin_amdgcn_readlane(q.p0, j);
+  r.blocks = __builtin_amdgcn_readlane(q.blocks, j);
+  r.tiles = __builtin_amdgcn_readlane(q.tiles, j);
+  return r;
+}
+
 // The workgroup's piece of the call, in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
 // side, and an XCD gets a range of them.
 __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
@@ -235,13 +248,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
     w.slot = local + __builtin_amdgcn_readlane(cut, j);
   }
   if (u < first64) {
-    info.q0 = __builtin_amdgcn_readlane(me.q0, j);
-    info.nq = __builtin_amdgcn_readlane(me.nq, j);
-    info.k0 = __builtin_amdgcn_readlane(me.k0, j);
-    info.nk = __builtin_amdgcn_readlane(me.nk, j);
-    info.p0 = __builtin_amdgcn_readlane(me.p0, j);
-    info.blocks = __builtin_amdgcn_readlane(me.blocks, j);
-    info.tiles = __builtin_amdgcn_readlane(me.tiles, j);
+    info = from_lane(me, j);
   } else {
     int before = first64;
     for (int b = 64;; b += 64) {
@@ -255,7 +262,7 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
         w.seq = b + j;
         local = u - __builtin_amdgcn_readlane(at, j);
         w.slot = local + __builtin_amdgcn_readlane(slot, j);
-        info = seq_info(a, w.seq);
+        info = from_lane(q, j);
         break;
       }
       before += sum;
@@ -263,15 +270,6 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
       if (b + 64 >= a.n_seq) return false;      // (lengths that changed meanwhile)
     }
   }
-  // (scalars from here on, whatever they were worked out with)
-  info.q0 = scalar(info.q0);
-  info.nq = scalar(info.nq);
-  info.k0 = scalar(info.k0);
-  info.nk = scalar(info.nk);
-  info.p0 = scalar(info.p0);
-  info.blocks = scalar(info.blocks);
-  info.tiles = scalar(info.tiles);
-  w.seq = scalar(w.seq);
   w.pieces = u < whole ? 1 : scalar(pieces_of(info.tiles, s));
   if (w.pieces > 1 && w.slot >= a.slots) return false;      // (offsets that do not ascend)
   const int skip = u < whole ? 0 : whole / info.blocks;     // heads
@@ -1193,27 +1191,23 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int tok = blockIdx.x;
   const int piece_len = *a.chosen;
-  if (piece_len == kUncut) return;
-  // the token's sequence and the number of the first piece of it
-  int seq = -1, before = 0;
-  for (int b = 0; b < a.n_seq && seq < 0; b += 64) {
+  // the token's sequence and the number of its first slot
+  SeqInfo s = {0, 0, 0, 0, 0, 0, 0};
+  int before = 0;
+  for (int b = 0; b < a.n_seq; b += 64) {
     const SeqInfo q = lane_seq(a, b, lane);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(tok >= q.q0 && tok < q.q0 + q.nq);
-    if (a.n_seq == 1) {
-      seq = hit ? 0 : -1;
-      break;
-    }
-    int sum;
-    const int start = before + wave_scan(slots_taken(a, q, piece_len), sum);
-    before += sum;
+    int sum = 0, start = 0;
+    if (a.n_seq > 1) start = wave_scan(slots_taken(a, q, piece_len), sum);
     if (hit) {
       const int j = scalar(__ffsll((unsigned long long)hit) - 1);
-      seq = b + j;
-      before = __builtin_amdgcn_readlane(start, j);
+      s = from_lane(q, j);
+      before += __builtin_amdgcn_readlane(start, j);
+      break;
     }
+    before += sum;
   }
-  if (seq < 0) return;
-  const SeqInfo s = seq_info(a, seq);
+  if (s.nq == 0) return;
   const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
   if (pieces == 1) return;          // written already
   const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
