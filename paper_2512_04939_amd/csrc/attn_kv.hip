@@ -6,13 +6,19 @@
 // scaled, when a sum passes 2^40 (a score lies 40 binades above the reference).  Sums and references are per row and fp32.
 //
 // A row is a (query token, head) pair; the heads that share a kv head are rows of one block, so K and V are read once for
-// all of them.  Two kernels: k_kv_attn_few has blocks of 32 rows whose four waves take every fourth tile of 32 keys
-// each (a few rows over many keys: bound by reading K and V); k_kv_attn_many has 32 or 64 rows per wave and 64-key stages of K and V in
-// LDS that all four waves read (bound by MFMA and VALU issue).  In both a long key axis is cut into pieces
-// that different workgroups take; k_kv_attn_join puts their sums together.
+// all of them.  Two kernels.  k_kv_attn_few: blocks of 32 or 64 rows whose four waves take 32 of every 128 keys each; bound by
+// reading K and V (5.0 TB/s of 5.8 that a read alone reaches here, over 32 ragged sequences of an E4M3 cache).  k_kv_attn_many: blocks of
+// 256 rows that walk the keys in stages of 64, which all waves read from LDS; bound, at 64 channels, by the weights' VALU work (a
+// tile of 32 x 32 costs 256 cycles of exp2 and some 170 of multiply-adds, sums and roundings, against 256 of MFMA, which is busy
+// 55 % of the time), at 128 by MFMA (0.96 to 1.1 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
+// both a long key axis is cut into pieces that different workgroups take; k_kv_attn_join puts their sums together.
 //
 // Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
 // weights already lie as the B operand of O^T += V^T P^T.  K and V lie in LDS as rows; V's fragments come out by transposing reads.
+//
+// Rounded to bf16: the weights, for the second product (their sum is that of the unrounded ones), q after its normalisation
+// (as K was before it), and the result.  An E4M3 code times a power of two is a bf16 value: nothing is rounded there.  The scale is
+// multiplied to the fp32 scores and not into q, where it would cost a rounding (7 % of the time at 64 channels).
 #include <algorithm>
 
 #include "internal.h"
@@ -24,13 +30,13 @@ namespace {
 
 constexpr int kGrp = 16;                 // rows of K or V that are fetched together; a page holds a multiple of it
 constexpr int kUncut = 0x7fffffff;       // tiles of a piece where nothing is cut
-constexpr int kNoKey = 0x7fff0000;       // beyond every position that rows see
+constexpr int kNoKey = 0x7fff0000;       // the position of a key that is not there: beyond all that rows see
 constexpr float kUnset = -1e30f;         // reference of a row that has seen no key
 constexpr float kRowRaise = 1.0995116e12f;   // 2^40
 constexpr int kCus = 256;
-constexpr int kWholeTiles = 8;           // no call is cut whose sequences have fewer tiles (what joining costs)
-constexpr int kSide = 16;                // units side by side that one XCD takes, at most
-constexpr int kRounds = 3;               // a call's pieces fill these slots at most so often
+constexpr int kWholeTiles = 8;           // no call is cut whose sequences have fewer tiles: joining is a launch (8 or 16: level)
+constexpr int kSide = 16;                // units side by side that one XCD takes, at most (find_work)
+constexpr int kRounds = 3;               // a call's pieces fill the chip's slots at most so often
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -177,7 +183,7 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
   } else {
     units = work * inv + 0.5f * (float)a.n_seq * (float)a.kv_heads;
   }
-  // (a piece's sums are written and read: 8 stages of many rows' time for the slots' 512 of 64 KB)
+  // (a piece's sums are written and read: 8 tiles of many rows' time for the slots' 512 of 64 KB; 3 to 11 make no difference to speak of)
   const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 64 ? 11 : 3)) + (s < most ? 6.f : 0.f);
   // the least, of equal ones the later (longer pieces)
   const uint32_t key = (uint32_t)fminf(cost * 8.f, 67108863.f) << 6 | (uint32_t)(63 - lane);
@@ -218,7 +224,10 @@ __device__ __forceinline__ SeqInfo from_lane(const SeqInfo &q, int j) {
 }
 
 // The workgroup's piece of the call, in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
-// side, and an XCD gets a range of them.
+// side, and up to 8 (several sequences) or 16 of them go to one XCD, whose L2 then brings K and V once.  (Many rows; each of
+// them by itself in turn: 1374 queries over 138,774 keys 889 us against 851, 32 x 2000 over 4000 1126 against 1068, both 16 heads of 64.
+// All blocks' tiles as one line in equal shares, so that nothing has to be searched: 1365 for the latter, sharers walk at different
+// places.)
 __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   const SeqInfo me = lane_seq(a, 0, lane);
   const int s = piece_tiles(a, lane, me);
@@ -589,7 +598,9 @@ struct Rows {
 // Few rows.  A workgroup has 32 or 64 rows of a (sequence, kv head) and a piece of its keys, in tiles of 128: wave w takes the w-th 32
 // keys of each, through LDS of its own, so nobody waits for anybody before the end.  bf16: two
 // tiles in LDS, the next one on its way while one is computed with; E4M3: the next tile's codes on their way in registers, turned
-// into bf16 in LDS.
+// into bf16 in LDS.  Two workgroups per CU where LDS allows.  5 queries over 137,405 keys, 16 heads of 64, bf16: 100 us, 5.6 TB/s, and 5 to
+// join; 32 tokens over 301 to 30,011 keys, 16 heads on 4 of 128, E4M3: 94 us, and 5 to join.  (Eight waves to a
+// workgroup where there are few of them: 34.1 us against 32.0 for 24 rows over 30,000 keys, 17.2 against 14.4 for 48 over 2000.)
 template <Kv KV, int D, int QB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_few(Call a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -739,6 +750,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //   C(t): scores (t + 1) | K(t + 2) is read | output (t - 1) | V(t) is read;  weights (t)
 //
 // No register may go to scratch in the loops: reading it back waits for the fetches (three times the time).
+//
+// 13,740 queries over 14,316 states, 16 heads of 64: 770 us (1.05 PFLOP/s), and 28 to join; 1374 over 138,774 keys in pages: 825 and 24; six
+// chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages 405 and 18;
+// 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128: 116, and 6 for K's normalisation and 12 to join.
 template <int D>
 struct Many {
   static constexpr int QB = D == 64 ? 2 : 1, kWaves = 8 / QB, kRows = 32 * QB;
@@ -1184,7 +1199,8 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
 
 // ---------------------------------------------------------------------------------------
 // The sums of a row's pieces put together, always in the same order.  A row has D / 4 lanes times SL: each of
-// these takes every SL-th piece (few rows, many pieces), and they meet in LDS.
+// these takes every SL-th piece (few rows, many pieces), and they meet in LDS.  Bound by the way from the lengths to the sums and
+// by reading the latter: 4 pieces of 7 heads of 13,740 rows in 28 us, 3.5 TB/s.
 template <int D, int SL>
 __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   constexpr int kCh = D / 4, kRowsWg = 256 / (kCh * SL);
@@ -1275,7 +1291,8 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
       u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 
-// K's rows normalised per head, for cross attention with qk_norm
+// K's rows normalised per head, for cross attention with qk_norm: once for all blocks that read them.  Bound by HBM: 27,216 states
+// of 2 heads of 128 in 6.2 us.
 template <int D>
 __global__ __launch_bounds__(256) void k_norm_rows(const uint16_t *k, int64_t stride, int64_t n_rows, int kv_heads, uint16_t *out) {
   constexpr int L = D / 8;
@@ -1299,7 +1316,9 @@ struct Form {
   int target;        // pieces beside these at most
 };
 
-// Which kernel: by the rows that a (sequence, kv head) has on average.
+// Which kernel: by the rows that a (sequence, kv head) has on average.  64 channels, 16 heads of one sequence: 24 rows over 30,000
+// keys 32 us in blocks of 32 rows, 51 in those of 256; 48 rows 34 us in blocks of 64, 49 of 32, 50 of 256 (over 2000 keys 14.4, -, 20.7);
+// 100 rows 89 of 32, 58 of 256.  128 channels: 48 rows of 8 sequences 101 us in blocks of 32, 65 of 256 (64 do not fit the registers).
 Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
   Form f;
   const int group = heads / kv_heads;
@@ -1310,7 +1329,8 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m
   f.resident = kCus * (head_dim == 64 || (f.few && e4m3) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
-  // (blocks that fill the chip several times over leave nothing to gain)
+  // (Blocks of several sequences that fill the chip four times over are not cut: 32 x 2000 queries over 4000 keys, 16 heads of 64
+  // 1068 us against 1111 cut, of 128 2181 against 2305, 64 ragged sequences 1287 against 1346.  One sequence: whole_heads.)
   const int64_t target = f.units >= 4 * f.resident && !f.few && n_seq > 1 ? 0 : tiles < kWholeTiles ? 0 : kRounds * f.resident;
   f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
   return f;

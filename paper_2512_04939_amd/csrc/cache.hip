@@ -3,6 +3,8 @@
 //
 // A page holds page_tokens consecutive positions of one sequence, [kv head][position][channel], so that what attention
 // reads of one head is one piece of memory.  Both kernels are bound by HBM: a token's row is read once and written once.
+// 43,968 tokens of 16 heads of 64 written as E4M3: 59 us, 4.6 TB/s; 137,400 read back: 166 us, 5.1 TB/s (a copy of 4 GB reaches 4.8 on
+// the same card).  A single token takes 3 us of the GPU and twice that of the host.
 #include "internal.h"
 #include "common.h"
 
