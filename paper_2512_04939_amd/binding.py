@@ -178,15 +178,15 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream() -> int:
-    torch = _torch()
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    c = _torch_c()
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 @functools.lru_cache(maxsize=None)
-def _torch():
+def _torch_c():
     import torch
     torch.cuda.current_stream()      # (initialises the device: the calls after this one only ask for the handle)
-    return torch
+    return torch._C
 
 
 def litevggt_strerror(code: int) -> str:

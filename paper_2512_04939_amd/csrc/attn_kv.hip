@@ -10,7 +10,7 @@
 // reading K and V (5.0 TB/s of 5.8 that a read alone reaches here, over 32 ragged sequences of an E4M3 cache).  k_kv_attn_many: blocks of
 // 256 rows that walk the keys in stages of 64, which all waves read from LDS; bound, at 64 channels, by the weights' VALU work (a
 // tile of 32 x 32 costs 256 cycles of exp2 and some 170 of multiply-adds, sums and roundings, against 256 of MFMA, which is busy
-// 55 % of the time), at 128 by MFMA (0.96 to 1.1 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
+// 55 % of the time), at 128 by MFMA (0.93 to 0.97 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
 // both a long key axis is cut into pieces that different workgroups take; k_kv_attn_join puts their sums together.
 //
 // Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
@@ -751,7 +751,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //
 // No register may go to scratch in the loops: reading it back waits for the fetches (three times the time).
 //
-// 13,740 queries over 14,316 states, 16 heads of 64: 770 us (1.05 PFLOP/s), and 28 to join; 1374 over 138,774 keys in pages: 825 and 24; six
+// 13,740 queries over 14,316 states, 16 heads of 64: 770 to 790 us (1.02 to 1.05 PFLOP/s), and 28 to join; 1374 over 138,774 keys in pages: 830 and 24; six
 // chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages 405 and 18;
 // 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128: 116, and 6 for K's normalisation and 12 to join.
 template <int D>
