@@ -61,7 +61,8 @@ struct Call {
   int target;                            // pieces to aim at; 0: nothing is cut
   int most_units;                        // units that there is room for
   int resident;                          // workgroups that the chip holds at once
-  int *chosen;                           // tiles of a piece, for the kernel that joins them
+  int *chosen;                           // tiles of a piece, units of the call: for the kernels that come after who works them out
+  int *starts, *taken;                   // more than 64 sequences: units, slots before each (k_kv_attn_plan); else null
   float *part;                           // [slot][rows_per_block][D] sums
   float2 *part_ml;                       // [slot][rows_per_block] reference, sum of weights
   int slots;
@@ -75,24 +76,32 @@ struct SeqInfo {
   int blocks, tiles;
 };
 
-__device__ __forceinline__ SeqInfo seq_info(const Call &a, int s) {
+__device__ __forceinline__ SeqInfo seq_of_numbers(const Call &a, int off, int next, int begin, int end) {
   SeqInfo r;
-  r.q0 = min(max(a.q_off[s], 0), a.n_q);
-  r.nq = min(max(a.q_off[s + 1], r.q0), a.n_q) - r.q0;
-  const int end = a.k_end[s];
+  r.q0 = min(max(off, 0), a.n_q);
+  r.nq = min(max(next, r.q0), a.n_q) - r.q0;
   if (a.table) {
     const int64_t most = (int64_t)a.max_pages << a.page_shift;
     r.k0 = 0;
     r.nk = (int)min((int64_t)max(end, 0), most);
     r.p0 = max(end, 0) - r.nq;
   } else {
-    r.k0 = min(max(a.k_begin[s], 0), a.n_kv);
+    r.k0 = min(max(begin, 0), a.n_kv);
     r.nk = min(max(end, r.k0), a.n_kv) - r.k0;
     r.p0 = 0;
   }
   r.blocks = (int)(((uint32_t)(r.nq * a.group) + a.rows_per_block - 1) >> a.block_shift);
   r.tiles = (int)(((uint32_t)r.nk + a.tile - 1) >> a.tile_shift);
   return r;
+}
+__device__ __forceinline__ SeqInfo seq_info(const Call &a, int s) {
+  return seq_of_numbers(a, a.q_off[s], a.q_off[s + 1], a.table ? 0 : a.k_begin[s], a.k_end[s]);
+}
+// One number for all lanes, in a scalar register: it comes by a scalar load (what a vector load brings drags all that hangs on it into
+// vector registers)
+__device__ __forceinline__ int uniform_at(const int32_t *p, int i) { return ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)p)[i]; }
+__device__ __forceinline__ SeqInfo uniform_seq(const Call &a, int s) {
+  return seq_of_numbers(a, uniform_at(a.q_off, s), uniform_at(a.q_off, s + 1), a.table ? 0 : uniform_at(a.k_begin, s), uniform_at(a.k_end, s));
 }
 
 // Keys that the row of query i of a sequence sees (all up to this one)
@@ -129,12 +138,11 @@ __device__ __forceinline__ int wave_prefix(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
   return v;
 }
-__device__ __forceinline__ int wave_sum_int(int v) { return __builtin_amdgcn_readlane(wave_prefix(v), 63); }
 
-// The sequence of the call that this lane looks at (step b of 64)
-__device__ __forceinline__ SeqInfo lane_seq(const Call &a, int b, int lane) {
+// The sequence of the call that this lane looks at, of the first 64
+__device__ __forceinline__ SeqInfo lane_seq(const Call &a, int lane) {
   SeqInfo q = {0, 0, 0, 0, 0, 0, 0};
-  if (b + lane < a.n_seq) q = seq_info(a, b + lane);
+  if (lane < a.n_seq) q = seq_info(a, lane);
   return q;
 }
 
@@ -145,27 +153,13 @@ __device__ __forceinline__ int whole_heads(const Call &a, int blocks) {
   return min((int)((uint32_t)(blocks * a.kv_heads / a.resident * a.resident) / (uint32_t)blocks), a.kv_heads);
 }
 
-// How the keys are cut: the tiles of a piece.  Every wave works it out from the lengths, the same in all of them; `me`: lane_seq(0).  A
+// How the keys are cut: the tiles of a piece.  Up to 64 sequences every wave works it out from the lengths, the same in all of them.  A
 // candidate per lane: its pieces' number, and from that how long the call would take in tiles (rounds of the
-// chip's slots, each as long as a piece and what a workgroup costs to start and end).
-__device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInfo &me) {
-  if (a.target == 0) return kUncut;
-  float work = (float)me.blocks * (float)me.tiles;
-  int most = me.blocks ? me.tiles : 0;
-  for (int b = 64; b < a.n_seq; b += 64) {
-    const SeqInfo q = lane_seq(a, b, lane);
-    work += (float)q.blocks * (float)q.tiles;
-    most = max(most, q.blocks ? q.tiles : 0);
-  }
-  if (a.n_seq > 1) {
-    work = wave_sum_ordered(work);
-    most = (int)~wave_min_u32(~(uint32_t)most);
-  } else {
-    work = __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, work)));
-  }
-  const int heads = a.kv_heads - whole_heads(a, me.blocks);     // (of one sequence: every lane that has one)
-  work *= (float)(a.n_seq > 1 ? a.kv_heads : scalar(heads));
-  most = scalar(most);
+// chip's slots, each as long as a piece and what a workgroup costs to start and end).  `me`: lane_seq(0); work: blocks times tiles of all
+// sequences, most: the most tiles.
+__device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInfo &me, float work, int most) {
+  const int heads = a.n_seq > 1 ? a.kv_heads : scalar(a.kv_heads - whole_heads(a, me.blocks));
+  work *= (float)heads;
   if (most <= 1 || work == 0.f) return kUncut;
   static_assert(kRounds == 3, "candidates");
   // lane 63: uncut; the others: 1 .. kRounds rounds, 21 steps of 4 % less pieces in each.  (A hair longer than the quotient: the
@@ -179,7 +173,7 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
       const int tiles = __builtin_amdgcn_readlane(me.tiles, i);
       units += (float)__builtin_amdgcn_readlane(me.blocks, i) * fmaxf(ceilf((float)tiles * inv - 1e-4f), 1.0f);
     }
-    units *= (float)(a.n_seq > 1 ? a.kv_heads : scalar(heads));
+    units *= (float)heads;
   } else {
     units = work * inv + 0.5f * (float)a.n_seq * (float)a.kv_heads;
   }
@@ -188,6 +182,20 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
   // the least, of equal ones the later (longer pieces)
   const uint32_t key = (uint32_t)fminf(cost * 8.f, 67108863.f) << 6 | (uint32_t)(63 - lane);
   return __builtin_amdgcn_readlane(s, 63 - (int)(wave_min_u32(key) & 63u));
+}
+
+__device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInfo &me) {
+  if (a.target == 0) return kUncut;
+  float work = (float)me.blocks * (float)me.tiles;
+  int most = me.blocks ? me.tiles : 0;
+  if (a.n_seq > 1) {
+    work = wave_sum_ordered(work);
+    most = (int)~wave_min_u32(~(uint32_t)most);
+  } else {
+    work = __builtin_bit_cast(float, scalar(__builtin_bit_cast(int, work)));
+    most = scalar(most);
+  }
+  return piece_tiles(a, lane, me, work, most);
 }
 
 __device__ __forceinline__ int pieces_of(int tiles, int s) { return s == kUncut ? 1 : max((int)((uint32_t)(tiles + s - 1) / (uint32_t)s), 1); }
@@ -228,59 +236,50 @@ __device__ __forceinline__ SeqInfo from_lane(const SeqInfo &q, int j) {
 // them by itself in turn: 1374 queries over 138,774 keys 889 us against 851, 32 x 2000 over 4000 1126 against 1068, both 16 heads of 64.
 // All blocks' tiles as one line in equal shares, so that nothing has to be searched: 1365 for the latter, sharers walk at different
 // places.)
-__device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
-  const SeqInfo me = lane_seq(a, 0, lane);
-  const int s = piece_tiles(a, lane, me);
-  if (a.target && blockIdx.x == 0 && threadIdx.x == 0) *a.chosen = s;
-  const int whole = scalar(whole_heads(a, me.blocks)) * scalar(me.blocks);     // units that are not cut, ahead of the others
-  const int mine = a.n_seq > 1 ? units_of(a, me, s) : whole + (me.blocks * a.kv_heads - whole) * pieces_of(me.tiles, s);
-  int total = scalar(mine), start = 0, cut = 0, taken = 0;     // of the first 64 sequences; units before the lane's, slots before them
-  if (a.n_seq > 1) {
-    start = wave_scan(mine, total);
-    if (a.target) cut = wave_scan(slots_taken(a, me, s), taken);
+__device__ __forceinline__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
+  SeqInfo me;
+  int s, total, whole = 0, start = 0, cut = 0, mine = 0, none;     // units of the call, and of these, ahead of the others, those that are not cut
+  if (a.starts) {
+    s = uniform_at(a.chosen, 0);
+    total = uniform_at(a.chosen, 1);
+  } else {
+    me = lane_seq(a, lane);
+    s = piece_tiles(a, lane, me);
+    if (a.target && blockIdx.x == 0 && threadIdx.x == 0) *a.chosen = s;
+    if (a.n_seq > 1) {
+      mine = units_of(a, me, s);
+      start = wave_scan(mine, total);
+      if (a.target) cut = wave_scan(slots_taken(a, me, s), none);
+    } else {
+      whole = scalar(whole_heads(a, me.blocks)) * scalar(me.blocks);
+      total = scalar(whole + (me.blocks * a.kv_heads - whole) * pieces_of(me.tiles, s));
+    }
   }
-  const int first64 = total;
-  for (int b = 64; b < a.n_seq; b += 64) total += scalar(wave_sum_int(units_of(a, lane_seq(a, b, lane), s)));
   // XCDs take turns with a few units that stand side by side
   const int side = a.rows_per_block <= 64 ? 1 : a.n_seq > 1 ? 8 : min(max(scalar(me.blocks), 1), kSide);
   const uint32_t y = blockIdx.x / kXcd, turn = y / (uint32_t)side;
   const int u = (int)((turn * kXcd + blockIdx.x % kXcd) * side + (y - turn * side));
   if (u >= total || u >= a.most_units) return false;
-  int local = u, j = 0;
+  int local = u;
   w.seq = 0;
   w.slot = u - whole;
-  if (a.n_seq > 1 && u < first64) {
+  if (a.starts) {
+    w.seq = scalar(max(last_at_most(a.starts, a.n_seq, u, lane), 0));
+    info = uniform_seq(a, w.seq);
+    local = u - uniform_at(a.starts, w.seq);
+    w.slot = local + uniform_at(a.taken, w.seq);
+  } else if (a.n_seq > 1) {
     const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= start && u < start + mine);
-    j = scalar(__ffsll((unsigned long long)hit) - 1);
-    w.seq = j;
-    local = u - __builtin_amdgcn_readlane(start, j);
-    w.slot = local + __builtin_amdgcn_readlane(cut, j);
-  }
-  if (u < first64) {
-    info = from_lane(me, j);
+    w.seq = scalar(__ffsll((unsigned long long)hit) - 1);
+    info = from_lane(me, w.seq);
+    local = u - __builtin_amdgcn_readlane(start, w.seq);
+    w.slot = local + __builtin_amdgcn_readlane(cut, w.seq);
   } else {
-    int before = first64;
-    for (int b = 64;; b += 64) {
-      const SeqInfo q = lane_seq(a, b, lane);
-      const int v = units_of(a, q, s);
-      int sum, slots;
-      const int at = before + wave_scan(v, sum), slot = taken + wave_scan(slots_taken(a, q, s), slots);
-      const uint64_t hit = __builtin_amdgcn_ballot_w64(u >= at && u < at + v);
-      if (hit) {
-        j = scalar(__ffsll((unsigned long long)hit) - 1);
-        w.seq = b + j;
-        local = u - __builtin_amdgcn_readlane(at, j);
-        w.slot = local + __builtin_amdgcn_readlane(slot, j);
-        info = from_lane(q, j);
-        break;
-      }
-      before += sum;
-      taken += slots;
-      if (b + 64 >= a.n_seq) return false;      // (lengths that changed meanwhile)
-    }
+    info = from_lane(me, 0);
   }
   w.pieces = u < whole ? 1 : scalar(pieces_of(info.tiles, s));
-  if (w.pieces > 1 && w.slot >= a.slots) return false;      // (offsets that do not ascend)
+  // (offsets that do not ascend, lengths that changed meanwhile.  A second way out of the branches above costs four registers.)
+  if (local >= info.blocks * a.kv_heads * w.pieces || (w.pieces > 1 && w.slot >= a.slots)) return false;
   const int skip = u < whole ? 0 : whole / info.blocks;     // heads
   local -= skip * info.blocks;
   const int len = w.pieces == 1 ? info.tiles : (int)((uint32_t)(info.tiles + w.pieces - 1) / (uint32_t)w.pieces);
@@ -291,6 +290,69 @@ __device__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   w.t0 = scalar(min(piece * len, info.tiles));
   w.t1 = min(w.t0 + scalar(len), info.tiles);
   return true;
+}
+
+// More than 64 sequences: one workgroup works out what the others would take long to, each for itself (one token for each of 1024
+// sequences of 1000 keys, 16 heads on 4 of 128: 390 us so, 623 with every wave looking at all lengths; of 4096 of 250: 593 and
+// 5204; of 256 of 1000: 107 and 121).  Sums in a fixed order.
+__global__ __launch_bounds__(1024) void k_kv_attn_plan(Call a) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
+  __shared__ float works[16];
+  __shared__ int mosts[16], units[2][16], slots[2][16];
+  int s = kUncut;
+  if (a.target) {
+    float work = 0.f;
+    int most = 0;
+    for (int i = tid; i < a.n_seq; i += 1024) {
+      const SeqInfo q = seq_info(a, i);
+      work += (float)q.blocks * (float)q.tiles;
+      most = max(most, q.blocks ? q.tiles : 0);
+    }
+    work = wave_sum_ordered(work);
+    most = (int)~wave_min_u32(~(uint32_t)most);
+    if (lane == 0) {
+      works[wave] = work;
+      mosts[wave] = most;
+    }
+    __syncthreads();
+    work = 0.f;
+    most = 0;
+    for (int i = 0; i < 16; ++i) {
+      work += works[i];
+      most = max(most, mosts[i]);
+    }
+    const SeqInfo none = {0, 0, 0, 0, 0, 0, 0};      // (read for 16 sequences and fewer only)
+    s = piece_tiles(a, lane, none, work, most);
+  }
+  int before = 0, taken = 0;
+  for (int b = 0; b < a.n_seq; b += 1024) {
+    const int i = b + tid, turn = b >> 10 & 1;
+    SeqInfo q = {0, 0, 0, 0, 0, 0, 0};
+    if (i < a.n_seq) q = seq_info(a, i);
+    int u, t;
+    int at = wave_scan(units_of(a, q, s), u), slot = wave_scan(slots_taken(a, q, s), t);
+    if (lane == 0) {
+      units[turn][wave] = u;
+      slots[turn][wave] = t;
+    }
+    __syncthreads();      // (the other of the two is read by nobody any more behind it)
+    for (int x = 0; x < 16; ++x) {
+      at += x < wave ? units[turn][x] : 0;
+      slot += x < wave ? slots[turn][x] : 0;
+    }
+    if (i < a.n_seq) {
+      a.starts[i] = before + at;
+      a.taken[i] = taken + slot;
+    }
+    for (int x = 0; x < 16; ++x) {
+      before += units[turn][x];
+      taken += slots[turn][x];
+    }
+  }
+  if (tid == 0) {
+    a.chosen[0] = s;
+    a.chosen[1] = before;
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1206,24 +1268,26 @@ __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   constexpr int kCh = D / 4, kRowsWg = 256 / (kCh * SL);
   const int tid = threadIdx.x, lane = tid & 63;
   const int tok = blockIdx.x;
-  const int piece_len = *a.chosen;
+  const int piece_len = uniform_at(a.chosen, 0);
   // the token's sequence and the number of its first slot
   SeqInfo s = {0, 0, 0, 0, 0, 0, 0};
   int before = 0;
-  for (int b = 0; b < a.n_seq; b += 64) {
-    const SeqInfo q = lane_seq(a, b, lane);
+  if (a.starts) {
+    const int seq = scalar(last_at_most(a.q_off, a.n_seq, tok, lane));
+    if (seq < 0) return;
+    s = uniform_seq(a, seq);
+    if (tok >= s.q0 + s.nq) return;
+    before = uniform_at(a.taken, seq);
+  } else {
+    const SeqInfo q = lane_seq(a, lane);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(tok >= q.q0 && tok < q.q0 + q.nq);
-    int sum = 0, start = 0;
-    if (a.n_seq > 1) start = wave_scan(slots_taken(a, q, piece_len), sum);
-    if (hit) {
-      const int j = scalar(__ffsll((unsigned long long)hit) - 1);
-      s = from_lane(q, j);
-      before += __builtin_amdgcn_readlane(start, j);
-      break;
-    }
-    before += sum;
+    if (hit == 0) return;
+    const int j = scalar(__ffsll((unsigned long long)hit) - 1);
+    int none, start = 0;
+    if (a.n_seq > 1) start = wave_scan(slots_taken(a, q, piece_len), none);
+    s = from_lane(q, j);
+    before = __builtin_amdgcn_readlane(start, j);
   }
-  if (s.nq == 0) return;
   const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
   if (pieces == 1) return;          // written already
   const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
@@ -1337,9 +1401,9 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m
 }
 // Blocks that are cut take a piece each beside those aimed at, and at most twice as many as were aimed at (slots_taken)
 int64_t slots_of(const Form &f) { return std::min(f.units + f.target, 2 * (int64_t)f.target); }
-size_t sums_bytes(const Form &f, int head_dim) {
-  return f.target == 0 ? 0 : 256 + align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256);
-}
+size_t sums_bytes(const Form &f, int head_dim) { return align_up((size_t)slots_of(f) * f.rows * (head_dim + 2) * sizeof(float), 256); }
+// In front of the sums: 256 bytes, and the plan of more than 64 sequences
+size_t plan_bytes(int n_seq) { return 256 + (n_seq > 64 ? 2 * align_up((size_t)n_seq * sizeof(int), 256) : 0); }
 
 }  // namespace
 
@@ -1351,7 +1415,7 @@ size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_di
   size_t most = 0;
   for (int64_t n : {(int64_t)n_q, (int64_t)32 * n_seq / group, (int64_t)64 * n_seq / group, (256 * cut + 255) / group})
     if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, e4m3, most_keys), head_dim));
-  return most;
+  return most || n_seq > 64 ? plan_bytes(n_seq) + most : 0;
 }
 
 template <typename K, size_t LDS>
@@ -1416,7 +1480,9 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.resident = f.resident;
   c.most_units = (int)(f.units + f.target);
   c.chosen = (int *)ws;
-  c.part = f.target ? (float *)((char *)ws + 256) : nullptr;
+  c.starts = x.n_seq > 64 ? (int *)((char *)ws + 256) : nullptr;
+  c.taken = x.n_seq > 64 ? (int *)((char *)c.starts + align_up((size_t)x.n_seq * sizeof(int), 256)) : nullptr;
+  c.part = f.target ? (float *)((char *)ws + plan_bytes(x.n_seq)) : nullptr;
   c.part_ml = f.target ? (float2 *)(c.part + (size_t)c.slots * f.rows * x.head_dim) : nullptr;
   const int side = f.few ? 1 : x.n_seq > 1 ? 8 : kSide;
   const uint32_t grid = (uint32_t)((f.units + f.target) / kXcd * kXcd + kXcd * (side + 1));     // (whole turns of units side by side)
@@ -1424,6 +1490,7 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
     constexpr Kv KV = decltype(kv)::value;
     return x.head_dim == 64 ? launch_form<KV, 64>(f, c, grid, st) : launch_form<KV, 128>(f, c, grid, st);
   };
+  if (c.starts) k_kv_attn_plan<<<dim3(1), 1024, 0, st>>>(c);
   int rc;
   if (!x.paged) rc = by_kv(std::integral_constant<Kv, Kv::ROWS>{});
   else if (!x.cv.e4m3) rc = by_kv(std::integral_constant<Kv, Kv::PAGES>{});

@@ -12,19 +12,13 @@ namespace lv {
 
 namespace {
 
-// The sequence of token `tok` by its offsets (off[s] <= tok < off[s + 1]), -1 for a token of none.  The wave looks at 64
-// offsets at a time; all its lanes call it with the same tok.
+// The sequence of token `tok` by its offsets (off[s] <= tok < off[s + 1]), -1 for a token of none.  All lanes of the wave call it
+// with the same tok.
 __device__ __forceinline__ int seq_of(const int32_t *off, int n_seq, int tok, int lane, int &start) {
-  int s = 0;
-  for (int b = 0; b < n_seq; b += 64) {
-    const bool past = b + lane < n_seq && off[b + lane + 1] <= tok;
-    const int c = __popcll(__builtin_amdgcn_ballot_w64(past));
-    s += c;
-    if (c < 64) break;
-  }
-  if (s >= n_seq) return -1;
+  const int s = __builtin_amdgcn_readfirstlane(last_at_most(off, n_seq, tok, lane));
+  if (s < 0) return -1;
   start = __builtin_amdgcn_readfirstlane(off[s]);
-  return tok >= start ? s : -1;
+  return tok < __builtin_amdgcn_readfirstlane(off[s + 1]) ? s : -1;
 }
 
 // Bytes of the pool up to position `place` of page `id`, counted in rows

@@ -110,6 +110,19 @@ __device__ __forceinline__ float ga_score(float g, float v, float glo, float gr,
   return alpha * ng + beta * nv;
 }
 
+// The last of n ascending numbers that is at most x, -1 if there is none: the wave looks at 64 of them at a time (up to 2^18).
+__device__ __forceinline__ int last_at_most(const int32_t *v, int n, int x, int lane) {
+  int lo = 0, len = n;
+  for (int step = n <= 64 ? 1 : n <= 4096 ? 64 : 4096;; step >>= 6) {
+    const bool below = lane * step < len && v[lo + lane * step] <= x;
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(below));
+    if (c == 0) return lo - 1;      // (the first round; in the later ones the first of them is known to be)
+    lo += (c - 1) * step;
+    len = min(step, len - (c - 1) * step);
+    if (step == 1) return lo;
+  }
+}
+
 // Only a value that would raise the word sends an atomic (a stale read only sends one too many), and
 // one thread per workgroup does: a few thousand waves that start together all find the word at 0,
 // and their atomics on one address take longer than reading the tensor (5-10 ns each).  (Per wave in the E4M3 kernel with a

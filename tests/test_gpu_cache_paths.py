@@ -175,6 +175,39 @@ def test_many_sequences(n_seq, new, frame, dim, e4m3):
     Paged(4, lens, heads=4, kv_heads=2, dim=dim, e4m3=e4m3, page=32, frame=frame, lost=0.05).check(news)
 
 
+@pytest.mark.parametrize("n_seq", [65, 1000, 4096, 4097, 9000])
+def test_thousands_of_sequences(n_seq):
+    rng = np.random.default_rng(n_seq)
+    lens = rng.integers(0, 40, n_seq)
+    lens[[1, n_seq - 1]] = [2500, 1111]
+    news = np.minimum(rng.integers(0, 3, n_seq), lens)
+    news[[1, n_seq - 1]] = 2
+    some = [0, 1, 63, 64, n_seq // 2, n_seq - 2, n_seq - 1] + rng.integers(0, n_seq, 40).tolist()
+    Paged(17, lens, heads=2, kv_heads=1, dim=64, page=16, lost=0.02).check(news, some)
+    Paged(18, lens, heads=40, kv_heads=1, dim=128, e4m3=True, page=16, frame=1).check(news, some)
+
+
+@pytest.mark.parametrize("n_seq", [64, 65, 4097])
+def test_write_and_read_of_many_sequences(n_seq):
+    """What is written comes back; rows of no sequence are left alone on both sides."""
+    g, rng = gen_of(n_seq), np.random.default_rng(n_seq)
+    new = rng.integers(0, 4, n_seq)
+    pos = rng.integers(0, 30, n_seq)
+    first, n = 3, int(new.sum())      # (three rows before the first sequence's, four behind the last)
+    p = B.make_cache_params(n_seq, 2, 64, page_tokens=16, n_pages=3 * n_seq, max_pages=3)
+    c = B.alloc_cache(p)
+    c.page_table.copy_(torch.from_numpy(rng.permutation(3 * n_seq).reshape(n_seq, 3).astype(np.int32)))
+    off = i32(first + np.concatenate([[0], np.cumsum(new)]))
+    k, v = randn(g, n + 7, 2, 64), randn(g, n + 7, 2, 64)
+    c.k.zero_()
+    B.litevggt_cache_write(p, c, k, v, off, i32(pos))
+    assert int((c.k != 0).any(-1).any(1).sum()) == n
+    a, b = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    B.litevggt_cache_read(p, c, i32(pos), off, a, b)
+    assert torch.equal(a[first:first + n], k[first:first + n]) and torch.equal(b[first:first + n], v[first:first + n])
+    assert (a[:first] == 7.0).all() and (b[first + n:] == 7.0).all()
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("heads,kv", [(7, 1), (15, 5), (14, 2), (1, 1)])
 @pytest.mark.parametrize("new", [1, 5, 37, 90, 300])
