@@ -332,7 +332,7 @@ int litevggt_layers_run(const litevggt_params *p, int n_layers, const void *imag
  * batch has to be known on the host, and a captured call can be replayed with other lengths.  Every
  * number that is read there is checked against the sizes given here; what is out of range is
  * left out, never followed.  A call has fewer than 2^24 tokens (queries, states), and of these times their heads
- * fewer than 2^27.  Scratch for more tokens, all else equal, serves fewer.
+ * fewer than 2^26.  Scratch for more tokens, all else equal, serves fewer.
  */
 enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1 };
 

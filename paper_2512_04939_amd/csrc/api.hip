@@ -157,7 +157,7 @@ bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
   return ((uintptr_t)p & 15u) == 0 && stride % 8 == 0 && stride >= width && stride <= kMostStride && n >= 0;
 }
 // tokens of a call, and of these times heads (grids of 256 threads stay below 2^32 of them in x)
-bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n < ((int64_t)1 << 24) && n * heads < ((int64_t)1 << 27); }
+bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n < ((int64_t)1 << 24) && n * heads < ((int64_t)1 << 26); }
 
 }  // namespace
 

@@ -813,9 +813,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //
 // No register may go to scratch in the loops: reading it back waits for the fetches (three times the time).
 //
-// 13,740 queries over 14,316 states, 16 heads of 64: 770 to 790 us (1.02 to 1.05 PFLOP/s), and 28 to join; 1374 over 138,774 keys in pages: 830 and 24; six
-// chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages 405 and 18;
-// 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128: 116, and 6 for K's normalisation and 12 to join.
+// 13,740 queries over 14,316 states, 16 heads of 64: 770 to 790 us (1.02 to 1.05 PFLOP/s), and 27 to join; 1374 over 138,774 keys in pages: 810 and 18; six
+// chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages 410 and 16;
+// 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128: 116, and 6 for K's normalisation and 14 to join.
 template <int D>
 struct Many {
   static constexpr int QB = D == 64 ? 2 : 1, kWaves = 8 / QB, kRows = 32 * QB;
@@ -1261,98 +1261,113 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
 
 // ---------------------------------------------------------------------------------------
 // The sums of a row's pieces put together, always in the same order.  A row has D / 4 lanes times SL: each of
-// these takes every SL-th piece (few rows, many pieces), and they meet in LDS.  Bound by the way from the lengths to the sums and
-// by reading the latter: 4 pieces of 7 heads of 13,740 rows in 28 us, 3.5 TB/s.
+// these takes every SL-th piece (few rows, many pieces), and they meet in LDS.  SL = 1: 16 or 8 consecutive rows of one kv head, whose sums lie
+// side by side in a slot, mostly of one sequence (otherwise one after the other).  Bound by the way from the lengths to the sums and
+// by reading the latter: 4 pieces of 7 heads of 13,740 rows in 27 us, 4.1 TB/s.  (A token with all its
+// heads to a workgroup instead: 16 pieces of 1374 rows 24 us against 18, ragged rows of heads that share 12.2 against 13.7.)
 template <int D, int SL>
 __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
   constexpr int kCh = D / 4, kRowsWg = 256 / (kCh * SL);
+  static_assert(SL == 1 || kRowsWg == 1, "one sequence");
   const int tid = threadIdx.x, lane = tid & 63;
-  const int tok = blockIdx.x;
-  const int piece_len = uniform_at(a.chosen, 0);
-  // the token's sequence and the number of its first slot
-  SeqInfo s = {0, 0, 0, 0, 0, 0, 0};
-  int before = 0;
-  if (a.starts) {
-    const int seq = scalar(last_at_most(a.q_off, a.n_seq, tok, lane));
-    if (seq < 0) return;
-    s = uniform_seq(a, seq);
-    if (tok >= s.q0 + s.nq) return;
-    before = uniform_at(a.taken, seq);
-  } else {
-    const SeqInfo q = lane_seq(a, lane);
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(tok >= q.q0 && tok < q.q0 + q.nq);
-    if (hit == 0) return;
-    const int j = scalar(__ffsll((unsigned long long)hit) - 1);
-    int none, start = 0;
-    if (a.n_seq > 1) start = wave_scan(slots_taken(a, q, piece_len), none);
-    s = from_lane(q, j);
-    before = __builtin_amdgcn_readlane(start, j);
-  }
-  const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
-  if (pieces == 1) return;          // written already
   const int in_wg = tid / kCh / SL, sl = tid / kCh % SL, ch = tid % kCh * 4;
-  const int hq = blockIdx.y * kRowsWg + in_wg;
-  const bool there = hq < a.heads;
-  const int head = (there ? hq : 0) / a.group, g = (there ? hq : 0) % a.group;
-  const int r = (tok - s.q0) * a.group + g;
-  const int block = r >> a.block_shift, in_block = r & (a.rows_per_block - 1);
-  const int64_t slot0 = before + (int64_t)max(head - whole, 0) * pieces * s.blocks + block;
-  if (slot0 + (int64_t)(pieces - 1) * s.blocks >= a.slots) return;
-  auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
-  // four pieces at a time: their loads are on the way together
-  float top = kUnset, l = 0.f;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int x0 = sl; x0 < pieces; x0 += 4 * SL) {
-    float2 ml[4];
-    f32x4 y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t from = at(min(x0 + i * SL, pieces - 1));
-      ml[i] = a.part_ml[from];
-      y[i] = *(const f32x4 *)(a.part + from * D + ch);
-    }
-    float to = top;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to = fmaxf(to, ml[i].x);
-    const float g = __builtin_amdgcn_exp2f(top - to);
-    top = to;
-    l *= g;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] *= g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (x0 + i * SL >= pieces) break;
-      const float f = __builtin_amdgcn_exp2f(ml[i].x - to);
-      l += ml[i].y * f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += y[i][e] * f;
-    }
+  const int head = blockIdx.y;
+  const uint32_t row = blockIdx.x * kRowsWg + in_wg;
+  const int tok = (int)(row / (uint32_t)a.group), g = (int)row - tok * a.group;
+  const int piece_len = uniform_at(a.chosen, 0);
+  SeqInfo q;
+  int start = 0;
+  if (!a.starts) {
+    q = lane_seq(a, lane);
+    int none;
+    if (a.n_seq > 1) start = wave_scan(slots_taken(a, q, piece_len), none);
   }
-  if constexpr (SL > 1) {
-    __shared__ float tops[kRowsWg][SL], ls[kRowsWg][SL];
-    __shared__ f32x4 sums[kRowsWg][SL][kCh];
-    if (ch == 0) {
-      tops[in_wg][sl] = top;
-      ls[in_wg][sl] = l;
+  bool open = tok < a.n_q;
+  uint64_t left;
+#pragma unroll 1
+  while ((left = __builtin_amdgcn_ballot_w64(open)) != 0) {
+    // the sequence of the first row that is left, the number of its first slot
+    const int first = __builtin_amdgcn_readlane(tok, __ffsll((unsigned long long)left) - 1);
+    SeqInfo s = {0, 0, 0, 0, 0, 0, 0};
+    int before = 0;
+    if (a.starts) {
+      const int seq = scalar(last_at_most(a.q_off, a.n_seq, first, lane));
+      if (seq >= 0) {
+        s = uniform_seq(a, seq);
+        before = uniform_at(a.taken, seq);
+      }
+    } else {
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(first >= q.q0 && first < q.q0 + q.nq);
+      if (hit) {
+        const int j = scalar(__ffsll((unsigned long long)hit) - 1);
+        s = from_lane(q, j);
+        before = __builtin_amdgcn_readlane(start, j);
+      }
     }
-    sums[in_wg][sl][ch / 4] = sum;
-    __syncthreads();
-    if (sl) return;
-    for (int x = 1; x < SL; ++x) top = fmaxf(top, tops[in_wg][x]);
-    l = 0.f;
-    sum = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int x = 0; x < SL; ++x) {
-      const float f = __builtin_amdgcn_exp2f(tops[in_wg][x] - top);
-      const f32x4 y = sums[in_wg][x][ch / 4];
-      l += ls[in_wg][x] * f;
+    const bool its = open && tok >= s.q0 && tok < s.q0 + s.nq;
+    open = open && !its && tok != first;
+    const int pieces = pieces_of(s.tiles, piece_len), whole = whole_heads(a, s.blocks);
+    if (s.nq == 0 || pieces == 1 || head < whole) continue;          // of no sequence; written already
+    const int r = (tok - s.q0) * a.group + g;
+    const int block = r >> a.block_shift, in_block = r & (a.rows_per_block - 1);
+    const int64_t slot0 = before + (int64_t)(head - whole) * pieces * s.blocks + block;
+    const int n = its && slot0 + (int64_t)(pieces - 1) * s.blocks < a.slots ? pieces : 0;
+    auto at = [&](int x) { return (slot0 + (int64_t)x * s.blocks) * a.rows_per_block + in_block; };
+    // four pieces at a time: their loads are on the way together
+    float top = kUnset, l = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int x0 = sl; x0 < n; x0 += 4 * SL) {
+      float2 ml[4];
+      f32x4 y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+      for (int i = 0; i < 4; ++i) {
+        const int64_t from = at(min(x0 + i * SL, n - 1));
+        ml[i] = a.part_ml[from];
+        y[i] = *(const f32x4 *)(a.part + from * D + ch);
+      }
+      float to = top;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to = fmaxf(to, ml[i].x);
+      const float f0 = __builtin_amdgcn_exp2f(top - to);
+      top = to;
+      l *= f0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] *= f0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (x0 + i * SL >= n) break;
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - to);
+        l += ml[i].y * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += y[i][e] * f;
+      }
     }
+    if constexpr (SL > 1) {      // (one row in the workgroup: all of it comes here, and once)
+      __shared__ float tops[SL], ls[SL];
+      __shared__ f32x4 sums[SL][kCh];
+      if (ch == 0) {
+        tops[sl] = top;
+        ls[sl] = l;
+      }
+      sums[sl][ch / 4] = sum;
+      __syncthreads();
+      if (sl) return;
+      for (int x = 1; x < SL; ++x) top = fmaxf(top, tops[x]);
+      l = 0.f;
+      sum = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < SL; ++x) {
+        const float f = __builtin_amdgcn_exp2f(tops[x] - top);
+        const f32x4 y = sums[x][ch / 4];
+        l += ls[x] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += y[e] * f;
+      }
+    }
+    if (n == 0) continue;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    *(u32x2 *)(a.o + (int64_t)tok * a.o_stride + (head * a.group + g) * D + ch) =
+        u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
   }
-  if (!there || head < whole) return;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  *(u32x2 *)(a.o + (int64_t)tok * a.o_stride + hq * D + ch) =
-      u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
 }
 
 // K's rows normalised per head, for cross attention with qk_norm: once for all blocks that read them.  Bound by HBM: 27,216 states
@@ -1498,7 +1513,7 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   if (rc) return rc;
   if (f.target) {
     auto join = [&](auto kernel, int rows) {
-      kernel<<<dim3((uint32_t)x.n_q, (uint32_t)((x.heads + rows - 1) / rows)), 256, 0, st>>>(c);
+      kernel<<<dim3((uint32_t)(((int64_t)x.n_q * c.group + rows - 1) / rows), (uint32_t)x.kv_heads), 256, 0, st>>>(c);
     };
     if (x.head_dim == 64) f.few ? join(k_kv_attn_join<64, 16>, 1) : join(k_kv_attn_join<64, 1>, 16);
     else f.few ? join(k_kv_attn_join<128, 8>, 1) : join(k_kv_attn_join<128, 1>, 8);
