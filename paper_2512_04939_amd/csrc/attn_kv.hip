@@ -714,11 +714,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
     }
   };
+  if (n > 0) {      // (on its way while the rows come)
+    look_up(0);
+    fetch(0);
+  }
   Rows<D, QB> rows;
   rows.load(a, s, w.head, row0, lane);
   if (n > 0) {
-    look_up(0);
-    fetch(0);
     uint64_t shut_now = holes;
     for (int i = 0; i < n; ++i) {
       char *kt = mine + (i % kStages) * (2 * kTile);
