@@ -10,7 +10,7 @@
 // reading K and V (5.0 TB/s of 5.8 that a read alone reaches here, over 32 ragged sequences of an E4M3 cache).  k_kv_attn_many: blocks of
 // 256 rows that walk the keys in stages of 64, which all waves read from LDS; bound, at 64 channels, by the weights' VALU work (a
 // tile of 32 x 32 costs 256 cycles of exp2 and some 170 of multiply-adds, sums and roundings, against 256 of MFMA, which is busy
-// 55 % of the time), at 128 by MFMA (0.93 to 0.97 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
+// 55 % of the time), at 128 by MFMA (0.95 to 1.02 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
 // both a long key axis is cut into pieces that different workgroups take; k_kv_attn_join puts their sums together.
 //
 // Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
@@ -1085,7 +1085,24 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     // A phase: 2 KF products, and the weights of block bw among them, a pair of them to one or two products, each in three
     // steps that stand next to the other pairs' (the exponent of the next, exp2 of this, sum and rounding of the last).  `then` follows
     // product m (reads of fragments).
+    // Rows (no pages) of 128 channels: all weights, then the products, ahead of the other wave's weights: 32 x 2000 queries over 4000
+    // keys, 16 heads 2062 us, weights among the products 2128; of 64 channels 1127 and 1109; in pages, which need more registers, 1374 over
+    // 30,000 keys 511 and 445.
     auto phase = [&](auto scores, auto output, int bw, int bs, int bo, auto &&then) __attribute__((always_inline)) {
+      if constexpr (QB == 1 && KV == Kv::ROWS) {
+        __builtin_amdgcn_sched_barrier(0);
+        weights(bw);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int m = 0; m < 2 * KF; ++m) {
+          product(scores, output, m, bs, bo);
+          then(m);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
+        return;
+      }
       constexpr int kPer = 2 * KF / 8;
       const float ref = rows.ref[QB == 2 ? bw : 0];
       sum0 = sum1 = 0.f;
