@@ -390,8 +390,9 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
  * new_off[s+1]-1 of q are the last ones of sequence s's kv_len[s] positions.  Per query head:
  * o = softmax(q K^T * softmax_scale) V over the positions that are held and that the query sees
  * (frame_tokens); a query that sees none gives zeros.  What lies in positions that a query does not
- * see (infinities and NaN too) has no part in its result.  One token per sequence and whole frames go
- * through the same call.  Rows of no sequence are left as they were.
+ * see (infinities and NaN too) has no part in its result; what is not finite in V where it does see reaches its
+ * result in these channels (an infinity whose weight is below 2^-80 of the row's largest as such or as NaN).  One
+ * token per sequence and whole frames go through the same call.  Rows of no sequence are left as they were.
  *   q   [device] [n_tokens, heads, head_dim] bf16, o likewise, out; row strides in elements as above
  *   ws  litevggt_cached_attn_ws_bytes(p, n_tokens) bytes
  * The weights are rounded to bf16 for the second product; scores, the softmax's sums and

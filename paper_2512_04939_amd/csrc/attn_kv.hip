@@ -536,6 +536,21 @@ struct Rows {
     }
   }
 
+  // block b's references are raised to the largest of a tile's scores, and what has been summed is scaled
+  __device__ __forceinline__ void raise(int b, const f32x16 &s, float c) {
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float to = fmaxf(ref[b], top * c), f = __builtin_amdgcn_exp2f(ref[b] - to);
+    ref[b] = to;
+    l[b] *= f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[b][dt][r] *= f;
+  }
+
   // one tile of 32 keys, 16 from key0 and 16 from key1 on, K and V rows at k_lds and v_lds; what is not held is zeros, its
   // keys are kNoKey.  cut: some row does not see some of the keys.
   __device__ __forceinline__ void tile(const char *k_lds, const char *v_lds, float c, int key0, int key1, bool cut, int lane) {
@@ -589,7 +604,7 @@ struct Rows {
         for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[u][dt][i] & 0x7fff7fffu));
-      if (__builtin_amdgcn_ballot_w64(top.x >= 0x7f80 || top.y >= 0x7f80) != 0) {
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(top.x >= 0x7f80 || top.y >= 0x7f80) != 0, 0)) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -599,7 +614,7 @@ struct Rows {
               const uint32_t w = vf[u][dt][i];
               vf[u][dt][i] = w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
             }
-        add_wild(v_lds, key0, key1, lane);
+        add_wild(s, c, v_lds, key0, key1, lane);
       }
     }
 #pragma unroll
@@ -620,17 +635,7 @@ struct Rows {
       };
       weights();
       if (__builtin_amdgcn_ballot_w64(!(l[b] + (sum0 + sum1) <= kRowRaise)) != 0) {
-        float top = s[b][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[b][r]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float to = fmaxf(ref[b], top * c), f = __builtin_amdgcn_exp2f(ref[b] - to);
-        ref[b] = to;
-        l[b] *= f;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[b][dt][r] *= f;
+        raise(b, s[b], c);
         weights();
       }
       l[b] += sum0 + sum1;
@@ -644,11 +649,18 @@ struct Rows {
     }
   }
 
-  // entries of V that are not finite, to the rows that see their keys
-  __device__ __forceinline__ void add_wild(const char *v_lds, int key0, int key1, int lane) {
+  // Entries of V that are not finite, to the rows that see their keys.  The references are raised before: to raise one scales what has
+  // been summed, at a row's first tile by 0, and an infinity would become NaN.  (In the loop: ahead of it the compiler works it out for
+  // every tile that is cut, and the loops around lose their registers to it.)
+  __device__ __forceinline__ void add_wild(const f32x16 (&s)[QB], float c, const char *v_lds, int key0, int key1, int lane) {
     using T = Tile<D>;
     const int h = lane >> 5;
+#pragma unroll 1
     for (int t = 0; t < 32; ++t) {
+      if (t == 0) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) raise(b, s[b], c);
+      }
       const int key = t < 16 ? key0 + t : key1 + t - 16;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
