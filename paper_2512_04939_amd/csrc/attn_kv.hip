@@ -23,6 +23,7 @@
 
 #include "internal.h"
 #include "common.h"
+#include "kv_plan.h"
 
 namespace lv {
 
@@ -291,7 +292,7 @@ __device__ __forceinline__ bool find_work(const Call &a, int lane, Work &w, SeqI
   }
   w.pieces = u < whole ? 1 : scalar(pieces_of(info.tiles, s));
   // (offsets that do not ascend, lengths that changed meanwhile.  A second way out of the branches above costs four registers.)
-  if (local >= info.blocks * a.kv_heads * w.pieces || (w.pieces > 1 && w.slot >= a.slots)) return false;
+  if (!unit_there(local, info.blocks * a.kv_heads * w.pieces, w.pieces > 1, w.slot, a.slots)) return false;
   const int skip = u < whole ? 0 : whole / info.blocks;     // heads
   local -= skip * info.blocks;
   const int len = w.pieces == 1 ? info.tiles : (int)((uint32_t)(info.tiles + w.pieces - 1) / (uint32_t)w.pieces);
@@ -342,10 +343,10 @@ __global__ __launch_bounds__(1024) void k_kv_attn_plan(Call a) {
     SeqInfo q = {0, 0, 0, 0, 0, 0, 0};
     if (i < a.n_seq) q = seq_info(a, i);
     int u, t;
-    int at = wave_scan(units_of(a, q, s), u), slot = wave_scan(slots_taken(a, q, s), t);
+    int at = wave_scan(share_of(units_of(a, q, s), a.most_units), u), slot = wave_scan(share_of(slots_taken(a, q, s), a.slots), t);
     if (lane == 0) {
-      units[turn][wave] = u;
-      slots[turn][wave] = t;
+      units[turn][wave] = share_of(u, a.most_units);
+      slots[turn][wave] = share_of(t, a.slots);
     }
     __syncthreads();      // (the other of the two is read by nobody any more behind it)
     for (int x = 0; x < 16; ++x) {
@@ -353,12 +354,12 @@ __global__ __launch_bounds__(1024) void k_kv_attn_plan(Call a) {
       slot += x < wave ? slots[turn][x] : 0;
     }
     if (i < a.n_seq) {
-      a.starts[i] = before + at;
-      a.taken[i] = taken + slot;
+      a.starts[i] = start_of(before, at, a.most_units);
+      a.taken[i] = start_of(taken, slot, a.slots);
     }
     for (int x = 0; x < 16; ++x) {
-      before += units[turn][x];
-      taken += slots[turn][x];
+      before = start_of(before, units[turn][x], a.most_units);
+      taken = start_of(taken, slots[turn][x], a.slots);
     }
   }
   if (tid == 0) {
