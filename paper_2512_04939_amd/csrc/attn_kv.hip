@@ -181,8 +181,7 @@ __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInf
   // (a piece's sums are written and read: 8 tiles of many rows' time for the slots' 512 of 64 KB; 3 to 11 make no difference to speak of)
   const float cost = ceilf(units * (1.0f / (float)a.resident)) * (float)(min(s, most) + (s < most && a.rows_per_block > 64 ? 11 : 3)) + (s < most ? 6.f : 0.f);
   // the least, of equal ones the later (longer pieces)
-  const uint32_t key = (uint32_t)fminf(cost * 8.f, 67108863.f) << 6 | (uint32_t)(63 - lane);
-  return __builtin_amdgcn_readlane(s, 63 - (int)(wave_min_u32(key) & 63u));
+  return __builtin_amdgcn_readlane(s, candidate_of(wave_min_u32(cost_key(cost, lane))));
 }
 
 __device__ __forceinline__ int piece_tiles(const Call &a, int lane, const SeqInfo &me) {

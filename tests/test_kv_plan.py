@@ -48,6 +48,24 @@ int main() {
 """
 
 
+KEYS = r"""
+#include <cstdio>
+#include <cmath>
+#include "kv_plan.h"
+// the candidate with the least key, of 64 whose costs come on stdin
+int main() {
+  float cost;
+  uint32_t least = 0xffffffffu;
+  for (int i = 0; i < 64; ++i) {
+    if (scanf("%f", &cost) != 1) return 1;
+    const uint32_t key = lv::cost_key(cost, i);
+    least = key < least ? key : least;
+  }
+  printf("%d\n", lv::candidate_of(least));
+}
+"""
+
+
 @pytest.fixture(scope="module")
 def program(tmp_path_factory):
     d = tmp_path_factory.mktemp("kv_plan")
@@ -114,3 +132,23 @@ int main() {
     subprocess.run(["hipcc", "-O1", "-std=c++17", "--offload-arch=gfx950", "-I", build.CSRC, os.path.join(d, "below.hip"), "-o", os.path.join(d, "below")],
                    check=True, capture_output=True)
     assert subprocess.run([os.path.join(d, "below")]).returncode == 0
+
+
+def test_the_least_cost_is_chosen_however_large_the_costs_are(program):
+    """Up to 2^27 (262,144 blocks of 256 rows over 2^24 keys: 512 rounds of 262,144 tiles) and beyond; of equal ones the last."""
+    d = os.path.dirname(program)
+    with open(os.path.join(d, "keys.hip"), "w") as f:
+        f.write(KEYS)
+    subprocess.run(["hipcc", "-O1", "-std=c++17", "--offload-arch=gfx950", "-I", build.CSRC, os.path.join(d, "keys.hip"), "-o", os.path.join(d, "keys")],
+                   check=True, capture_output=True)
+
+    def chosen(costs):
+        r = subprocess.run([os.path.join(d, "keys")], input=" ".join(str(c) for c in costs), capture_output=True, text=True)
+        return int(r.stdout)
+
+    for size in (0, 7, 100, 1 << 17, 1 << 23, (1 << 23) + 8, 1 << 27, 1 << 31, 1 << 40):
+        for best in (0, 20, 62, 63):
+            costs = [size + max(size // 50, 1) * (1 + i % 9) for i in range(64)]
+            costs[best] = size
+            assert chosen(costs) == best, (size, best)
+        assert chosen([size] * 64) == 63 and chosen([size] * 30 + [2 * size + 1] * 34) == 29
