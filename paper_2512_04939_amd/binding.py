@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -325,15 +326,56 @@ def litevggt_global_block(p: Params, n_tokens: int, z, weights: BlockWeights, de
 class CacheBuffers:
     """Device tensors of a cache (owned by the caller).  ``k``, ``v``: [n_pages, kv_heads, page_tokens, head_dim]
     bf16 or uint8 codes; ``k_scale``, ``v_scale``: uint8 [n_pages, kv_heads, page_tokens] (None for a bf16
-    cache); ``page_table``: int32 [n_seq, max_pages], -1 where no page is held."""
+    cache); ``page_table``: int32 [n_seq, max_pages], -1 where no page is held.  All contiguous; a pool may have
+    more pages, a table more sequences than the parameters of a call say."""
     k: "object"
     v: "object"
     k_scale: "object"
     v_scale: "object"
     page_table: "object"
 
-    def struct(self) -> Cache:
-        return Cache(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), _ptr(self.page_table))
+    def struct(self, p: CacheParams) -> Cache:
+        """The pointers, of tensors that are what a call with these parameters reads and writes."""
+        n, h, g, d = p.n_pages, p.kv_heads, p.page_tokens, p.head_dim
+        table = _buffer(self.page_table, _int32(), (p.n_seq, p.max_pages), "page_table")
+        if p.cache_dtype == CACHE_E4M3:
+            u8 = _uint8()
+            return Cache(_buffer(self.k, u8, (n, h, g, d), "k of the cache"), _buffer(self.v, u8, (n, h, g, d), "v of the cache"),
+                         _buffer(self.k_scale, u8, (n, h, g), "k_scale"), _buffer(self.v_scale, u8, (n, h, g), "v_scale"), table)
+        bf16 = _bf16()
+        return Cache(_buffer(self.k, bf16, (n, h, g, d), "k of the cache"), _buffer(self.v, bf16, (n, h, g, d), "v of the cache"), None, None, table)
+
+    def on(self, p: CacheParams, here: int) -> bool:
+        """Whether what a call with these parameters reads and writes is on that device"""
+        k, v, table = self.k, self.v, self.page_table
+        return (k is None or k.get_device() == here) and (v is None or v.get_device() == here) and (table is None or table.get_device() == here) and (
+            p.cache_dtype != CACHE_E4M3 or all(t is None or t.get_device() == here for t in (self.k_scale, self.v_scale)))
+
+
+def _buffer(t, kind, shape, what: str):
+    """Pointer of a contiguous tensor of `shape`, or longer in its first dimension, or of as many values in a row."""
+    if t is None:      # (the call says so)
+        return None
+    if t.dtype is kind and t.is_contiguous() and t.shape == shape:
+        return t.data_ptr()
+    codes = kind is _uint8() and str(t.dtype) == "torch.float8_e4m3fn"
+    if not (t.dtype is kind or codes) or not t.is_contiguous() or not (
+            t.shape[1:] == shape[1:] and t.shape[0] >= shape[0] if t.dim() > 1 else t.numel() >= math.prod(shape)):
+        raise LiteVGGTError(f"{what}: {' x '.join(str(n) for n in shape)} contiguous values of {kind} wanted, got "
+                            f"{tuple(t.shape)} {t.dtype} with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _stream_of(p, cache, *tensors) -> int:
+    """The current stream, of the device that all of a call's tensors (None: left out) have to lie on."""
+    c = _torch_c()
+    here = c._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise LiteVGGTError(f"tensors on the current device, cuda:{here}, wanted, got one on {t.device}")
+    if cache is not None and not cache.on(p, here):
+        raise LiteVGGTError(f"tensors on the current device, cuda:{here}, wanted, got one of the cache elsewhere")
+    return c._cuda_getCurrentRawStream(here)
 
 
 def alloc_cache(p: CacheParams, device="cuda") -> CacheBuffers:
@@ -384,24 +426,30 @@ def _int32():
     return torch.int32
 
 
+@functools.lru_cache(maxsize=None)
+def _uint8():
+    import torch
+    return torch.uint8
+
+
 def litevggt_cache_write(p: CacheParams, cache: CacheBuffers, k, v, new_off, pos) -> None:
     n, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n, m, "k and v")
-    c = cache.struct()
-    _check(lib().litevggt_cache_write(C.byref(p), C.byref(c), n, kp, ks, vp, vs,
-                                      _ints(new_off, p.n_seq + 1, "new_off"), _ints(pos, p.n_seq, "pos"), _stream()),
-           "litevggt_cache_write")
+    op, pp = _ints(new_off, p.n_seq + 1, "new_off"), _ints(pos, p.n_seq, "pos")
+    c = cache.struct(p)
+    _check(lib().litevggt_cache_write(C.byref(p), C.byref(c), n, kp, ks, vp, vs, op, pp,
+                                      _stream_of(p, cache, k, v, new_off, pos)), "litevggt_cache_write")
 
 
 def litevggt_cache_read(p: CacheParams, cache: CacheBuffers, first, off, k, v) -> None:
     n, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n, m, "k and v")
-    c = cache.struct()
-    _check(lib().litevggt_cache_read(C.byref(p), C.byref(c), _ints(first, p.n_seq, "first"),
-                                     _ints(off, p.n_seq + 1, "off"), n, kp, ks, vp, vs, _stream()),
-           "litevggt_cache_read")
+    fp, op = _ints(first, p.n_seq, "first"), _ints(off, p.n_seq + 1, "off")
+    c = cache.struct(p)
+    _check(lib().litevggt_cache_read(C.byref(p), C.byref(c), fp, op, n, kp, ks, vp, vs,
+                                     _stream_of(p, cache, k, v, first, off)), "litevggt_cache_read")
 
 
 def litevggt_cached_attn_ws_bytes(p: CacheParams, n_tokens: int) -> int:
@@ -412,10 +460,11 @@ def litevggt_cached_attn(p: CacheParams, cache: CacheBuffers, q, new_off, kv_len
     n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
     m, op, os_ = _rows(o, p.heads, p.head_dim, "o")
     _same(n, m, "q and o")
-    c = cache.struct()
+    np_, lp = _ints(new_off, p.n_seq + 1, "new_off"), _ints(kv_len, p.n_seq, "kv_len")
+    c = cache.struct(p)
     wp, wn = _ws_args(ws)
-    _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, _ints(new_off, p.n_seq + 1, "new_off"),
-                                      _ints(kv_len, p.n_seq, "kv_len"), op, os_, wp, wn, _stream()), "litevggt_cached_attn")
+    _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, np_, lp, op, os_, wp, wn,
+                                      _stream_of(p, cache, q, o, new_off, kv_len, ws)), "litevggt_cached_attn")
 
 
 def litevggt_cross_attn_ws_bytes(p: CrossParams, n_q: int, n_kv: int) -> int:
@@ -429,9 +478,10 @@ def litevggt_cross_attn(p: CrossParams, q, q_off, k, v, kv_begin, kv_end, o, ws)
     n_kv, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
     m, vp, vs = _rows(v, p.kv_heads, p.head_dim, "v")
     _same(n_kv, m, "k and v")
+    fp, bp, ep = _ints(q_off, p.n_seq + 1, "q_off"), _ints(kv_begin, p.n_seq, "kv_begin"), _ints(kv_end, p.n_seq, "kv_end")
     wp, wn = _ws_args(ws)
-    _check(lib().litevggt_cross_attn(C.byref(p), n, qp, qs, _ints(q_off, p.n_seq + 1, "q_off"), n_kv, kp, ks, vp, vs,
-                                     _ints(kv_begin, p.n_seq, "kv_begin"), _ints(kv_end, p.n_seq, "kv_end"), op, os_, wp, wn, _stream()), "litevggt_cross_attn")
+    _check(lib().litevggt_cross_attn(C.byref(p), n, qp, qs, fp, n_kv, kp, ks, vp, vs, bp, ep, op, os_, wp, wn,
+                                     _stream_of(p, None, q, o, q_off, k, v, kv_begin, kv_end, ws)), "litevggt_cross_attn")
 
 
 def _same(a: int, b: int, what: str) -> None:
