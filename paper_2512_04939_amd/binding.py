@@ -244,7 +244,7 @@ def _ws_args(ws):
         return None, 0
     base = ws.data_ptr()
     aligned = (base + 255) // 256 * 256
-    return aligned, ws.numel() - (aligned - base)
+    return aligned, max(ws.numel() - (aligned - base), 0)
 
 
 def litevggt_importance(p: Params, images, x, grad_cache, recompute_grad: bool, score, ws) -> None:

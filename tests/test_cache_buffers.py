@@ -130,3 +130,16 @@ def test_tensors_of_another_device(e4m3, monkeypatch):
     for function, args in every:      # all of them on the CPU
         with pytest.raises(B.LiteVGGTError, match="current device, cuda:0, wanted, got one on cpu"):
             function(*args)
+
+
+@pytest.mark.parametrize("size", [0, 1, 10, 255])
+def test_a_workspace_that_ends_before_its_first_aligned_byte_has_none(size):
+    p = params(False, max_pages=64)
+    assert B.litevggt_cached_attn_ws_bytes(p, 5) > 0
+    pool = torch.zeros(1024, dtype=torch.uint8)
+    start = -pool.data_ptr() % 256 + 1                     # the next aligned byte is 255 behind it
+    ws = pool[start:start + size]
+    assert B._ws_args(ws)[1] == 0
+    c, q = B.alloc_cache(p, "cpu"), torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(B.LiteVGGTError, match="workspace"):
+        B.litevggt_cached_attn(p, c, q, OFF, ONE, q, ws)
