@@ -386,7 +386,7 @@ struct Tile {
 __device__ __forceinline__ void fetch_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)),
                "v"(off), "s"(rsrc)
-               : "memory", "m0");
+               : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_vm() {
