@@ -382,7 +382,8 @@ struct Tile {
 };
 
 // 16-byte pieces from global memory straight into LDS at `lds` + 16 * lane.  What lies beyond the range of `rsrc` arrives
-// as zeros.  Not waited for: vmcnt.  (The wait states are for a scalar register that a VALU instruction has just written.)
+// as zeros.  Not waited for: vmcnt.  (The wait states are for a scalar register that a VALU instruction has just written.  The compiler
+// takes no declaration of m0, which it keeps for itself: nothing else in these kernels may use it.)
 __device__ __forceinline__ void fetch_lds(u32x4 rsrc, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)),
                "v"(off), "s"(rsrc)
