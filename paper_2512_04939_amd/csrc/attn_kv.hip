@@ -50,7 +50,7 @@ struct Call {
   uint16_t *o;
   int64_t q_stride, o_stride;
   const int32_t *q_off, *k_begin, *k_end;
-  int n_q, n_seq, heads, kv_heads, group, qk_norm, frame, n_kv;
+  int n_q, n_seq, kv_heads, group, qk_norm, frame, n_kv;
   float c;
   const char *k, *v;
   int64_t k_stride, v_stride;            // bytes
@@ -1477,9 +1477,12 @@ size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_di
   return most || n_seq > 64 ? plan_bytes(n_seq) + most : 0;
 }
 
+// LDS that a kernel has of its own beside what its launch asks for, at most: the lists of pages of eight waves (k_kv_attn_many)
+constexpr size_t kStaticLds = 8 * 2 * 256 * sizeof(int);
+
 template <typename K, size_t LDS>
 static int go(K kernel, std::atomic<uint64_t> &done, std::integral_constant<size_t, LDS>, const Call &c, uint32_t grid, int threads, hipStream_t st) {
-  if constexpr (LDS > 60000) {     // (a kernel has up to 1 KB beside it)
+  if constexpr (LDS + kStaticLds > 65536) {     // (what a launch may take of its own accord)
     const int rc = allow_dynamic_lds<LDS>((const void *)kernel, done);
     if (rc) return rc;
   }
@@ -1513,7 +1516,6 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   c.k_end = x.k_end;
   c.n_q = x.n_q;
   c.n_seq = x.n_seq;
-  c.heads = x.heads;
   c.kv_heads = x.kv_heads;
   c.group = x.heads / x.kv_heads;
   c.qk_norm = x.qk_norm;
