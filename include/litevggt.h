@@ -338,8 +338,8 @@ enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1 };
 
 typedef struct {
   int32_t n_seq;           /* sequences of a call, 1 .. 65535                          */
-  int32_t heads;           /* query heads, a multiple of kv_heads: query head h uses kv head
-                              h / (heads / kv_heads)                                   */
+  int32_t heads;           /* query heads, at most 1024, a multiple of kv_heads: query head h
+                              uses kv head h / (heads / kv_heads)                      */
   int32_t kv_heads;        /* heads of K and V, 1 .. 1024; n_seq * kv_heads at most 2^22 */
   int32_t head_dim;        /* 64 or 128                                                */
   int32_t cache_dtype;     /* LV_CACHE_BF16 or LV_CACHE_E4M3                           */
@@ -397,7 +397,9 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
  *   ws  litevggt_cached_attn_ws_bytes(p, n_tokens) bytes
  * The weights are rounded to bf16 for the second product; scores, the softmax's sums and
  * the output's stay fp32 (weights may reach 2^40 before they are divided by their sum: V's finite values are
- * to lie below 2^80).  Results do not depend on the order in which workgroups run.
+ * to lie below 2^80, and scores, times softmax_scale, below 2^28 in magnitude: far beyond it a row may come out as
+ * if it saw no key; so does one whose scores are all minus infinity).  Results do not depend on the order in
+ * which workgroups run.
  */
 size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens);
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,

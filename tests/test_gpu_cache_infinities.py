@@ -61,3 +61,19 @@ def test_an_infinity_at_a_key_of_far_the_largest_score(new, dim):
     c.d = c.device()
     # (scores 8 * 10 * dim / sqrt(dim) = 640 or 905 against 0, products and sums exact)
     same(*c.attend([new], q=np.full((new, 2, dim), 10.0)))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [2, 40, 200])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_as_large_as_allowed(sign, new, dim):
+    """Scores of +-2^27 and half of that (64 channels; half as much again for 128): the keys of the larger ones share the weight, to the
+    last bit (the next ones' is exp(-2^26))."""
+    c = Case(44, [150 + new], heads=2, kv_heads=1, head_dim=dim, page=16, frame=0)
+    for t in range(150 + new):
+        page, row = c.o.place(0, t)
+        c.o.k[page, 0, row] = sign * (2.0 ** 13 if t % 3 else 2.0 ** 12)
+    c.d = c.device()
+    got, exact, _ = c.attend([new], q=np.full((new, 2, dim), 2.0 ** 11))
+    # equal weights, rounded equally: only the result's rounding is left, and fp32 sums of 300 values below 8
+    assert np.all(np.abs(got - exact) <= 2.0 ** -8 * np.abs(exact) + 300 * 8 * 2.0 ** -24)
