@@ -7,11 +7,13 @@
 //
 // A row is a (query token, head) pair; the heads that share a kv head are rows of one block, so K and V are read once for
 // all of them.  Two kernels.  k_kv_attn_few: blocks of 32 or 64 rows whose four waves take 32 of every 128 keys each; bound by
-// reading K and V (5.0 TB/s of 5.8 that a read alone reaches here, over 32 ragged sequences of an E4M3 cache).  k_kv_attn_many: blocks of
-// 256 rows that walk the keys in stages of 64, which all waves read from LDS; bound, at 64 channels, by the weights' VALU work (a
-// tile of 32 x 32 costs 256 cycles of exp2 and some 170 of multiply-adds, sums and roundings, against 256 of MFMA, which is busy
-// 55 % of the time), at 128 by MFMA (0.95 to 1.02 PFLOP/s; a library's product of 8192^3 reaches 1.37 on the same card).  In
-// both a long key axis is cut into pieces that different workgroups take; k_kv_attn_join puts their sums together.
+// reading K and V (5.2 TB/s of 5.9 that a read alone reaches here, over 32 ragged sequences of an E4M3 cache).  k_kv_attn_many: blocks of
+// 256 rows that walk the keys in stages of 64, which all waves read from LDS.  1.0 PFLOP/s for equal lengths, at 64 and at 128 channels (a
+// library's product of 8192^3 reaches 1.37 on the same card), where MFMA is busy 55 and 56 % of the time.  At 64 channels a tile of 32 x 32
+// costs 256 cycles of exp2 and some 170 of multiply-adds, sums and roundings against 256 of MFMA: instructions of the VALU, the
+// products' issue among them, are active 80 % of a SIMD's cycles, and its two waves wait 37 % of theirs for a turn to issue and 13 % for data
+// and barriers.  At 128 channels the VALU is active 56 %, the waves wait 36 and 25 %.  In
+// both kernels a long key axis is cut into pieces that different workgroups take; k_kv_attn_join puts their sums together.
 //
 // Scores are computed transposed, S^T = K Q^T (32x32x16 MFMA, K as A operand): a lane owns one row's scores, and the
 // weights already lie as the B operand of O^T += V^T P^T.  K and V lie in LDS as rows; V's fragments come out by transposing reads.
@@ -233,9 +235,8 @@ __device__ __forceinline__ SeqInfo from_lane(const SeqInfo &q, int j) {
 
 // The workgroup's piece of the call, in the order (sequence, head, piece, block): workgroups that read the same keys stand side by
 // side, and up to 8 (several sequences) or 16 of them go to one XCD, whose L2 then brings K and V once.  (Many rows; each of
-// them by itself in turn: 1374 queries over 138,774 keys 889 us against 851, 32 x 2000 over 4000 1126 against 1068, both 16 heads of 64.
-// All blocks' tiles as one line in equal shares, so that nothing has to be searched: 1365 for the latter, sharers walk at different
-// places.)
+// them by itself in turn: 1374 queries over 138,774 keys 871 us against 835, 32 x 2000 over 4000 1109 against 1046, both 16 heads of 64;
+// 1374 over 30,000 in pages, 16 heads of 128, 439 against 407.)
 __device__ __forceinline__ bool find_work(const Call &a, int lane, Work &w, SeqInfo &info) {
   SeqInfo me;
   int s, total, whole = 0, start = 0, cut = 0, mine = 0, none;     // units of the call, and of these, ahead of the others, those that are not cut
@@ -250,7 +251,7 @@ __device__ __forceinline__ bool find_work(const Call &a, int lane, Work &w, SeqI
       mine = units_of(a, me, s);
       if (a.rows_per_block > 64 && a.n_seq <= 16) {
         // the sequences of the longest pieces first, so that short ones fill the last round (12 of 100 to 2000 queries over 100 to 15,000
-        // keys 478 -> 463 us, 6 of 261 to 2088 over up to 20,097 488 -> 483; 64 sequences 186 -> 205, by the loop itself)
+        // keys 459 -> 449 us, 6 of 261 to 2088 over up to 20,097 417 -> 408; 64 of 70 to 400 over 100 to 2000 143 -> 160, by the loop itself)
         const int n = pieces_of(me.tiles, s), len = (int)((uint32_t)(me.tiles + n - 1) / (uint32_t)n);
         total = 0;
         for (int j = 0; j < a.n_seq; ++j) {
@@ -685,8 +686,8 @@ struct Rows {
 // Few rows.  A workgroup has 32 or 64 rows of a (sequence, kv head) and a piece of its keys, in tiles of 128: wave w takes the w-th 32
 // keys of each, through LDS of its own, so nobody waits for anybody before the end.  bf16: two
 // tiles in LDS, the next one on its way while one is computed with; E4M3: the next tile's codes on their way in registers, turned
-// into bf16 in LDS.  Two workgroups per CU where LDS allows.  5 queries over 137,405 keys, 16 heads of 64, bf16: 100 us, 5.6 TB/s, and 5 to
-// join; 32 tokens over 301 to 30,011 keys, 16 heads on 4 of 128, E4M3: 94 us, and 5 to join.  (Eight waves to a
+// into bf16 in LDS.  Two workgroups per CU where LDS allows.  5 queries over 137,405 keys, 16 heads of 64, bf16: 99 us, 5.7 TB/s, and 5 to
+// join; 32 tokens over 301 to 30,011 keys, 16 heads on 4 of 128, E4M3: 97 us, 5.2 TB/s, and 5 to join.  (Eight waves to a
 // workgroup where there are few of them: 34.1 us against 32.0 for 24 rows over 30,000 keys, 17.2 against 14.4 for 48 over 2000.)
 template <Kv KV, int D, int QB>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_few(Call a) {
@@ -840,9 +841,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //
 // No register may go to scratch in the loops: reading it back waits for the fetches (three times the time).
 //
-// 13,740 queries over 14,316 states, 16 heads of 64: 770 to 790 us (1.02 to 1.05 PFLOP/s), and 27 to join; 1374 over 138,774 keys in pages: 810 and 18; six
-// chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages 410 and 16;
-// 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128: 116, and 6 for K's normalisation and 14 to join.
+// Whole calls: 13,740 queries over 14,316 states, 16 heads of 64: 782 to 805 us (1.00 to 1.03 PFLOP/s), 28 of them to join; 1374 over 138,774
+// keys in pages 835 (0.93), 19 to join; six chunks of 261 to 2088 over up to 20,097 keys in E4M3 pages, every seventh given back, 408 to 413
+// (0.80), 17 to join; 3 to 701 queries over up to 6007 states, 16 heads on 2 of 128, 134 (0.57): 6 for K's normalisation, 14 to join.  16
+// heads of 128: 32 x 2000 over 4000 2045 (1.03), 1374 over 30,000 keys in pages 407 to 418 (0.81 to 0.83), 457 in E4M3 pages (0.74).
 template <int D>
 struct Many {
   static constexpr int QB = D == 64 ? 2 : 1, kWaves = 8 / QB, kRows = 32 * QB;
@@ -1099,8 +1101,8 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
     // steps that stand next to the other pairs' (the exponent of the next, exp2 of this, sum and rounding of the last).  `then` follows
     // product m (reads of fragments).
     // Rows (no pages) of 128 channels: all weights, then the products, ahead of the other wave's weights: 32 x 2000 queries over 4000
-    // keys, 16 heads 2062 us, weights among the products 2128; of 64 channels 1127 and 1109; in pages, which need more registers, 1374 over
-    // 30,000 keys 511 and 445.
+    // keys, 16 heads 2070 us, weights among the products 2092; of 64 channels 1080 and 1057.  Where calls are small or in pages the sides lie
+    // close, and not always so: 9 sets of 3 to 701 over up to 6007 134 and 127, 1374 over 30,000 keys in pages 407 and 414, in E4M3 pages level.
     auto phase = [&](auto scores, auto output, int bw, int bs, int bo, auto &&then) __attribute__((always_inline)) {
       if constexpr (QB == 1 && KV == Kv::ROWS) {
         __builtin_amdgcn_sched_barrier(0);
@@ -1307,7 +1309,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
 // The sums of a row's pieces put together, always in the same order.  A row has D / 4 lanes times SL: each of
 // these takes every SL-th piece (few rows, many pieces), and they meet in LDS.  SL = 1: 16 or 8 consecutive rows of one kv head, whose sums lie
 // side by side in a slot, mostly of one sequence (otherwise one after the other).  Bound by the way from the lengths to the sums and
-// by reading the latter: 4 pieces of 7 heads of 13,740 rows in 27 us, 4.1 TB/s.  (A token with all its
+// by reading the latter: 4 pieces of 7 heads of 13,740 rows in 28 us, 4.0 TB/s.  (A token with all its
 // heads to a workgroup instead: 16 pieces of 1374 rows 24 us against 18, ragged rows of heads that share 12.2 against 13.7.)
 template <int D, int SL>
 __global__ __launch_bounds__(256) void k_kv_attn_join(Call a) {
@@ -1440,8 +1442,9 @@ struct Form {
 };
 
 // Which kernel: by the rows that a (sequence, kv head) has on average.  64 channels, 16 heads of one sequence: 24 rows over 30,000
-// keys 32 us in blocks of 32 rows, 51 in those of 256; 48 rows 34 us in blocks of 64, 49 of 32, 50 of 256 (over 2000 keys 14.4, -, 20.7);
-// 100 rows 89 of 32, 58 of 256.  128 channels: 48 rows of 8 sequences 101 us in blocks of 32, 65 of 256 (64 do not fit the registers).
+// keys 29 us in blocks of 32 rows, 41 in those of 256; 48 rows 31 us in blocks of 64, 46 of 32, 41 of 256 (over 2000 keys 12.6, 12.1, 17);
+// 100 rows 51 of 64, 84 of 32, 49 of 256.  128 channels, 8 sequences over 4000 keys: 24 rows 54 us in blocks of 32, 61 of 256; 48 rows 90 and 63
+// (64 do not fit the registers).
 Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
   Form f;
   const int group = heads / kv_heads;
@@ -1453,7 +1456,7 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (Blocks of several sequences that fill the chip four times over are not cut: 32 x 2000 queries over 4000 keys, 16 heads of 64
-  // 1068 us against 1111 cut, of 128 2181 against 2305, 64 ragged sequences 1287 against 1346.  One sequence: whole_heads.)
+  // 1043 us against 1089 cut, of 128 2045 against 2177, 64 sequences of 100 to 2000 over 100 to 4000 608 against 650.  One sequence: whole_heads.)
   const int64_t target = f.units >= 4 * f.resident && !f.few && n_seq > 1 ? 0 : tiles < kWholeTiles ? 0 : kRounds * f.resident;
   f.target = (int)(target < f.units * tiles ? target : f.units * tiles);
   return f;
