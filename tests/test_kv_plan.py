@@ -106,7 +106,7 @@ def test_units_of_offsets_that_do_not_ascend(program, n_seq, kv_heads, n_q, cut)
     n_q -= n_q % 2
     units = [(n_q - s) * kv_heads // 32 if s % 2 == 0 else 0 for s in range(n_seq)]
     room = (n_q // 32 + n_seq) * kv_heads + 1536
-    slots = 3072 if cut else 0
+    slots = 3000 if cut else 0
     taken = units if cut else [0] * n_seq
     starts, before, found = plan(program, room, slots, units, taken)
     assert max(units) * (n_seq // 2) > room and starts == sorted(starts) and before == sorted(before)
@@ -121,9 +121,9 @@ def test_numbers_below_zero_are_no_units(program):
     source = PROGRAM[:PROGRAM.index("int main")] + r"""
 int main() {
   const int units = 12788 * 64;
-  return lv::unit_there(-2076502332, units, false, 0, 0) || lv::unit_there(-1, units, false, 0, 0) || lv::unit_there(0, units, true, -1, 3072) ||
+  return lv::unit_there(-2076502332, units, false, 0, 0) || lv::unit_there(-1, units, false, 0, 0) || lv::unit_there(0, units, true, -1, 3000) ||
          lv::unit_there(units, units, false, 0, 0) || lv::unit_there(0, 0, false, 0, 0) || !lv::unit_there(units - 1, units, false, -1, 0) ||
-         !lv::unit_there(0, units, true, 3071, 3072) || lv::unit_there(0, units, true, 3072, 3072);
+         !lv::unit_there(0, units, true, 2999, 3000) || lv::unit_there(0, units, true, 3000, 3000);
 }
 """
     d = os.path.dirname(program)
