@@ -334,7 +334,7 @@ int litevggt_layers_run(const litevggt_params *p, int n_layers, const void *imag
  * left out, never followed.  A call has fewer than 2^24 tokens (queries, states), and of these times their heads
  * fewer than 2^26.  Scratch for more tokens, all else equal, serves fewer.
  */
-enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1 };
+enum { LV_CACHE_BF16 = 0, LV_CACHE_E4M3 = 1, LV_CACHE_E2M1 = 4 };   /* 16, 8 and 4 bits */
 
 typedef struct {
   int32_t n_seq;           /* sequences of a call, 1 .. 65535                          */
@@ -342,7 +342,7 @@ typedef struct {
                               uses kv head h / (heads / kv_heads)                      */
   int32_t kv_heads;        /* heads of K and V, 1 .. 1024; n_seq * kv_heads at most 2^22 */
   int32_t head_dim;        /* 64 or 128                                                */
-  int32_t cache_dtype;     /* LV_CACHE_BF16 or LV_CACHE_E4M3                           */
+  int32_t cache_dtype;     /* LV_CACHE_BF16, LV_CACHE_E4M3 or LV_CACHE_E2M1            */
   int32_t page_tokens;     /* positions of a page: 16, 32, .. 1024                     */
   int32_t n_pages;         /* pages of the pool                                        */
   int32_t max_pages;       /* columns of the page table                                */
@@ -356,12 +356,15 @@ typedef struct {
 
 /* Caller-owned device buffers of a cache.  Position t of sequence s is row t % page_tokens of page
  * page_table[s][t / page_tokens]; a number outside 0 .. n_pages-1 (-1): the page is not held.
- * E4M3: value = code * 2^(scale - 127), scale 1 .. 254, one per row (token and kv head, K and V apart).  Pages
+ * E4M3: value = code * 2^(scale - 127), scale 1 .. 254, one per row (token and kv head, K and V apart).  E2M1: two codes to a byte, the even
+ * channel's in the low half (0 0.5 1 1.5 2 3 4 6 by its low three bits, the fourth is the sign); value = code * 2^(scale - 127), scale 1 ..
+ * 254, one per 32 consecutive channels of a row; 255: all 32 are NaN.  Pages
  * may serve several sequences for reading; a row where the writes of two sequences of a call, or of two calls at
  * once, meet may hold parts of both. */
 typedef struct {
-  void *k, *v;                  /* [n_pages][kv_heads][page_tokens][head_dim] bf16 or E4M3 codes */
-  uint8_t *k_scale, *v_scale;   /* [n_pages][kv_heads][page_tokens]; LV_CACHE_E4M3 only          */
+  void *k, *v;                  /* [n_pages][kv_heads][page_tokens][head_dim] bf16 or E4M3 codes,
+                                   [..][head_dim / 2] bytes of E2M1 codes                        */
+  uint8_t *k_scale, *v_scale;   /* E4M3: [n_pages][kv_heads][page_tokens]; E2M1: [..][page_tokens][head_dim / 32] */
   const int32_t *page_table;    /* [n_seq][max_pages]                                            */
 } litevggt_cache;
 
@@ -369,7 +372,8 @@ typedef struct {
  * sequence s, for new_off[s] <= row < new_off[s+1].  Rows of no sequence and positions whose page is not held are
  * left out; every other row of the pool keeps what it holds.  E4M3: a row's scale is the smallest power of two (at
  * least 2^-126, 1 for a row of zeros) with max|x| <= 448 * scale over the finite values of the row; code =
- * RNE(x / scale); infinities become +-448 * scale, NaN stays.
+ * RNE(x / scale); infinities become +-448 * scale, NaN stays.  E2M1: the same for each 32 channels with 6 in place of 448, but that a
+ * NaN makes all 32 NaN.  (A value that rounds to 2^128 is read back as infinity.)
  *   k, v     [device] [n_tokens, kv_heads, head_dim] bf16, rows k_stride, v_stride elements apart
  *            (multiples of 8, at least kv_heads * head_dim, at most 2^26)
  *   new_off  [device] [n_seq+1] ascending;  pos [device] [n_seq]
@@ -405,6 +409,67 @@ size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_t
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
                          const void *q, int64_t q_stride, const int32_t *new_off, const int32_t *kv_len,
                          void *o, int64_t o_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* The attention weight that the positions of a cache draw, added up: for the rows r of q (all query heads of kv head h, the tokens of
+ * sequence s, as in litevggt_cached_attn: same masks, same normalisation)
+ *   mass[s][h][t] = mass_in[s][h][t] + sum_r w_rt / sum_t' w_rt',   w_rt = exp(q_r . k_t * softmax_scale)
+ * for the positions t below kv_len[s] that are held, 0 for those that are not; what lies from kv_len[s] on is left as it was.  A row that
+ * sees no held position adds nothing; one with a score that is NaN makes all that it sees NaN.  Everything is fp32 (from bf16 q and K as
+ * it is held); results do not depend on the order in which workgroups run.  The call needs neither v nor v_scale.
+ *   mass_in  [device] [n_seq][kv_heads][max_pages * page_tokens] fp32, 16-byte aligned; NULL: zeros; may be the same buffer as mass
+ *   mass     [device] the same, out
+ *   ws       litevggt_cached_mass_ws_bytes(p, n_tokens) bytes
+ */
+size_t litevggt_cached_mass_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens);
+int litevggt_cached_mass(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens, const void *q, int64_t q_stride,
+                         const int32_t *new_off, const int32_t *kv_len, const float *mass_in, float *mass, void *ws, size_t ws_bytes,
+                         void *stream);
+
+/* Eviction: of every sequence the pages that have drawn the least leave until at most keep[s] are held.  Looked at are the held pages of the
+ * first ceil(kv_len[s] / page_tokens) columns of the page table; of these columns the first `first_pages` and the last `last_pages`
+ * stay in any case (their pages count among the held ones).  A page's mass is the sum over all kv heads and over its positions below
+ * kv_len[s]; of equal ones the earlier column leaves first; NaN counts as more than any number.
+ *   page_table [device] [n_seq][max_pages];  mass [device] as in litevggt_cached_mass
+ *   keep       [device] [n_seq] (below 0: as 0)
+ *   table_out  [device] the table with -1 where a page left; may be the same buffer as page_table
+ *   freed      [device] [n_seq][max_pages] the pages that left, in the order of their columns, -1 behind them; another buffer
+ *   n_freed    [device] [n_seq] how many
+ *   ws         litevggt_cache_evict_ws_bytes(p) bytes
+ * Positions keep their numbers: what stays is attended to as before.  Pages that serve several sequences: each gives back its own use of them.
+ * Of p: n_seq, kv_heads, page_tokens, n_pages, max_pages; the rest has to be valid.
+ */
+size_t litevggt_cache_evict_ws_bytes(const litevggt_cache_params *p);
+int litevggt_cache_evict(const litevggt_cache_params *p, const int32_t *page_table, const int32_t *kv_len, const float *mass,
+                         const int32_t *keep, int first_pages, int last_pages, int32_t *table_out, int32_t *freed, int32_t *n_freed,
+                         void *ws, size_t ws_bytes, void *stream);
+
+/* Rotary positions with several axes (row and column of a patch; time, row and column; ..): q and k before they are used or stored.
+ * Axis a turns pairs[a] pairs of every head's channels, R = sum of pairs.  Pair i (j-th of axis a, whose first is i_a):
+ *   y1 = x1 cos t - x2 sin t,  y2 = x2 cos t + x1 sin t,   t = pos[token][a] * freq(i),   rounded once, to bf16
+ *   LV_ROPE_AXIS_HALVES  channels 2 i_a + j and 2 i_a + pairs[a] + j
+ *   LV_ROPE_HEAD_HALVES  channels i and R + i
+ *   LV_ROPE_ADJACENT     channels 2 i and 2 i + 1
+ *   freq(i) = base^(-j / pairs[a]), with `joint` base^(-i / R), or p->freq[i] where that is given
+ * Channels from 2 R on are copied.  Angles are exact to 2^-24 turns or so at any position.  `inverse`: by -t, which undoes it and is its gradient.
+ *   pos    [device] [n_tokens][axes] int32, of any sign
+ *   q, q_out [device] [n_tokens, heads, head_dim] bf16;  k, k_out [device] [n_tokens, kv_heads, head_dim] bf16, not read with
+ *            kv_heads = 0; row strides in elements (multiples of 8); an output may be its input, with the same stride
+ */
+enum { LV_ROPE_AXIS_HALVES = 0, LV_ROPE_HEAD_HALVES = 1, LV_ROPE_ADJACENT = 2 };
+typedef struct {
+  int32_t heads;           /* 1 .. 1024                                                */
+  int32_t kv_heads;        /* 0 .. 1024                                                */
+  int32_t head_dim;        /* 64 or 128                                                */
+  int32_t axes;            /* 1 .. 4                                                   */
+  int32_t pairs[4];        /* at least 1 for each axis, 2 R at most head_dim           */
+  int32_t pairing;         /* LV_ROPE_*                                                */
+  int32_t joint;           /* != 0: the frequencies of all axes are one ladder         */
+  int32_t inverse;
+  float   base;            /* > 0 (100 for patches, 10000); not read where freq is given */
+  const double *freq;      /* [host] [R] radians a position, at most 1e6 in magnitude, or NULL */
+} litevggt_rope_params;
+int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t *pos, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream);
 
 /* Cross attention: the queries q_off[s] .. q_off[s+1]-1 attend to the states kv_begin[s] ..
  * kv_end[s]-1, rows of another set of another length (ranges may overlap: several query sets over the

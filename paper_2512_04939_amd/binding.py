@@ -23,7 +23,8 @@ LINEAR_BF16, LINEAR_FP8_E4M3 = 0, 1
 FP8_CURRENT, FP8_DELAYED = 0, 1
 FP8_HISTORY = 80
 FP8_STATE_BYTES = 4 * (FP8_HISTORY + 2) * 4
-CACHE_BF16, CACHE_E4M3 = 0, 1
+CACHE_BF16, CACHE_E4M3, CACHE_E2M1 = 0, 1, 4
+ROPE_AXIS_HALVES, ROPE_HEAD_HALVES, ROPE_ADJACENT = 0, 1, 2
 ROLE_PROTECTED, ROLE_DST, ROLE_SRC = 0, 1, 2
 
 STATIC_SCORE_MAX = 2 * 1024 * 1024
@@ -33,7 +34,8 @@ EXPORTS = ["litevggt_strerror", "litevggt_plan", "litevggt_attn_ws_bytes", "lite
            "litevggt_unmerge", "litevggt_frame_attn_ws_bytes", "litevggt_frame_attn",
            "litevggt_global_block_ws_bytes", "litevggt_global_block",
            "litevggt_cache_write", "litevggt_cache_read", "litevggt_cached_attn_ws_bytes",
-           "litevggt_cached_attn", "litevggt_cross_attn_ws_bytes", "litevggt_cross_attn",
+           "litevggt_cached_attn", "litevggt_cached_mass_ws_bytes", "litevggt_cached_mass",
+           "litevggt_cache_evict_ws_bytes", "litevggt_cache_evict", "litevggt_rope", "litevggt_cross_attn_ws_bytes", "litevggt_cross_attn",
            "litevggt_layers_run", "litevggt_probe_mfma", "litevggt_probe_stream",
            "litevggt_probe_mfma_flop", "litevggt_probe_gather"]
 
@@ -88,6 +90,12 @@ class Cache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")]
 
 
+class RopeParams(C.Structure):
+    """Mirror of ``litevggt_rope_params``."""
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("axes", C.c_int32), ("pairs", C.c_int32 * 4),
+                ("pairing", C.c_int32), ("joint", C.c_int32), ("inverse", C.c_int32), ("base", C.c_float), ("freq", C.POINTER(C.c_double))]
+
+
 class CrossParams(C.Structure):
     """Mirror of ``litevggt_cross_params``."""
     _fields_ = [(n, C.c_int32) for n in ("n_seq", "heads", "kv_heads", "head_dim", "qk_norm")] + [
@@ -102,6 +110,16 @@ def make_cache_params(n_seq, heads, head_dim, *, kv_heads=None, cache_dtype=CACH
 
 def make_cross_params(n_seq, heads, head_dim, *, kv_heads=None, qk_norm=0, softmax_scale=0.0) -> CrossParams:
     return CrossParams(n_seq, heads, heads if kv_heads is None else kv_heads, head_dim, qk_norm, softmax_scale)
+
+
+def make_rope_params(heads, head_dim, pairs, *, kv_heads=None, pairing=ROPE_AXIS_HALVES, joint=0, inverse=0, base=100.0, freq=None) -> RopeParams:
+    """``pairs``: the pairs of channels that each axis turns; ``freq``: radians a position for every pair, in place of ``base``."""
+    pairs = list(pairs)
+    if not 1 <= len(pairs) <= 4 or (freq is not None and len(freq) != sum(pairs)):
+        raise LiteVGGTError(f"rope: pairs of 1 to 4 axes and as many frequencies as pairs wanted, got {pairs} and "
+                            f"{None if freq is None else len(freq)}")
+    return RopeParams(heads, heads if kv_heads is None else kv_heads, head_dim, len(pairs), (C.c_int32 * 4)(*pairs), pairing, joint, inverse, base,
+                      None if freq is None else (C.c_double * len(freq))(*freq))
 
 
 def make_params(frames, grid_h, grid_w, dim, heads, *, head_dim=64, n_special=5, patch=14,
@@ -152,6 +170,13 @@ def lib() -> C.CDLL:
         L.litevggt_cached_attn_ws_bytes.restype = sz
         L.litevggt_cached_attn_ws_bytes.argtypes = [CP, i64]
         L.litevggt_cached_attn.argtypes = [CP, CC, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+        L.litevggt_cached_mass_ws_bytes.restype = sz
+        L.litevggt_cached_mass_ws_bytes.argtypes = [CP, i64]
+        L.litevggt_cached_mass.argtypes = [CP, CC, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.litevggt_cache_evict_ws_bytes.restype = sz
+        L.litevggt_cache_evict_ws_bytes.argtypes = [CP]
+        L.litevggt_cache_evict.argtypes = [CP, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.litevggt_rope.argtypes = [C.POINTER(RopeParams), i64, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
         L.litevggt_cross_attn_ws_bytes.restype = sz
         L.litevggt_cross_attn_ws_bytes.argtypes = [XP, i64, i64]
         L.litevggt_cross_attn.argtypes = [XP, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
@@ -325,8 +350,8 @@ def litevggt_global_block(p: Params, n_tokens: int, z, weights: BlockWeights, de
 @dataclass
 class CacheBuffers:
     """Device tensors of a cache (owned by the caller).  ``k``, ``v``: [n_pages, kv_heads, page_tokens, head_dim]
-    bf16 or uint8 codes; ``k_scale``, ``v_scale``: uint8 [n_pages, kv_heads, page_tokens] (None for a bf16
-    cache); ``page_table``: int32 [n_seq, max_pages], -1 where no page is held.  All contiguous; a pool may have
+    bf16 or uint8 codes (E2M1: [.., head_dim // 2], two codes a byte); ``k_scale``, ``v_scale``: uint8 [n_pages, kv_heads, page_tokens]
+    (E2M1: [.., head_dim // 32]; None for a bf16 cache); ``page_table``: int32 [n_seq, max_pages], -1 where no page is held.  All contiguous; a pool may have
     more pages, a table more sequences than the parameters of a call say."""
     k: "object"
     v: "object"
@@ -342,6 +367,11 @@ class CacheBuffers:
             u8 = _uint8()
             return Cache(_buffer(self.k, u8, (n, h, g, d), "k of the cache"), _buffer(self.v, u8, (n, h, g, d), "v of the cache"),
                          _buffer(self.k_scale, u8, (n, h, g), "k_scale"), _buffer(self.v_scale, u8, (n, h, g), "v_scale"), table)
+        if p.cache_dtype == CACHE_E2M1:
+            u8 = _uint8()
+            return Cache(_buffer(self.k, u8, (n, h, g, d // 2), "k of the cache", False), _buffer(self.v, u8, (n, h, g, d // 2), "v of the cache", False),
+                         _buffer(self.k_scale, u8, (n, h, g, d // 32), "k_scale", False), _buffer(self.v_scale, u8, (n, h, g, d // 32), "v_scale", False),
+                         table)
         bf16 = _bf16()
         return Cache(_buffer(self.k, bf16, (n, h, g, d), "k of the cache"), _buffer(self.v, bf16, (n, h, g, d), "v of the cache"), None, None, table)
 
@@ -349,16 +379,16 @@ class CacheBuffers:
         """Whether what a call with these parameters reads and writes is on that device"""
         k, v, table = self.k, self.v, self.page_table
         return (k is None or k.get_device() == here) and (v is None or v.get_device() == here) and (table is None or table.get_device() == here) and (
-            p.cache_dtype != CACHE_E4M3 or all(t is None or t.get_device() == here for t in (self.k_scale, self.v_scale)))
+            p.cache_dtype == CACHE_BF16 or all(t is None or t.get_device() == here for t in (self.k_scale, self.v_scale)))
 
 
-def _buffer(t, kind, shape, what: str):
+def _buffer(t, kind, shape, what: str, or_e4m3: bool = True):
     """Pointer of a contiguous tensor of `shape`, or longer in its first dimension, or of as many values in a row."""
     if t is None:      # (the call says so)
         return None
     if t.dtype is kind and t.is_contiguous() and t.shape == shape:
         return t.data_ptr()
-    codes = kind is _uint8() and str(t.dtype) == "torch.float8_e4m3fn"
+    codes = or_e4m3 and kind is _uint8() and str(t.dtype) == "torch.float8_e4m3fn"
     if not (t.dtype is kind or codes) or not t.is_contiguous() or not (
             t.shape[1:] == shape[1:] and t.shape[0] >= shape[0] if t.dim() > 1 else t.numel() >= math.prod(shape)):
         raise LiteVGGTError(f"{what}: {' x '.join(str(n) for n in shape)} contiguous values of {kind} wanted, got "
@@ -382,9 +412,10 @@ def alloc_cache(p: CacheParams, device="cuda") -> CacheBuffers:
     """An empty cache: no sequence holds a page.  (Pages need not be cleared before they are handed out.)"""
     import torch
     shape = (p.n_pages, p.kv_heads, p.page_tokens)
-    e4m3 = p.cache_dtype == CACHE_E4M3
-    rows = [torch.empty(*shape, p.head_dim, dtype=torch.uint8 if e4m3 else torch.bfloat16, device=device) for _ in range(2)]
-    scales = [torch.empty(shape, dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2)]
+    coded, e2m1 = p.cache_dtype != CACHE_BF16, p.cache_dtype == CACHE_E2M1
+    rows = [torch.empty(*shape, p.head_dim // 2 if e2m1 else p.head_dim, dtype=torch.uint8 if coded else torch.bfloat16, device=device)
+            for _ in range(2)]
+    scales = [torch.empty(shape + ((p.head_dim // 32,) if e2m1 else ()), dtype=torch.uint8, device=device) if coded else None for _ in range(2)]
     return CacheBuffers(*rows, *scales, torch.full((p.n_seq, p.max_pages), -1, dtype=torch.int32, device=device))
 
 
@@ -396,9 +427,9 @@ def _rows(t, heads: int, head_dim: int, what: str):
         return 0, None, width
     shape, stride = t.shape, t.stride()
     if len(shape) == 3:
-        ok = shape[1] == heads and shape[2] == head_dim and stride[2] == 1 and (stride[1] == head_dim or heads == 1)
+        ok = shape[1] == heads and shape[2] == head_dim and (shape[0] == 0 or (stride[2] == 1 and (stride[1] == head_dim or heads == 1)))
     else:
-        ok = len(shape) == 2 and shape[1] == width and stride[1] == 1
+        ok = len(shape) == 2 and shape[1] == width and (shape[0] == 0 or stride[1] == 1)
     if not ok or t.dtype is not _bf16():
         raise LiteVGGTError(f"{what}: bf16 rows of {heads} x {head_dim} contiguous values wanted, got "
                             f"{tuple(shape)} {t.dtype} with strides {stride}")
@@ -424,6 +455,12 @@ def _bf16():
 def _int32():
     import torch
     return torch.int32
+
+
+@functools.lru_cache(maxsize=None)
+def _float32():
+    import torch
+    return torch.float32
 
 
 @functools.lru_cache(maxsize=None)
@@ -465,6 +502,70 @@ def litevggt_cached_attn(p: CacheParams, cache: CacheBuffers, q, new_off, kv_len
     wp, wn = _ws_args(ws)
     _check(lib().litevggt_cached_attn(C.byref(p), C.byref(c), n, qp, qs, np_, lp, op, os_, wp, wn,
                                       _stream_of(p, cache, q, o, new_off, kv_len, ws)), "litevggt_cached_attn")
+
+
+def alloc_mass(p: CacheParams, device="cuda"):
+    """Masses of a cache whose positions have drawn nothing yet."""
+    import torch
+    return torch.zeros(p.n_seq, p.kv_heads, p.max_pages * p.page_tokens, dtype=torch.float32, device=device)
+
+
+def _masses(t, p: CacheParams, what: str):
+    """Pointer of masses [n_seq, kv_heads, max_pages * page_tokens], or of more sequences."""
+    if t is None:
+        return None
+    shape = (p.n_seq, p.kv_heads, p.max_pages * p.page_tokens)
+    if t.dtype is not _float32() or not t.is_contiguous() or t.dim() != 3 or t.shape[1:] != shape[1:] or t.shape[0] < shape[0]:
+        raise LiteVGGTError(f"{what}: {' x '.join(str(n) for n in shape)} contiguous fp32 values wanted, got {tuple(t.shape)} {t.dtype} "
+                            f"with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def litevggt_cached_mass_ws_bytes(p: CacheParams, n_tokens: int) -> int:
+    return int(lib().litevggt_cached_mass_ws_bytes(C.byref(p), n_tokens))
+
+
+def litevggt_cached_mass(p: CacheParams, cache: CacheBuffers, q, new_off, kv_len, mass_in, mass, ws) -> None:
+    """``mass_in``: None, or the same tensor as ``mass``, or another.  ``cache.v`` and ``cache.v_scale`` may be None."""
+    n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
+    np_, lp = _ints(new_off, p.n_seq + 1, "new_off"), _ints(kv_len, p.n_seq, "kv_len")
+    ip, mp = _masses(mass_in, p, "mass_in"), _masses(mass, p, "mass")
+    c = cache.struct(p)
+    wp, wn = _ws_args(ws)
+    _check(lib().litevggt_cached_mass(C.byref(p), C.byref(c), n, qp, qs, np_, lp, ip, mp, wp, wn,
+                                      _stream_of(p, cache, q, new_off, kv_len, mass_in, mass, ws)), "litevggt_cached_mass")
+
+
+def litevggt_cache_evict_ws_bytes(p: CacheParams) -> int:
+    return int(lib().litevggt_cache_evict_ws_bytes(C.byref(p)))
+
+
+def litevggt_cache_evict(p: CacheParams, page_table, kv_len, mass, keep, first_pages: int, last_pages: int, table_out, freed, n_freed, ws) -> None:
+    """``table_out`` may be ``page_table`` itself."""
+    shape = (p.n_seq, p.max_pages)
+    tp, op, fp = (_buffer(t, _int32(), shape, what) for t, what in ((page_table, "page_table"), (table_out, "table_out"), (freed, "freed")))
+    lp, kp, np_ = _ints(kv_len, p.n_seq, "kv_len"), _ints(keep, p.n_seq, "keep"), _ints(n_freed, p.n_seq, "n_freed")
+    mp = _masses(mass, p, "mass")
+    wp, wn = _ws_args(ws)
+    _check(lib().litevggt_cache_evict(C.byref(p), tp, lp, mp, kp, first_pages, last_pages, op, fp, np_, wp, wn,
+                                      _stream_of(p, None, page_table, kv_len, mass, keep, table_out, freed, n_freed, ws)), "litevggt_cache_evict")
+
+
+def litevggt_rope(p: RopeParams, pos, q, k, q_out, k_out) -> None:
+    """``k``, ``k_out``: None with ``kv_heads=0``.  An output may be its input."""
+    n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
+    m, op, os_ = _rows(q_out, p.heads, p.head_dim, "q_out")
+    _same(n, m, "q and q_out")
+    kp = kop = None
+    ks = kos = 0
+    if p.kv_heads > 0:
+        m, kp, ks = _rows(k, p.kv_heads, p.head_dim, "k")
+        _same(n, m, "q and k")
+        m, kop, kos = _rows(k_out, p.kv_heads, p.head_dim, "k_out")
+        _same(n, m, "k and k_out")
+    pp = _ints(pos, n * p.axes, "pos")
+    _check(lib().litevggt_rope(C.byref(p), n, pp, qp, qs, kp, ks, op, os_, kop, kos, _stream_of(p, None, pos, q, q_out, *((k, k_out) if p.kv_heads else ()))),
+           "litevggt_rope")
 
 
 def litevggt_cross_attn_ws_bytes(p: CrossParams, n_q: int, n_kv: int) -> int:

@@ -129,7 +129,7 @@ int check_cache(const litevggt_cache_params *p, CacheView *cv) {
   if (!p) return LV_ERR_NULL;
   const int rc = check_heads(p->n_seq, p->heads, p->kv_heads, p->head_dim, p->softmax_scale);
   if (rc) return rc;
-  if (p->cache_dtype != LV_CACHE_BF16 && p->cache_dtype != LV_CACHE_E4M3) return LV_ERR_DTYPE;
+  if (p->cache_dtype != LV_CACHE_BF16 && p->cache_dtype != LV_CACHE_E4M3 && p->cache_dtype != LV_CACHE_E2M1) return LV_ERR_DTYPE;
   int shift = 4;
   while (shift < 10 && (1 << shift) < p->page_tokens) ++shift;
   if ((1 << shift) != p->page_tokens || p->n_pages < 1 || p->max_pages < 1) return LV_ERR_SHAPE;
@@ -141,13 +141,13 @@ int check_cache(const litevggt_cache_params *p, CacheView *cv) {
   cv->page_shift = shift;
   cv->n_pages = p->n_pages;
   cv->max_pages = p->max_pages;
-  cv->e4m3 = p->cache_dtype == LV_CACHE_E4M3;
+  cv->dtype = p->cache_dtype;
   cv->table = nullptr;
   return LV_OK;
 }
 int check_cache_buffers(const litevggt_cache *c, CacheView *cv) {
   if (!c || !c->k || !c->v || !c->page_table) return LV_ERR_NULL;
-  if (cv->e4m3 && (!c->k_scale || !c->v_scale)) return LV_ERR_NULL;
+  if (cv->dtype != LV_CACHE_BF16 && (!c->k_scale || !c->v_scale)) return LV_ERR_NULL;
   if (((uintptr_t)c->k | (uintptr_t)c->v) & 15u) return LV_ERR_SHAPE;
   cv->table = c->page_table;
   return LV_OK;
@@ -466,7 +466,7 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
 size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
   CacheView cv;
   if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
-  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.e4m3, (int64_t)p->max_pages << cv.page_shift);
+  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.dtype != LV_CACHE_BF16, (int64_t)p->max_pages << cv.page_shift);
 }
 
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
@@ -555,6 +555,102 @@ int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void 
   a.k_end = kv_end;
   a.n_kv = (int)n_kv;
   return launch_kv_attn(a, ws, st);
+}
+
+int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t *pos, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream) {
+  if (!p) return LV_ERR_NULL;
+  if (p->heads < 1 || p->heads > 1024 || p->kv_heads < 0 || p->kv_heads > 1024) return LV_ERR_SHAPE;
+  if (p->head_dim != 64 && p->head_dim != 128) return LV_ERR_SHAPE;
+  if (p->axes < 1 || p->axes > 4) return LV_ERR_SHAPE;
+  if (p->pairing != LV_ROPE_AXIS_HALVES && p->pairing != LV_ROPE_HEAD_HALVES && p->pairing != LV_ROPE_ADJACENT) return LV_ERR_PARAM;
+  RopePairs r = {};
+  r.axes = p->axes;
+  r.pairing = p->pairing;
+  for (int a = 0; a < p->axes; ++a) {
+    if (p->pairs[a] < 1 || p->pairs[a] > p->head_dim / 2) return LV_ERR_SHAPE;
+    r.first[a + 1] = r.first[a] + p->pairs[a];
+  }
+  if (2 * r.first[p->axes] > p->head_dim) return LV_ERR_SHAPE;
+  constexpr double kTurn = 0.15915494309189533577;      // 1 / 2 pi
+  if (p->freq) {
+    for (int i = 0; i < r.first[p->axes]; ++i) {
+      if (!(fabs(p->freq[i]) <= 1e6)) return LV_ERR_PARAM;
+      r.turns[i] = p->freq[i] * kTurn;
+    }
+  } else {
+    if (!(p->base > 0.f) || !isfinite(p->base)) return LV_ERR_PARAM;
+    // an axis' frequencies fall by the same factor: one exponential each, then products (64 of them: off by 64 roundings of 2^-64)
+    for (int a = 0; a < p->axes; ++a) {
+      const int of = p->joint ? r.first[p->axes] : p->pairs[a];
+      const long double step = expl(-logl((long double)p->base) / of);
+      long double f = a == 0 || !p->joint ? 1.0L : powl(step, r.first[a]);
+      for (int i = r.first[a]; i < r.first[a + 1]; ++i, f *= step) r.turns[i] = (double)(f * (long double)kTurn);
+    }
+  }
+  if (n_tokens > 0 && (!pos || !q || !q_out || (p->kv_heads > 0 && (!k || !k_out)))) return LV_ERR_NULL;
+  if (!count_ok(n_tokens, p->heads + p->kv_heads)) return LV_ERR_SHAPE;
+  if (n_tokens == 0) return LV_OK;
+  const int64_t width = (int64_t)p->heads * p->head_dim, kw = (int64_t)p->kv_heads * p->head_dim;
+  if (!rows_ok(q, q_stride, n_tokens, width) || !rows_ok(q_out, q_out_stride, n_tokens, width)) return LV_ERR_SHAPE;
+  if (p->kv_heads > 0 && (!rows_ok(k, k_stride, n_tokens, kw) || !rows_ok(k_out, k_out_stride, n_tokens, kw))) return LV_ERR_SHAPE;
+  return launch_rope(r, pos, (int)n_tokens, p->heads, p->kv_heads, p->head_dim, p->inverse != 0, (const uint16_t *)q, q_stride,
+                     (const uint16_t *)k, k_stride, (uint16_t *)q_out, q_out_stride, (uint16_t *)k_out, k_out_stride, (hipStream_t)stream);
+}
+
+size_t litevggt_cached_mass_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
+  CacheView cv;
+  if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
+  return mass_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, (int64_t)p->max_pages << cv.page_shift);
+}
+
+int litevggt_cached_mass(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens, const void *q, int64_t q_stride,
+                         const int32_t *new_off, const int32_t *kv_len, const float *mass_in, float *mass, void *ws, size_t ws_bytes,
+                         void *stream) {
+  MassArgs a = {};
+  int rc = check_cache(p, &a.cv);
+  if (rc) return rc;
+  if (!cache || !cache->k || !cache->page_table || (a.cv.dtype != LV_CACHE_BF16 && !cache->k_scale)) return LV_ERR_NULL;
+  if (!new_off || !kv_len || !mass || (n_tokens > 0 && !q)) return LV_ERR_NULL;
+  if (((uintptr_t)cache->k & 15u) || ((uintptr_t)mass & 15u) || ((uintptr_t)mass_in & 15u)) return LV_ERR_SHAPE;
+  if (!count_ok(n_tokens, p->heads)) return LV_ERR_SHAPE;
+  if (n_tokens > 0 && !rows_ok(q, q_stride, n_tokens, (int64_t)p->heads * p->head_dim)) return LV_ERR_SHAPE;
+  if (!ws_ok(ws, ws_bytes, litevggt_cached_mass_ws_bytes(p, n_tokens))) return LV_ERR_WORKSPACE;
+  a.q = (const uint16_t *)q;
+  a.q_stride = q_stride;
+  a.q_off = new_off;
+  a.kv_len = kv_len;
+  a.n_q = (int)n_tokens;
+  a.heads = p->heads;
+  a.scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
+  a.qk_norm = n_tokens > 0 && p->qk_norm;
+  a.frame = p->frame_tokens;
+  a.k = cache->k;
+  a.k_scale = cache->k_scale;
+  a.cv.table = cache->page_table;
+  a.mass_in = mass_in;
+  a.mass = mass;
+  return launch_mass(a, ws, (hipStream_t)stream);
+}
+
+size_t litevggt_cache_evict_ws_bytes(const litevggt_cache_params *p) {
+  CacheView cv;
+  return check_cache(p, &cv) ? 0 : evict_ws_bytes(p->n_seq, cv.page_shift, p->max_pages);
+}
+
+int litevggt_cache_evict(const litevggt_cache_params *p, const int32_t *page_table, const int32_t *kv_len, const float *mass,
+                         const int32_t *keep, int first_pages, int last_pages, int32_t *table_out, int32_t *freed, int32_t *n_freed,
+                         void *ws, size_t ws_bytes, void *stream) {
+  CacheView cv;
+  const int rc = check_cache(p, &cv);
+  if (rc) return rc;
+  if (!page_table || !kv_len || !mass || !keep || !table_out || !freed || !n_freed) return LV_ERR_NULL;
+  if (freed == table_out || freed == page_table || ((uintptr_t)mass & 15u)) return LV_ERR_SHAPE;
+  if (first_pages < 0 || last_pages < 0) return LV_ERR_PARAM;
+  if (!ws_ok(ws, ws_bytes, litevggt_cache_evict_ws_bytes(p))) return LV_ERR_WORKSPACE;
+  EvictArgs a = {p->n_seq, p->kv_heads, cv.page_shift, p->n_pages, p->max_pages, page_table, kv_len, keep, mass, first_pages, last_pages,
+                 table_out, freed, n_freed};
+  return launch_evict(a, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"

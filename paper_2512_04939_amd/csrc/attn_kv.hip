@@ -44,7 +44,9 @@ constexpr int kRounds = 3;               // a call's pieces fill the chip's slot
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-enum class Kv { ROWS, PAGES, E4M3 };
+enum class Kv { ROWS, PAGES, E4M3, E2M1 };
+template <Kv KV> constexpr bool kCoded = KV == Kv::E4M3 || KV == Kv::E2M1;                // codes that become bf16 on their way into LDS
+template <Kv KV, int D> constexpr int kRowBytes = KV == Kv::E2M1 ? D / 2 : KV == Kv::E4M3 ? D : 2 * D;
 
 // What a kernel needs of the call, by value
 struct Call {
@@ -410,7 +412,7 @@ struct Group {
 
 template <Kv KV, int D>
 __device__ __forceinline__ Group group_at(const Call &a, int head, int k0, int key, int end, int page) {
-  constexpr int row_bytes = KV == Kv::E4M3 ? D : 2 * D;
+  constexpr int row_bytes = kRowBytes<KV, D>;
   const int rows = min(scalar(max(end - key, 0)), kGrp);     // (in one they become a vector instruction, and all that hangs on it)
   Group g;
   if constexpr (KV == Kv::ROWS) {
@@ -472,7 +474,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_rsrc(const void *p, int
 }
 
 // E4M3: a group's codes and exponents (of K or of V) in registers, then as bf16 in LDS.  D = 64: one load of a wave has all 16 rows.
-template <int D>
+template <Kv KV, int D>
 struct Codes {
   static constexpr int kLoads = D / 64, kPer = D / 16, kRows = 64 / kPer;   // loads; 16-byte pieces of a row, rows of a load
   u32x4 c[kLoads];
@@ -494,6 +496,34 @@ struct Codes {
       *(u32x4 *)(lds + row * T::kRow + ((p ^ x) * 16)) = dequant8(u32x2{c[j].x, c[j].y}, f);
       *(u32x4 *)(lds + row * T::kRow + (((p + 1) ^ x) * 16)) = dequant8(u32x2{c[j].z, c[j].w}, f);
     }
+  }
+};
+
+// E2M1: four lanes to a row, all 16 rows in one load.  A lane has 16 (64 channels) or 32 consecutive channels, which share a scale.
+template <int D>
+struct Codes<Kv::E2M1, D> {
+  static constexpr int kWords = D / 32;     // of codes; 16-byte pieces of bf16 that they become
+  uint32_t c[kWords];
+  uint32_t e;
+  __device__ __forceinline__ void load(const char *codes, const uint8_t *scales, const Group &g, int lane) {
+    const __amdgpu_buffer_rsrc_t rc = scalar_rsrc(codes, g.k_bytes), rs = scalar_rsrc(scales + g.row * (D / 32), g.k_bytes / 16);
+    if constexpr (D == 64) {
+      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rc, lane * 8, 0, 0));
+      c[0] = w.x;
+      c[1] = w.y;
+    } else {
+      const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rc, lane * 16, 0, 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = w[i];
+    }
+    e = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, D == 64 ? lane / 2 : lane, 0, 0);
+  }
+  __device__ __forceinline__ void store(char *lds, bool of_v, int lane) const {
+    using T = Tile<D>;
+    const int row = lane / 4, p = kWords * (lane % 4), x = of_v ? T::v_xor(row) : T::k_xor(row);
+    const float f = __uint_as_float(e << 23);
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) *(u32x4 *)(lds + row * T::kRow + (((p + i) ^ x) * 16)) = dequant8(c[i], f);
   }
 };
 
@@ -695,7 +725,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   using T = Tile<D>;
   constexpr int kRows = 32 * QB;
   constexpr int kTile = 32 * T::kRow;          // bytes of a tile's K or V
-  constexpr int kStages = KV == Kv::E4M3 ? 1 : 2;
+  constexpr int kStages = kCoded<KV> ? 1 : 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work w;
   SeqInfo s;
@@ -709,7 +739,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   char *const mine = lds + wave * (2 * kStages * kTile);
   const uint32_t mine_at = __builtin_amdgcn_readfirstlane(lds_addr(mine));
   Offsets<D> ko, vo;
-  if constexpr (KV != Kv::E4M3) {
+  if constexpr (!kCoded<KV>) {
     ko.init(lane, KV == Kv::ROWS ? a.k_stride : T::kRow, false);
     vo.init(lane, KV == Kv::ROWS ? a.v_stride : T::kRow, true);
   }
@@ -723,14 +753,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       holes = __builtin_amdgcn_ballot_w64((key < (uint32_t)end && ids[0] < 0) || (key + kGrp < (uint32_t)end && ids[1] < 0));
     }
   };
-  Codes<D> kc[2], vc[2];
+  Codes<KV, D> kc[2], vc[2];
   auto fetch = [&](int i) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int key = begin + i * 128 + g * kGrp;
       const int page = KV == Kv::ROWS ? 0 : __builtin_amdgcn_readlane(ids[g], i & 63);
       const Group at = group_at<KV, D>(a, w.head, s.k0, key, i < n ? end : 0, page);
-      if constexpr (KV == Kv::E4M3) {
+      if constexpr (kCoded<KV>) {
         kc[g].load(at.k, a.k_scale, at, lane);
         vc[g].load(at.v, a.v_scale, at, lane);
       } else {
@@ -753,7 +783,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       int shut = 0;
       if (KV != Kv::ROWS && (shut_now >> (i & 63) & 1))
         shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
-      if constexpr (KV == Kv::E4M3) {
+      if constexpr (kCoded<KV>) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           kc[g].store(kt + g * kGrp * T::kRow, false, lane);
@@ -763,8 +793,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       if (i + 1 < n) {
         if ((i + 1) % 64 == 0) look_up(i + 1);
         fetch(i + 1);
-        if constexpr (KV != Kv::E4M3) wait_vm<4 * T::kFetches>();
-      } else if constexpr (KV != Kv::E4M3) {
+        if constexpr (!kCoded<KV>) wait_vm<4 * T::kFetches>();
+      } else if constexpr (!kCoded<KV>) {
         wait_vm<0>();
       }
       const int key0 = begin + i * 128;
@@ -855,7 +885,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   using T = Tile<D>;
   constexpr int QB = Many<D>::QB, kWaves = Many<D>::kWaves, kRows = Many<D>::kRows;
   constexpr int kHalf = 64 * T::kRow;                     // bytes of a stage's K or V
-  constexpr int kStages = KV == Kv::E4M3 ? 3 : 4;
+  constexpr int kStages = kCoded<KV> ? 3 : 4;
   constexpr int kFetch = (kWaves == 4 ? 2 : 1) * T::kFetches;     // fetches of a wave and stage
   constexpr int KF = D / 16, DT = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -872,7 +902,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   const int group = kWaves == 4 ? wave : wave >> 1;
   const bool only_v = kWaves == 8 && (wave & 1);
   Offsets<D> off, off_v;
-  if constexpr (KV != Kv::E4M3) {
+  if constexpr (!kCoded<KV>) {
     off.init(lane, KV != Kv::ROWS ? T::kRow : only_v ? a.v_stride : a.k_stride, only_v);
     if constexpr (kWaves == 4) off_v.init(lane, KV != Kv::ROWS ? T::kRow : a.v_stride, true);
   }
@@ -923,7 +953,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
       plain = i + (ragged ? __ffsll((unsigned long long)ragged) - 1 : 64);
     }
   };
-  Codes<D> codes, codes_v;
+  Codes<KV, D> codes, codes_v;
   // Rows: what the next fetch brings, and the rows that are left of it on
   const int64_t row_first = (int64_t)s.k0 + begin + group * kGrp;
   const char *next_k = a.k + row_first * a.k_stride + w.head * T::kRow, *next_v = a.v + row_first * a.v_stride + w.head * T::kRow;
@@ -946,12 +976,12 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
       next_v += step_v;
       left -= 64;
     } else {
-      constexpr int kBytes = KV == Kv::E4M3 ? D : 2 * D;
+      constexpr int kBytes = kRowBytes<KV, D>;
       const uint32_t lo = __builtin_amdgcn_readlane(own, i - from), hi = __builtin_amdgcn_readlane(own_hi, i - from);
       Group at;
       at.row = (int64_t)((uint64_t)(hi & 0xffffffu) << 32 | lo);
       at.k_bytes = at.v_bytes = (int)(hi >> 24) * kBytes;
-      if constexpr (KV == Kv::E4M3) {
+      if constexpr (kCoded<KV>) {
         codes.load((only_v ? a.v : a.k) + at.row * kBytes, only_v ? a.v_scale : a.k_scale, at, lane);
         if constexpr (kWaves == 4) codes_v.load(a.v + at.row * kBytes, a.v_scale, at, lane);
       } else {
@@ -959,7 +989,7 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
         if constexpr (kWaves == 4) fetch_group<D>(a.v + at.row * kBytes, at.k_bytes, off_v, ring + kHalf);
       }
     }
-    if constexpr (KV != Kv::E4M3) ring = ring == base + (kStages - 1) * (2 * kHalf) ? base : ring + 2 * kHalf;
+    if constexpr (!kCoded<KV>) ring = ring == base + (kStages - 1) * (2 * kHalf) ? base : ring + 2 * kHalf;
   };
   auto put = [&](int i) __attribute__((always_inline)) {
     char *p = lds + ((uint32_t)i % kStages) * (2 * kHalf) + to;
@@ -969,16 +999,16 @@ __global__ __launch_bounds__(64 * Many<D>::kWaves) __attribute__((amdgpu_waves_p
   // this wave's part of stage i + 1 has landed; behind the barrier all of it, and nobody reads stage i - 1 any more
   auto publish = [&](int i) __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KV != Kv::E4M3) wait_vm<(kStages - 3) * kFetch>();
+    if constexpr (!kCoded<KV>) wait_vm<(kStages - 3) * kFetch>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KV == Kv::E4M3) put(i + 2);
+    if constexpr (kCoded<KV>) put(i + 2);
     fetch(i + 3);
   };
   auto start = [&]() __attribute__((always_inline)) {
     fetch(0);
-    if constexpr (KV == Kv::E4M3) {
+    if constexpr (kCoded<KV>) {
       put(0);
       fetch(1);
       put(1);
@@ -1445,14 +1475,14 @@ struct Form {
 // keys 29 us in blocks of 32 rows, 41 in those of 256; 48 rows 31 us in blocks of 64, 46 of 32, 41 of 256 (over 2000 keys 12.6, 12.1, 17);
 // 100 rows 51 of 64, 84 of 32, 49 of 256.  128 channels, 8 sequences over 4000 keys: 24 rows 54 us in blocks of 32, 61 of 256; 48 rows 90 and 63
 // (64 do not fit the registers).
-Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
+Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys) {
   Form f;
   const int group = heads / kv_heads;
   const double rows = (double)n_q * group / n_seq;
   f.few = rows <= (head_dim == 64 ? 64.0 : 32.0);
   f.rows = f.few ? (rows <= 32.0 ? 32 : 64) : 256;
   f.tile = f.few ? 128 : 64;
-  f.resident = kCus * (head_dim == 64 || (f.few && e4m3) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
+  f.resident = kCus * (head_dim == 64 || (f.few && coded) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (Blocks of several sequences that fill the chip four times over are not cut: 32 x 2000 queries over 4000 keys, 16 heads of 64
@@ -1469,14 +1499,14 @@ size_t plan_bytes(int n_seq) { return 256 + (n_seq > 64 ? 2 * align_up((size_t)n
 
 }  // namespace
 
-size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys) {
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys) {
   // What the call needs grows with n_q inside a form only.  The size is the largest up to n_q, so that scratch for a
   // longer call serves the shorter ones.
   const int group = heads / kv_heads;
   const int64_t cut = (4 * kCus * (head_dim == 64 ? 2 : 1) - 1) / kv_heads - n_seq;     // most blocks of many rows that are cut (form_of)
   size_t most = 0;
   for (int64_t n : {(int64_t)n_q, (int64_t)32 * n_seq / group, (int64_t)64 * n_seq / group, (256 * cut + 255) / group})
-    if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, e4m3, most_keys), head_dim));
+    if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, coded, most_keys), head_dim));
   return most || n_seq > 64 ? plan_bytes(n_seq) + most : 0;
 }
 
@@ -1498,17 +1528,17 @@ static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t 
   constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
   static std::atomic<uint64_t> d0{0}, d1{0}, d2{0};
   // (the ring of four waves' tiles, and room for their sums at the end)
-  constexpr size_t ring = KV == Kv::E4M3 ? 2 * tile : 4 * tile, sums = 4 * 32 * D * sizeof(float);
+  constexpr size_t ring = kCoded<KV> ? 2 * tile : 4 * tile, sums = 4 * 32 * D * sizeof(float);
   if (f.few && f.rows == 32) return go(k_kv_attn_few<KV, D, 1>, d0, std::integral_constant<size_t, std::max(ring, sums)>{}, c, grid, 256, st);
   if constexpr (D == 64)
     if (f.few) return go(k_kv_attn_few<KV, D, 2>, d1, std::integral_constant<size_t, std::max(ring, 2 * sums)>{}, c, grid, 256, st);
-  return go(k_kv_attn_many<KV, D>, d2, std::integral_constant<size_t, KV == Kv::E4M3 ? 3 * tile : 4 * tile>{}, c, grid,
+  return go(k_kv_attn_many<KV, D>, d2, std::integral_constant<size_t, kCoded<KV> ? 3 * tile : 4 * tile>{}, c, grid,
             64 * Many<D>::kWaves, st);
 }
 
 int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   const int64_t most = x.paged ? (int64_t)x.cv.max_pages << x.cv.page_shift : x.n_kv;
-  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, x.paged && x.cv.e4m3, most);
+  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, x.paged && x.cv.dtype != LV_CACHE_BF16, most);
   Call c;
   c.q = x.q;
   c.o = x.o;
@@ -1557,8 +1587,9 @@ int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   if (c.starts) k_kv_attn_plan<<<dim3(1), 1024, 0, st>>>(c);
   int rc;
   if (!x.paged) rc = by_kv(std::integral_constant<Kv, Kv::ROWS>{});
-  else if (!x.cv.e4m3) rc = by_kv(std::integral_constant<Kv, Kv::PAGES>{});
-  else rc = by_kv(std::integral_constant<Kv, Kv::E4M3>{});
+  else if (x.cv.dtype == LV_CACHE_BF16) rc = by_kv(std::integral_constant<Kv, Kv::PAGES>{});
+  else if (x.cv.dtype == LV_CACHE_E4M3) rc = by_kv(std::integral_constant<Kv, Kv::E4M3>{});
+  else rc = by_kv(std::integral_constant<Kv, Kv::E2M1>{});
   if (rc) return rc;
   if (f.target) {
     auto join = [&](auto kernel, int rows) {

@@ -33,11 +33,11 @@ __device__ __forceinline__ int page_of(const CacheView &cv, int seq, int64_t pos
   return (uint32_t)id < (uint32_t)cv.n_pages ? id : -1;
 }
 
-template <int LANES>   // largest over the 8 or 16 lanes of a row
+template <int LANES>   // largest over the 4 lanes of a block, the 8 or 16 of a row
 __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, dpp_take<0xB1, 0xF>(v));    // quad_perm [1,0,3,2]
   v = fmaxf(v, dpp_take<0x4E, 0xF>(v));    // quad_perm [2,3,0,1]
-  v = fmaxf(v, dpp_take<0x141, 0xF>(v));   // row_half_mirror
+  if (LANES >= 8) v = fmaxf(v, dpp_take<0x141, 0xF>(v));   // row_half_mirror
   if (LANES == 16) v = fmaxf(v, dpp_take<0x140, 0xF>(v));   // row_mirror
   return v;
 }
@@ -77,12 +77,31 @@ __device__ __forceinline__ u32x2 quant_row8(const u32x4 w, uint32_t &exp_byte) {
   return u32x2{cvt4_fp8(x[0], x[1], x[2], x[3]), cvt4_fp8(x[4], x[5], x[6], x[7])};
 }
 
+// Eight channels of a row as E2M1 codes, and the exponent byte of the 32 channels that they are a quarter of: the smallest power of two
+// that brings the largest finite |value| to 6 or less (6 = 1.5 * 2^2).  E2M1 has no NaN: a byte of 255 makes all 32 NaN, and one among
+// them sets it.
+__device__ __forceinline__ uint32_t quant_block8(const u32x4 w, uint32_t &exp_byte) {
+  float x[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float m = fabsf(x[i]);
+    a = fmaxf(a, m < INFINITY ? m : m != m ? INFINITY : 0.f);
+  }
+  a = row_max<4>(a);
+  const uint32_t bits = __float_as_uint(a);
+  int e = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0);
+  e = bits == 0u ? 127 : max(e, 1);
+  exp_byte = a < INFINITY ? (uint32_t)e : 255u;
+  return a < INFINITY ? cvt8_fp4(x, __uint_as_float((uint32_t)e << 23)) : 0u;
+}
+
 }  // namespace
 
 // A wave takes eight (64 channels) or four (128) consecutive tokens of one head, 16 bytes of K and of V per lane: what it
 // writes is one piece of a page, what it reads are whole 128-byte lines.  Waves of neighbouring heads stand side by side, so
 // a workgroup reads longer pieces of the tokens' rows.
-template <int D, bool E4M3>
+template <int D, int DTYPE>
 __global__ __launch_bounds__(256) void k_cache_write(CacheView cv, char *kp, char *vp, uint8_t *ksc, uint8_t *vsc,
                                                      const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
                                                      const int32_t *off, const int32_t *pos0, int n, int64_t units, int qk_norm) {
@@ -118,7 +137,19 @@ __global__ __launch_bounds__(256) void k_cache_write(CacheView cv, char *kp, cha
     const float r = 1.0f / sqrtf(row_sum<L>(sumsq8(wk)) * (1.0f / D) + kQkEps);
     wk = scale8(wk, r);
   }
-  if constexpr (E4M3) {
+  if constexpr (DTYPE == LV_CACHE_E2M1) {
+    uint32_t ek, ev;
+    const uint32_t ck = quant_block8(wk, ek), cw = quant_block8(wv, ev);
+    if (tok < n && id >= 0) {
+      const int64_t row = row_of(cv, id, head, (int)(pos & ((1 << cv.page_shift) - 1)));
+      *(uint32_t *)(kp + row * (D / 2) + (lane % L) * 4) = ck;
+      *(uint32_t *)(vp + row * (D / 2) + (lane % L) * 4) = cw;
+      if (lane % 4 == 0) {
+        ksc[row * (D / 32) + lane % L / 4] = (uint8_t)ek;
+        vsc[row * (D / 32) + lane % L / 4] = (uint8_t)ev;
+      }
+    }
+  } else if constexpr (DTYPE == LV_CACHE_E4M3) {
     uint32_t ek, ev;
     const u32x2 ck = quant_row8<L>(wk, ek), cw = quant_row8<L>(wv, ev);
     if (tok < n && id >= 0) {
@@ -138,7 +169,7 @@ __global__ __launch_bounds__(256) void k_cache_write(CacheView cv, char *kp, cha
 }
 
 // The reverse; positions that are not held read as zeros.
-template <int D, bool E4M3>
+template <int D, int DTYPE>
 __global__ __launch_bounds__(256) void k_cache_read(CacheView cv, const char *kp, const char *vp, const uint8_t *ksc,
                                                     const uint8_t *vsc, const int32_t *first, const int32_t *off, uint16_t *k,
                                                     int64_t k_stride, uint16_t *v, int64_t v_stride, int n, int64_t units) {
@@ -170,7 +201,11 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheView cv, const char *kp
   u32x4 wk = {0, 0, 0, 0}, wv = {0, 0, 0, 0};
   if (id >= 0) {
     const int64_t row = row_of(cv, id, head, (int)(pos & ((1 << cv.page_shift) - 1)));
-    if constexpr (E4M3) {
+    if constexpr (DTYPE == LV_CACHE_E2M1) {
+      const uint32_t ck = *(const uint32_t *)(kp + row * (D / 2) + (lane % L) * 4), cw = *(const uint32_t *)(vp + row * (D / 2) + (lane % L) * 4);
+      wk = dequant8(ck, __uint_as_float((uint32_t)ksc[row * (D / 32) + lane % L / 4] << 23));
+      wv = dequant8(cw, __uint_as_float((uint32_t)vsc[row * (D / 32) + lane % L / 4] << 23));
+    } else if constexpr (DTYPE == LV_CACHE_E4M3) {
       const u32x2 ck = *(const u32x2 *)(kp + row * D + (lane % L) * 8), cw = *(const u32x2 *)(vp + row * D + (lane % L) * 8);
       wk = dequant8(ck, __uint_as_float((uint32_t)ksc[row] << 23));
       wv = dequant8(cw, __uint_as_float((uint32_t)vsc[row] << 23));
@@ -191,8 +226,9 @@ int launch_cache_write(const CacheView &cv, const litevggt_cache &c, const uint1
     kernel<<<dim3((uint32_t)((units + 3) / 4)), 256, 0, st>>>(cv, (char *)c.k, (char *)c.v, c.k_scale, c.v_scale, k, k_stride, v, v_stride,
                                                               off, pos, n, units, qk_norm);
   };
-  if (cv.e4m3) cv.head_dim == 64 ? go(k_cache_write<64, true>) : go(k_cache_write<128, true>);
-  else cv.head_dim == 64 ? go(k_cache_write<64, false>) : go(k_cache_write<128, false>);
+  if (cv.dtype == LV_CACHE_E2M1) cv.head_dim == 64 ? go(k_cache_write<64, LV_CACHE_E2M1>) : go(k_cache_write<128, LV_CACHE_E2M1>);
+  else if (cv.dtype == LV_CACHE_E4M3) cv.head_dim == 64 ? go(k_cache_write<64, LV_CACHE_E4M3>) : go(k_cache_write<128, LV_CACHE_E4M3>);
+  else cv.head_dim == 64 ? go(k_cache_write<64, LV_CACHE_BF16>) : go(k_cache_write<128, LV_CACHE_BF16>);
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
 }
@@ -205,8 +241,9 @@ int launch_cache_read(const CacheView &cv, const litevggt_cache &c, const int32_
     kernel<<<dim3((uint32_t)((units + 3) / 4)), 256, 0, st>>>(cv, (const char *)c.k, (const char *)c.v, c.k_scale, c.v_scale, first, off, k,
                                                               k_stride, v, v_stride, n, units);
   };
-  if (cv.e4m3) cv.head_dim == 64 ? go(k_cache_read<64, true>) : go(k_cache_read<128, true>);
-  else cv.head_dim == 64 ? go(k_cache_read<64, false>) : go(k_cache_read<128, false>);
+  if (cv.dtype == LV_CACHE_E2M1) cv.head_dim == 64 ? go(k_cache_read<64, LV_CACHE_E2M1>) : go(k_cache_read<128, LV_CACHE_E2M1>);
+  else if (cv.dtype == LV_CACHE_E4M3) cv.head_dim == 64 ? go(k_cache_read<64, LV_CACHE_E4M3>) : go(k_cache_read<128, LV_CACHE_E4M3>);
+  else cv.head_dim == 64 ? go(k_cache_read<64, LV_CACHE_BF16>) : go(k_cache_read<128, LV_CACHE_BF16>);
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
 }

@@ -128,7 +128,7 @@ int launch_attn(const uint16_t *q, const uint16_t *k, const uint16_t *v, uint16_
 // The pages of a cache as its kernels see them (validated: see check_cache in api.hip)
 struct CacheView {
   int n_seq, kv_heads, head_dim, page_shift, n_pages, max_pages;
-  bool e4m3;
+  int dtype;              // LV_CACHE_*
   const int32_t *table;   // [n_seq][max_pages]
 };
 int launch_cache_write(const CacheView &cv, const litevggt_cache &c, const uint16_t *k, int64_t k_stride, const uint16_t *v,
@@ -156,9 +156,49 @@ struct KvAttnArgs {
   CacheView cv;
   const uint8_t *k_scale, *v_scale;
 };
-size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool e4m3, int64_t most_keys);
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys);
 int launch_kv_attn(const KvAttnArgs &a, void *ws, hipStream_t st);
 // k normalised per head (row stride in elements) into rows of kv_heads * head_dim
 int launch_norm_rows(const uint16_t *k, int64_t k_stride, int n, int kv_heads, int head_dim, uint16_t *out, hipStream_t st);
+
+// rope.hip
+// The pairs of channels that an axis turns: numbers first[a] .. first[a + 1] - 1; turns[i]: frequency of pair i over 2 pi
+struct RopePairs {
+  int axes, pairing;
+  int first[5];
+  double turns[64];
+};
+// n tokens; k (kv_heads may be 0) and q each to its output, which may be the same rows; strides in elements
+int launch_rope(const RopePairs &pairs, const int32_t *pos, int n, int heads, int kv_heads, int head_dim, bool inverse, const uint16_t *q,
+                int64_t q_stride, const uint16_t *k, int64_t k_stride, uint16_t *q_out, int64_t q_out_stride, uint16_t *k_out,
+                int64_t k_out_stride, hipStream_t st);
+
+// mass.hip
+struct MassArgs {
+  const uint16_t *q;
+  int64_t q_stride;
+  const int32_t *q_off, *kv_len;
+  int n_q, heads;
+  float scale;
+  int qk_norm, frame;
+  const void *k;
+  const uint8_t *k_scale;
+  CacheView cv;
+  const float *mass_in;
+  float *mass;
+};
+size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys);
+int launch_mass(const MassArgs &a, void *ws, hipStream_t st);
+
+// evict.hip
+struct EvictArgs {
+  int n_seq, kv_heads, page_shift, n_pages, max_pages;
+  const int32_t *table, *kv_len, *keep;
+  const float *mass;
+  int first_pages, last_pages;
+  int32_t *table_out, *freed, *n_freed;
+};
+size_t evict_ws_bytes(int n_seq, int page_shift, int max_pages);
+int launch_evict(const EvictArgs &a, void *ws, hipStream_t st);
 
 }  // namespace lv

@@ -1,0 +1,148 @@
+"""The attention weight that positions draw, on the GPU, against the plain implementation in 64 bits (tolerance: stream_cases.Pool.draw)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_04939_amd import binding as B
+
+from stream_cases import DTYPES, Pool, dev, host, i32, rows
+
+pytestmark = pytest.mark.gpu
+
+FORMS = [
+    dict(lens=[1], new=[1]), dict(lens=[394], new=[1], page=64, frame=1, heads=4, kv_heads=4), dict(lens=[130], new=[5], heads=4, kv_heads=2, page=32),
+    dict(lens=[301, 1, 0, 77], new=[1, 1, 0, 3], heads=8, kv_heads=2, head_dim=128, frame=1),
+    dict(lens=[301, 1, 0, 77], new=[9, 1, 0, 3], heads=8, kv_heads=2, head_dim=64, frame=4),
+    dict(lens=[200, 63], new=[40, 63], heads=4, kv_heads=4, frame=9), dict(lens=[700], new=[300], heads=2, kv_heads=1, frame=50, page=32),
+    dict(lens=[700, 90], new=[300, 90], heads=4, kv_heads=2, frame=1, head_dim=128), dict(lens=[2600], new=[2], heads=2, kv_heads=2, page=16),
+    dict(lens=[2600], new=[40], heads=2, kv_heads=2, page=16, head_dim=128, frame=13), dict(lens=[1300], new=[600], heads=2, kv_heads=2),
+    dict(lens=[33] * 70, new=[1] * 70, heads=2, kv_heads=2, frame=1), dict(lens=[40, 600], new=[1, 90], heads=3, kv_heads=1, frame=1),
+]
+
+
+@pytest.mark.parametrize("holes", [False, True])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("form", FORMS, ids=str)
+def test_mass(form, dtype, holes):
+    form = dict(form)
+    lens, new = form.pop("lens"), form.pop("new")
+    page = form.get("page", 16)
+    gone = [(s, c) for s, n in enumerate(lens) for c in range(-(-n // page)) if c % 3 == 1] if holes else ()
+    Pool(21, lens, dtype=dtype, holes=gone, **form).draw(new, tail=2)
+
+
+@pytest.mark.parametrize("new", [2, 30, 90])
+def test_norm_scale_and_sizes_of_scores(new):
+    Pool(22, [300], heads=2, kv_heads=2, qk_norm=1, dtype="bf16").draw([new])
+    Pool(23, [300], heads=2, kv_heads=2, dtype="bf16", scale=0.5).draw([new])
+    Pool(24, [300], heads=2, kv_heads=2, dtype="e4m3", head_dim=128).draw([new])
+
+
+@pytest.mark.parametrize("new", [1, 20, 200])
+def test_scores_far_apart(new):
+    """Keys that grow along the sequence: every tile's scores are far above those before."""
+    c = Pool(25, [500], heads=1, kv_heads=1, dtype="bf16", scale=1.0)
+    q = np.ones((new, 1, 64))
+    k = np.zeros_like(c.o.k)
+    for t in range(500):
+        k[c.table[0, t // 16], :, t % 16, 0] = t // 2
+    c.o.k = k
+    c.d = c.device()
+    # whole numbers: scores are exact, weights e^-(difference); positions beyond e^-87 of the largest are 0 in 32 bits or next to it
+    got = c.draw([new], q=q, had=None)
+    assert abs(got[0, 0, :500].sum() - new) <= new * 2.0 ** -16 and got[0, 0, 499] > 0.3 * new
+
+
+def test_in_place_none_and_what_lies_behind():
+    c = Pool(26, [90, 41], heads=2, kv_heads=2, dtype="bf16", more_columns=2)
+    c.draw([7, 3], in_place=True)
+    c.draw([7, 3], had=None)
+    c.draw([0, 0])
+    # nothing new at all: what was there is carried over
+    p = c.p
+    had = torch.rand(2, 2, p.max_pages * 16, device="cuda")
+    out = torch.full_like(had, 5.0)
+    q = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    B.litevggt_cached_mass(p, c.d, q, i32([0, 0, 0]), i32([90, 41]), had, out, None)
+    assert torch.equal(out[0, :, :90], had[0, :, :90]) and torch.equal(out[1, :, :41], had[1, :, :41])
+    assert (out[0, :, 90:] == 5).all() and (out[1, :, 41:] == 5).all()
+
+
+def test_the_call_needs_no_v():
+    c = Pool(27, [60], heads=2, kv_heads=2)
+    c.draw([3], cache=B.CacheBuffers(c.d.k, None, c.d.k_scale, None, c.d.page_table))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e2m1"])
+@pytest.mark.parametrize("new", [3, 25, 120])
+def test_what_is_not_seen_has_no_part(dtype, new):
+    """NaN in K behind the last position, in pages of others, and in positions of a frame that only the last queries see."""
+    c = Pool(28, [250], heads=2, kv_heads=2, dtype=dtype, frame=10, holes=[(0, 3)])
+
+    def spoil(page, rows_):
+        if dtype == "bf16":
+            c.d.k[page, :, rows_] = float("nan")
+        else:
+            c.d.k_scale[page, :, rows_] = 255
+
+    t = c.table[0]
+    spoil(int(t[250 // 16]), slice(250 % 16, None))
+    for j in set(range(c.n_pages)) - set(t[t >= 0].tolist()):
+        spoil(j, slice(None))
+    assert np.isfinite(c.draw([new])).all()
+    # position 241, which the last ten queries see: what they see becomes NaN, and nothing else is different
+    if new > 10:
+        spoil(int(t[241 // 16]), slice(241 % 16, 241 % 16 + 1))
+        p = c.p
+        q = rows(np.random.default_rng(3), new - 10, 2, 64)
+        out = torch.zeros(1, 2, p.max_pages * 16, device="cuda")
+        ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, new))
+        B.litevggt_cached_mass(p, c.d, dev(q), i32([0, new - 10]), i32([240]), None, out, ws)
+        assert torch.isfinite(out).all()
+        full = torch.zeros_like(out)
+        B.litevggt_cached_mass(p, c.d, dev(rows(np.random.default_rng(3), new, 2, 64)), i32([0, new]), i32([250]), None, full, ws)
+        held = np.repeat(t >= 0, 16)[:250]
+        assert torch.isnan(full[0, :, :250]).cpu().numpy()[:, held].all() and (full[0, :, :250].cpu().numpy()[:, ~held] == 0).all()
+
+
+def test_offsets_and_lengths_out_of_range_are_left_out():
+    c = Pool(29, [64, 64], heads=2, kv_heads=2, dtype="bf16")
+    p = c.p
+    q = dev(rows(np.random.default_rng(1), 6, 2, 64))
+    ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, 6))
+    for off, length in (([0, 3, 900], [64, 64]), ([-5, 3, 2], [64, 64]), ([4, 2, 6], [64, 5000]), ([0, 3, 6], [-7, 2 ** 31 - 1]), ([9, 9, 9], [1, 1])):
+        out = torch.zeros(2, 2, p.max_pages * 16, device="cuda")
+        B.litevggt_cached_mass(p, c.d, q, i32(off), i32(length), None, out, ws)
+        assert torch.isfinite(out).all() and (out >= 0).all()
+
+
+def test_same_bits_again_in_a_graph_and_with_scratch_of_a_longer_call():
+    c = Pool(30, [700, 333], heads=4, kv_heads=2, frame=1)
+    p = c.p
+    q = dev(rows(np.random.default_rng(2), 90, 4, 64))
+    off, length = i32([0, 60, 90]), i32([700, 333])
+    had = torch.rand(2, 2, p.max_pages * 16, device="cuda")
+    outs = []
+    for n in (90, 90, 4000):
+        assert B.litevggt_cached_mass_ws_bytes(p, n) >= B.litevggt_cached_mass_ws_bytes(p, 90)
+        ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, n)).fill_(255)
+        out = torch.zeros_like(had)
+        B.litevggt_cached_mass(p, c.d, q, off, length, had, out, ws)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    torch.cuda.synchronize()
+    out = torch.zeros_like(had)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.litevggt_cached_mass(p, c.d, q, off, length, had, out, ws)
+    for now in ([700, 333], [80, 30], [500, 333]):
+        length.copy_(i32(now))
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        again = torch.zeros_like(had)
+        B.litevggt_cached_mass(p, c.d, q, off, length, had, again, ws)
+        assert torch.equal(out, again)
+    length.copy_(i32([700, 333]))
+    g.replay()
+    assert torch.equal(out, outs[0])
