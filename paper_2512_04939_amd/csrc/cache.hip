@@ -33,11 +33,11 @@ __device__ __forceinline__ int page_of(const CacheView &cv, int seq, int64_t pos
   return (uint32_t)id < (uint32_t)cv.n_pages ? id : -1;
 }
 
-template <int LANES>   // largest over the 4 lanes of a block, the 8 or 16 of a row
+template <int LANES>   // largest over the 8 or 16 lanes of a row
 __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, dpp_take<0xB1, 0xF>(v));    // quad_perm [1,0,3,2]
   v = fmaxf(v, dpp_take<0x4E, 0xF>(v));    // quad_perm [2,3,0,1]
-  if (LANES >= 8) v = fmaxf(v, dpp_take<0x141, 0xF>(v));   // row_half_mirror
+  v = fmaxf(v, dpp_take<0x141, 0xF>(v));   // row_half_mirror
   if (LANES == 16) v = fmaxf(v, dpp_take<0x140, 0xF>(v));   // row_mirror
   return v;
 }
@@ -80,20 +80,34 @@ __device__ __forceinline__ u32x2 quant_row8(const u32x4 w, uint32_t &exp_byte) {
 // Eight channels of a row as E2M1 codes, and the exponent byte of the 32 channels that they are a quarter of: the smallest power of two
 // that brings the largest finite |value| to 6 or less (6 = 1.5 * 2^2).  E2M1 has no NaN: a byte of 255 makes all 32 NaN, and one among
 // them sets it.
-__device__ __forceinline__ uint32_t quant_block8(const u32x4 w, uint32_t &exp_byte) {
-  float x[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)};
-  float a = 0.f;
+__device__ __forceinline__ uint32_t quant_block8(u32x4 w, uint32_t &exp_byte) {
+  // the largest magnitude by its bits, two values to a word
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  auto mag = [](uint32_t v) { return __builtin_bit_cast(u16x2, v & 0x7fff7fffu); };
+  auto larger = [](u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); };
+  auto largest = [&](const u32x4 v) {
+    u16x2 m = larger(larger(mag(v.x), mag(v.y)), larger(mag(v.z), mag(v.w)));
+    m = larger(m, __builtin_bit_cast(u16x2, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0xB1, 0xF, 0xF, false)));
+    m = larger(m, __builtin_bit_cast(u16x2, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0x4E, 0xF, 0xF, false)));
+    return (uint32_t)max(m.x, m.y);
+  };
+  uint32_t top = largest(w);
+  bool wild = false;      // the block has a NaN
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(top >= 0x7f80u) != 0, 0)) {
+    wild = top > 0x7f80u;
+    // the scale is that of the finite values; infinities saturate
+    u32x4 f = w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float m = fabsf(x[i]);
-    a = fmaxf(a, m < INFINITY ? m : m != m ? INFINITY : 0.f);
+    for (int i = 0; i < 4; ++i) {
+      f[i] &= (f[i] & 0x7f80u) == 0x7f80u ? 0xffff0000u : ~0u;
+      f[i] &= (f[i] & 0x7f800000u) == 0x7f800000u ? 0xffffu : ~0u;
+    }
+    top = largest(f);
   }
-  a = row_max<4>(a);
-  const uint32_t bits = __float_as_uint(a);
-  int e = (int)(bits >> 23) - 2 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0);
-  e = bits == 0u ? 127 : max(e, 1);
-  exp_byte = a < INFINITY ? (uint32_t)e : 255u;
-  return a < INFINITY ? cvt8_fp4(x, __uint_as_float((uint32_t)e << 23)) : 0u;
+  // biased exponent of the largest, less 2, one more for a mantissa over 1.5; at least 2^-126, 2^0 for a block of zeros
+  const int e = top == 0u ? 127 : max((int)(top >> 7) - 2 + ((top & 0x7fu) > 0x40u ? 1 : 0), 1);
+  exp_byte = wild ? 255u : (uint32_t)e;
+  return wild ? 0u : cvt8_fp4(w, __uint_as_float((uint32_t)e << 23));
 }
 
 }  // namespace

@@ -194,13 +194,14 @@ __device__ __forceinline__ u32x4 dequant8(const u32x2 w, float scale) {
   };
   return u32x4{two(w.x, std::false_type{}), two(w.x, std::true_type{}), two(w.y, std::false_type{}), two(w.y, std::true_type{})};
 }
-// E2M1 (0 0.5 1 1.5 2 3 4 6 and their negatives, no infinities, no NaN): 8 floats over a power of two as codes, two to a byte, the
-// first in the low half (v_cvt_scalef32_pk_fp4_f32: round to nearest even, saturating)
-__device__ __forceinline__ uint32_t cvt8_fp4(const float (&x)[8], float scale) {
-  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+// E2M1 (0 0.5 1 1.5 2 3 4 6 and their negatives, no infinities, no NaN): 8 bf16 values over a power of two as codes, two to a byte, the
+// first in the low half (v_cvt_scalef32_pk_fp4_bf16: round to nearest even, saturating)
+__device__ __forceinline__ uint32_t cvt8_fp4(const u32x4 x, float scale) {
+  auto two = [](uint32_t v) { return __builtin_bit_cast(bf16x2, v); };
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, two(x.x), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(x.y), scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(x.z), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two(x.w), scale, 3);
 }
 // 8 such codes times a power of two as 8 bf16 values (exact; a scale with all exponent bits set gives NaN)
 __device__ __forceinline__ u32x4 dequant8(const uint32_t w, float scale) {

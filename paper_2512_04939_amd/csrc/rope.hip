@@ -17,91 +17,120 @@ struct RopeCall {
   uint16_t *y[2];
   int64_t x_stride[2], y_stride[2];
   int heads, all;          // of q; of both
-  int n, axes, head_dim;
-  int parts, per;          // the heads are taken in so many parts of `per`
+  int n, axes;
+  int parts;               // the heads are taken in so many
   int rotated;             // channels that are; the others are copied
   float sign;              // of the sine
 };
 
-// What a lane does with its eight channels: channel e turns with pair `pair`, its partner lies `dist` channels away (below: it is the second of
-// the pair, whose first is its partner)
-struct Lane {
-  int pair, axis, dist;
+// Channel c's axis (its channels lie in [2 first, 2 first + 2 pairs) where an axis' halves are paired), pair and the distance of its partner, below 0
+// where it is the pair's second; 0: not turned
+struct Channel {
+  int axis, pair, dist;
 };
-
-// By how the channels of a pair lie: next to each other; as many apart as an axis has pairs; as many as there are in all
-__device__ __forceinline__ Lane lane_of(const RopePairs &r, int c) {
-  Lane l = {0, 0, 0};
-  if (c >= 2 * r.first[r.axes]) return l;
+__device__ __forceinline__ int axis_of(const RopePairs &r, int pair) {
+  return (pair >= r.first[1] && r.axes > 1) + (pair >= r.first[2] && r.axes > 2) + (pair >= r.first[3] && r.axes > 3);
+}
+__device__ __forceinline__ Channel channel_of(const RopePairs &r, int all, int c) {
+  Channel l = {0, 0, 0};
+  if (c >= 2 * all) return l;
   if (r.pairing == LV_ROPE_ADJACENT) {
     l.pair = c >> 1;
     l.dist = c & 1 ? -1 : 1;
+    l.axis = axis_of(r, l.pair);
   } else if (r.pairing == LV_ROPE_HEAD_HALVES) {
-    const int all = r.first[r.axes];
     l.pair = c < all ? c : c - all;
     l.dist = c < all ? all : -all;
+    l.axis = axis_of(r, l.pair);
   } else {
-    int a = 0;
-    while (c >= 2 * r.first[a + 1]) ++a;
-    const int p = r.first[a + 1] - r.first[a], j = c - 2 * r.first[a];
-    l.pair = r.first[a] + (j < p ? j : j - p);
+    l.axis = axis_of(r, c >> 1);
+    const int lo = l.axis == 0 ? 0 : l.axis == 1 ? r.first[1] : l.axis == 2 ? r.first[2] : r.first[3];
+    const int hi = l.axis == 0 ? r.first[1] : l.axis == 1 ? r.first[2] : l.axis == 2 ? r.first[3] : r.first[4];
+    const int j = c - 2 * lo, p = hi - lo;
+    l.pair = lo + (j < p ? j : j - p);
     l.dist = j < p ? p : -p;
   }
-  while (l.pair >= r.first[l.axis + 1]) ++l.axis;
   return l;
 }
 
 }  // namespace
 
-// D / 8 lanes take the heads of one token in turn, 16 bytes of each, so that a lane works its angles out once for all of them.  The partners
-// come from memory as well, where the first read of the line has just brought them: as 16 bytes where they lie so (WIDE: an axis has a
-// multiple of 8 pairs), else one by one; adjacent pairs lie in the lane's own bytes.  All that a head needs has been read before any of it is
-// written, so the output may take the input's place.
-template <int D, int MODE>      // 0: adjacent pairs, 1: partners in 16 bytes, 2: one by one
+// D / 8 lanes take heads of one token, 16 bytes of each, so that a lane works its angles out once for PER of them.  The partners come from
+// memory as well, where the first read of the line has just brought them: as 16 bytes where they lie so (an axis has a multiple
+// of 8 pairs), else one by one; adjacent pairs lie in the lane's own bytes.  All reads of a lane's heads are on the way before its angles are
+// worked out, and all that a head needs has been read before any of it is written, so the output may take the input's place.
+template <int D, int MODE, int PER>      // 0: adjacent pairs, 1: partners in 16 bytes, 2: one by one
 __global__ __launch_bounds__(256) void k_rope(RopeCall a, RopePairs r) {
   constexpr int L = D / 8;
-  const int64_t unit = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const uint32_t unit = blockIdx.x * (256 / L) + threadIdx.x / L;
   const int c0 = threadIdx.x % L * 8;
-  const int tok = (int)(unit / a.parts), part = (int)(unit - (int64_t)tok * a.parts);
+  const int tok = (int)(unit / (uint32_t)a.parts), h0 = (int)(unit - (uint32_t)tok * a.parts) * PER;
   if (tok >= a.n) return;
-  float cs[8], sn[8];
+  const int all = a.rotated >> 1;
   int dist[8];
+  Channel ch = channel_of(r, all, c0);
+  if constexpr (MODE == 1) dist[0] = ch.dist;
+  if constexpr (MODE == 2) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const Lane l = lane_of(r, c0 + e);
-    dist[e] = l.dist;
-    double turns = (double)a.pos[(int64_t)tok * a.axes + l.axis] * r.turns[l.pair];
-    turns -= __builtin_floor(turns);
-    const float f = (float)turns;
-    cs[e] = l.dist ? __builtin_amdgcn_cosf(f) : 1.0f;
-    sn[e] = l.dist ? __builtin_amdgcn_sinf(f) * (l.dist < 0 ? a.sign : -a.sign) : 0.0f;
+    for (int e = 0; e < 8; ++e) dist[e] = channel_of(r, all, c0 + e).dist;
   }
-  const int end = min((part + 1) * a.per, a.all);
-  for (int h = part * a.per; h < end; ++h) {
-    const int which = h >= a.heads, head = which ? h - a.heads : h;
-    const uint16_t *x = a.x[which] + (int64_t)tok * a.x_stride[which] + head * D + c0;
-    const u32x4 w = *(const u32x4 *)x;
-    float v[8] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), bf16_lo(w.z), bf16_hi(w.z), bf16_lo(w.w), bf16_hi(w.w)}, p[8];
-    if constexpr (MODE == 0) {
+  u32x4 w[PER];
+  uint32_t o[PER][4];      // the partners: two bf16 to a word
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = v[e ^ 1];
-    } else if constexpr (MODE == 1) {
-      const u32x4 o = *(const u32x4 *)(x + dist[0]);
-      p[0] = bf16_lo(o.x), p[1] = bf16_hi(o.x), p[2] = bf16_lo(o.y), p[3] = bf16_hi(o.y);
-      p[4] = bf16_lo(o.z), p[5] = bf16_hi(o.z), p[6] = bf16_lo(o.w), p[7] = bf16_hi(o.w);
+  for (int i = 0; i < PER; ++i) {
+    const int h = min(h0 + i, a.all - 1), which = h >= a.heads, head = which ? h - a.heads : h;
+    const uint16_t *x = (which ? a.x[1] : a.x[0]) + (int64_t)tok * (which ? a.x_stride[1] : a.x_stride[0]) + head * D + c0;
+    w[i] = *(const u32x4 *)x;
+    if constexpr (MODE == 1) {
+      const u32x4 y = *(const u32x4 *)(x + dist[0]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = y[e];
+    }
+    if constexpr (MODE == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][e] = (uint32_t)x[2 * e + dist[2 * e]] | (uint32_t)x[2 * e + 1 + dist[2 * e + 1]] << 16;
+    }
+  }
+  float cs[8], sn[8];
+  const int32_t *pos = a.pos + (int64_t)tok * a.axes;
+  int at = pos[ch.axis];
+#pragma unroll
+  for (int e = 0; e < (MODE == 0 ? 4 : 8); ++e) {
+    if constexpr (MODE == 1) {
+      ch.pair += e ? 1 : 0;
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = bf16_to_f32(x[e + dist[e]]);
+      ch = channel_of(r, all, MODE == 0 ? c0 + 2 * e : c0 + e);
+      at = pos[ch.axis];
     }
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = v[e] * cs[e] + p[e] * sn[e];
-    if (c0 + 8 > a.rotated) {      // channels that are copied: also what is not finite there
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = c0 + e < a.rotated ? y[e] : v[e];
+    double turns = (double)at * r.turns[ch.pair];
+    turns -= __builtin_floor(turns);
+    const float f = (float)turns, co = __builtin_amdgcn_cosf(f), si = __builtin_amdgcn_sinf(f) * a.sign;
+    if constexpr (MODE == 0) {
+      cs[2 * e] = cs[2 * e + 1] = co;
+      sn[2 * e] = -si;
+      sn[2 * e + 1] = si;
+    } else {
+      cs[e] = co;
+      sn[e] = ch.dist < 0 ? si : -si;
     }
-    *(u32x4 *)(a.y[which] + (int64_t)tok * a.y_stride[which] + head * D + c0) =
-        u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int h = h0 + i, which = h >= a.heads, head = which ? h - a.heads : h;
+    const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x0 = bf16_lo(v[e]), x1 = bf16_hi(v[e]);
+      const float p0 = MODE == 0 ? x1 : bf16_lo(o[i][e]), p1 = MODE == 0 ? x0 : bf16_hi(o[i][e]);
+      y[e] = pack_bf16(x0 * cs[2 * e] + p0 * sn[2 * e], x1 * cs[2 * e + 1] + p1 * sn[2 * e + 1]);
+      if (c0 + 8 > a.rotated) {      // channels that are copied, bit by bit
+        const uint32_t keep = (c0 + 2 * e < a.rotated ? 0u : 0xffffu) | (c0 + 2 * e + 1 < a.rotated ? 0u : 0xffff0000u);
+        y[e] = (y[e] & ~keep) | (v[e] & keep);
+      }
+    }
+    if (h < a.all)
+      *(u32x4 *)((which ? a.y[1] : a.y[0]) + (int64_t)tok * (which ? a.y_stride[1] : a.y_stride[0]) + head * D + c0) = u32x4{y[0], y[1], y[2], y[3]};
   }
 }
 
@@ -118,19 +147,24 @@ int launch_rope(const RopePairs &pairs, const int32_t *pos, int n, int heads, in
   a.all = heads + kv_heads;
   a.n = n;
   a.axes = pairs.axes;
-  a.head_dim = head_dim;
   a.rotated = 2 * pairs.first[pairs.axes];
   a.sign = inverse ? -1.0f : 1.0f;
-  a.per = 8;
-  a.parts = (a.all + a.per - 1) / a.per;
   const int per_group = 256 / (head_dim / 8);
+  // four heads to a lane, so that the angles are worked out once for all of them; one where the chip would not be full so
+  const bool few = (int64_t)n * a.all <= 8192;
+  const int per = few ? 1 : 4;
+  a.parts = (a.all + per - 1) / per;
   const uint32_t grid = (uint32_t)(((int64_t)n * a.parts + per_group - 1) / per_group);
   bool wide = true;
   for (int i = 1; i <= pairs.axes; ++i) wide = wide && pairs.first[i] % 8 == 0;
   const int mode = pairs.pairing == LV_ROPE_ADJACENT ? 0 : wide ? 1 : 2;
   auto go = [&](auto kernel) { kernel<<<dim3(grid), 256, 0, st>>>(a, pairs); };
-  if (head_dim == 64) mode == 0 ? go(k_rope<64, 0>) : mode == 1 ? go(k_rope<64, 1>) : go(k_rope<64, 2>);
-  else mode == 0 ? go(k_rope<128, 0>) : mode == 1 ? go(k_rope<128, 1>) : go(k_rope<128, 2>);
+  auto by_mode = [&](auto dim, auto p) {
+    constexpr int D = decltype(dim)::value, PER = decltype(p)::value;
+    mode == 0 ? go(k_rope<D, 0, PER>) : mode == 1 ? go(k_rope<D, 1, PER>) : go(k_rope<D, 2, PER>);
+  };
+  auto by_per = [&](auto dim) { few ? by_mode(dim, std::integral_constant<int, 1>{}) : by_mode(dim, std::integral_constant<int, 4>{}); };
+  head_dim == 64 ? by_per(std::integral_constant<int, 64>{}) : by_per(std::integral_constant<int, 128>{});
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
 }
