@@ -600,8 +600,8 @@ int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t
 
 size_t litevggt_cached_mass_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
   CacheView cv;
-  if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
-  return mass_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, (int64_t)p->max_pages << cv.page_shift);
+  if (check_cache(p, &cv) || !count_ok(n_tokens, p->heads)) return 0;
+  return mass_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.dtype, (int64_t)p->max_pages << cv.page_shift);
 }
 
 int litevggt_cached_mass(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens, const void *q, int64_t q_stride,

@@ -14,15 +14,18 @@ namespace {
 
 constexpr int kSpan = 256;       // positions that a workgroup sums at a time
 constexpr int kBins = 2048;
+constexpr int kList = 512;       // keys that are compared one by one
+constexpr int kLdsKeys = 16384;  // columns whose keys lie in LDS
 
 __device__ __forceinline__ int used_columns(const EvictArgs &a, int s) {
   const int64_t len = max(a.kv_len[s], 0);
   return (int)min((len + (1 << a.page_shift) - 1) >> a.page_shift, (int64_t)a.max_pages);
 }
 
-// Doubles in their order as whole numbers, NaN above all others (a page whose mass is not known stays)
+// Doubles in their order as whole numbers, NaN above all others (a page whose mass is not known stays), and below the mark of a column that
+// may not leave
 __device__ __forceinline__ uint64_t key_of(double v) {
-  if (v != v) return ~(uint64_t)0;
+  if (v != v) return ~(uint64_t)1;
   v = v == 0.0 ? 0.0 : v;       // (-0)
   const uint64_t b = __builtin_bit_cast(uint64_t, v);
   return b >> 63 ? ~b : b | (uint64_t)1 << 63;
@@ -72,45 +75,50 @@ __device__ __forceinline__ int wave_prefix(int v, int lane) {     // up to the l
   }
   return v;
 }
+__device__ __forceinline__ uint64_t lower(uint64_t a, uint64_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 }  // namespace
 
-__global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, double *sums, uint64_t *keys) {
-  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// LDS: the keys lie there and not in the workspace
+template <bool LDS>
+__global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, const double *sums, uint64_t *room) {
+  extern __shared__ uint64_t keys_lds[];
+  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int used = used_columns(a, s), per = max(1 << a.page_shift >> 8, 1);
   const int64_t len = min((int64_t)max(a.kv_len[s], 0), (int64_t)a.max_pages << a.page_shift);
   const int32_t *table = a.table + (int64_t)s * a.max_pages;
   sums += (int64_t)s * a.max_pages * per;
-  keys += (int64_t)s * a.max_pages;
+  uint64_t *const keys = LDS ? keys_lds : room + (int64_t)s * a.max_pages;
   __shared__ uint32_t bins[kBins];
-  __shared__ int counts[16][2];
-  __shared__ uint64_t ends[16][2];
-  __shared__ int found[2];
+  __shared__ int counts[16][2], found[2], listed;
+  __shared__ uint64_t ends[16][2], list[kList], at_last;
   const int lo_col = min(a.first_pages, used), hi_col = max(used - min(a.last_pages, used), lo_col);
 
-  // keys of the pages that may leave, how many these are, how many are held, the least and the largest key
-  auto held_at = [&](int j) { return (uint32_t)table[j] < (uint32_t)a.n_pages; };
+  // keys of the pages that may leave (all bits set: may not), how many these are, how many are held, the least and the largest key
   int held = 0, open = 0;
   uint64_t lo = ~(uint64_t)0, hi = 0;
   for (int j = tid; j < used; j += 1024) {
-    if (!held_at(j)) continue;
-    ++held;
-    if (j < lo_col || j >= hi_col) continue;
-    ++open;
-    double sum = 0.0;
-    for (int i = 0; i < per; ++i)
-      if (((int64_t)j << a.page_shift) + i * kSpan < len) sum += sums[(int64_t)j * per + i];
-    const uint64_t k = key_of(sum);
+    const bool is_held = (uint32_t)table[j] < (uint32_t)a.n_pages, is_open = is_held && j >= lo_col && j < hi_col;
+    uint64_t k = ~(uint64_t)0;
+    held += is_held;
+    if (is_open) {
+      double sum = sums[(int64_t)j * per];
+      for (int i = 1; i < per; ++i)
+        if (((int64_t)j << a.page_shift) + i * kSpan < len) sum += sums[(int64_t)j * per + i];
+      k = key_of(sum);
+      lo = lower(lo, k);
+      hi = higher(hi, k);
+      ++open;
+    }
     keys[j] = k;
-    lo = min(lo, k);
-    hi = max(hi, k);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     held += __shfl_xor(held, o, 64);
     open += __shfl_xor(open, o, 64);
-    lo = min(lo, (uint64_t)__shfl_xor((unsigned long long)lo, o, 64));
-    hi = max(hi, (uint64_t)__shfl_xor((unsigned long long)hi, o, 64));
+    lo = lower(lo, (uint64_t)__shfl_xor((unsigned long long)lo, o, 64));
+    hi = higher(hi, (uint64_t)__shfl_xor((unsigned long long)hi, o, 64));
   }
   if (lane == 0) {
     counts[wave][0] = held;
@@ -118,25 +126,27 @@ __global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, double *sums
     ends[wave][0] = lo;
     ends[wave][1] = hi;
   }
+  if (tid == 0) listed = 0;
   __syncthreads();
   held = open = 0;
   for (int i = 0; i < 16; ++i) {
     held += counts[i][0];
     open += counts[i][1];
-    lo = min(lo, ends[i][0]);
-    hi = max(hi, ends[i][1]);
+    lo = lower(lo, ends[i][0]);
+    hi = higher(hi, ends[i][1]);
   }
   const int leave = max(min(held - max(a.keep[s], 0), open), 0);
+  __syncthreads();
 
-  // the key up to which they leave: below `lo` all do, of those equal to it the first `ties`.  Every turn leaves a 2048th of the range.
-  int ties = leave;
+  // the key up to which they leave: below `lo` all do, of those equal to it the first `ties`.  A turn leaves a 2048th of the range; once
+  // its keys fit a list, each is compared with all others there.
+  int ties = leave, inside = open;      // keys in lo .. hi
   if (leave > 0) {
-    while (lo < hi) {
-      const int width = 64 - __builtin_clzll(hi - lo), shift = max(width - 11, 0);
+    while (lo < hi && inside > kList) {
+      const int shift = max(64 - __builtin_clzll(hi - lo) - 11, 0);
       for (int i = tid; i < kBins; i += 1024) bins[i] = 0;
       __syncthreads();
       for (int j = lo_col + tid; j < hi_col; j += 1024) {
-        if (!held_at(j)) continue;
         const uint64_t k = keys[j];
         if (k >= lo && k <= hi) atomicAdd(&bins[(k - lo) >> shift], 1u);
       }
@@ -148,58 +158,81 @@ __global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, double *sums
       __syncthreads();
       int before = upto - b0 - b1;
       for (int i = 0; i < wave; ++i) before += counts[i][0];
-      if (before < ties && ties <= before + b0) {
-        found[0] = 2 * tid;
-        found[1] = before;
-      } else if (before + b0 < ties && ties <= before + b0 + b1) {
-        found[0] = 2 * tid + 1;
-        found[1] = before + b0;
+      if (before < ties && ties <= before + b0 + b1) {
+        const bool second = ties > before + b0;
+        found[0] = 2 * tid + second;
+        found[1] = second ? before + b0 : before;
       }
       __syncthreads();
-      const uint64_t at = lo + ((uint64_t)found[0] << shift);
+      inside = (int)bins[found[0]];
       ties -= found[1];
+      lo += (uint64_t)found[0] << shift;
       const uint64_t rest = ((uint64_t)1 << shift) - 1;
-      hi = hi - at < rest ? hi : at + rest;
-      lo = at;
+      hi = hi - lo < rest ? hi : lo + rest;
       __syncthreads();
+    }
+    if (lo < hi) {
+      for (int j = lo_col + tid; j < hi_col; j += 1024) {
+        const uint64_t k = keys[j];
+        if (k >= lo && k <= hi) list[atomicAdd(&listed, 1)] = k;
+      }
+      __syncthreads();
+      if (tid < inside) {
+        const uint64_t k = list[tid];
+        int less = 0, same = 0;
+        for (int i = 0; i < inside; ++i) {
+          less += list[i] < k;
+          same += list[i] == k;
+        }
+        if (less < ties && ties <= less + same) {      // (all that are equal write the same)
+          at_last = k;
+          found[1] = less;
+        }
+      }
+      __syncthreads();
+      lo = at_last;
+      ties -= found[1];
     }
   }
 
-  __syncthreads();
-
-  // columns in their order
-  int tied = 0, gone = 0;
-  int32_t *freed = a.freed + (int64_t)s * a.max_pages;
-  for (int j0 = 0; j0 < a.max_pages; j0 += 1024) {
-    const int j = j0 + tid;
-    const bool mine = j < a.max_pages;
-    const int id = mine ? table[j] : -1;
-    bool leaves = false;
-    if (j0 < hi_col && leave > 0) {       // (the same for all)
-      const bool is_open = j >= lo_col && j < hi_col && (uint32_t)id < (uint32_t)a.n_pages;
-      const uint64_t k = is_open ? keys[j] : ~(uint64_t)0;
-      const uint64_t same = __builtin_amdgcn_ballot_w64(is_open && k == lo);
-      if (lane == 0) counts[wave][0] = __popcll(same);
-      __syncthreads();
-      int t = tied + __popcll(same & (((uint64_t)1 << lane) - 1));
-      for (int i = 0; i < 16; ++i) {
-        t += i < wave ? counts[i][0] : 0;
-        tied += counts[i][0];
-      }
-      leaves = is_open && (k < lo || (k == lo && t < ties));
+  // columns in their order: a wave has a run of them, and counts first
+  const int32_t *const from = table;
+  int32_t *const to = a.table_out + (int64_t)s * a.max_pages, *const freed = a.freed + (int64_t)s * a.max_pages;
+  if (leave > 0) {
+    const int run = (used + 1023) / 1024 * 64, j0 = wave * run;
+    int less = 0, same = 0;
+    for (int j = j0 + lane; j < j0 + run; j += 64) {
+      const uint64_t k = j < used ? keys[j] : ~(uint64_t)0;
+      less += __popcll(__builtin_amdgcn_ballot_w64(k < lo));
+      same += __popcll(__builtin_amdgcn_ballot_w64(k == lo));
+    }
+    if (lane == 0) {
+      counts[wave][0] = less;
+      counts[wave][1] = same;
+    }
+    __syncthreads();
+    int tied = 0, gone = 0;
+    for (int i = 0; i < wave; ++i) {
+      gone += counts[i][0] + min(max(ties - tied, 0), counts[i][1]);
+      tied += counts[i][1];
+    }
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    for (int j = j0 + lane; j < j0 + run; j += 64) {
+      const uint64_t k = j < used ? keys[j] : ~(uint64_t)0;
+      const uint64_t equal = __builtin_amdgcn_ballot_w64(k == lo);
+      const bool leaves = k < lo || (k == lo && tied + __popcll(equal & below) < ties);
       const uint64_t out = __builtin_amdgcn_ballot_w64(leaves);
-      if (lane == 0) counts[wave][1] = __popcll(out);
-      __syncthreads();
-      int at = gone + __popcll(out & (((uint64_t)1 << lane) - 1));
-      for (int i = 0; i < 16; ++i) {
-        at += i < wave ? counts[i][1] : 0;
-        gone += counts[i][1];
+      if (j < used) {
+        const int id = from[j];
+        if (leaves) freed[gone + __popcll(out & below)] = id;
+        to[j] = leaves ? -1 : id;
       }
-      if (leaves) freed[at] = id;
+      tied += __popcll(equal);
+      gone += __popcll(out);
     }
-    if (mine) a.table_out[(int64_t)s * a.max_pages + j] = leaves ? -1 : id;
-    if (mine && j >= leave) freed[j] = -1;
   }
+  for (int j = (leave > 0 ? used : 0) + tid; j < a.max_pages; j += 1024) to[j] = from[j];
+  for (int j = leave + tid; j < a.max_pages; j += 1024) freed[j] = -1;
   if (tid == 0) a.n_freed[s] = leave;
 }
 
@@ -215,7 +248,15 @@ int launch_evict(const EvictArgs &a, void *ws, hipStream_t st) {
   const int64_t spans = (((int64_t)a.max_pages << a.page_shift) + kSpan - 1) / kSpan;
   const int side = (int)std::max((int64_t)1, std::min(spans, (int64_t)(8192 / a.n_seq)));
   k_evict_sums<<<dim3((uint32_t)(side * (int64_t)a.n_seq)), 256, 0, st>>>(a, sums, side);
-  k_evict_select<<<dim3((uint32_t)a.n_seq), 1024, 0, st>>>(a, sums, keys);
+  if (a.max_pages <= kLdsKeys) {
+    static std::atomic<uint64_t> done{0};
+    const size_t lds = (size_t)a.max_pages * sizeof(uint64_t);
+    const int rc = allow_dynamic_lds<kLdsKeys * sizeof(uint64_t)>((const void *)k_evict_select<true>, done);
+    if (rc) return rc;
+    k_evict_select<true><<<dim3((uint32_t)a.n_seq), 1024, lds, st>>>(a, sums, keys);
+  } else {
+    k_evict_select<false><<<dim3((uint32_t)a.n_seq), 1024, 0, st>>>(a, sums, keys);
+  }
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
 }

@@ -187,7 +187,7 @@ struct MassArgs {
   const float *mass_in;
   float *mass;
 };
-size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys);
+size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys);
 int launch_mass(const MassArgs &a, void *ws, hipStream_t st);
 
 // evict.hip

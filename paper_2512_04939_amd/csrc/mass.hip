@@ -27,7 +27,7 @@ enum class Kind { BF16, E4M3, E2M1 };
 
 struct Call {
   const uint16_t *q;
-  int64_t q_stride;
+  int64_t q_stride;        // 0: rows lie as their numbers count (k_mass_pack)
   const int32_t *q_off, *kv_len;
   int n_q, n_seq, kv_heads, group, frame;
   float c;
@@ -35,12 +35,14 @@ struct Call {
   const uint8_t *k_scale;
   const int32_t *table;
   int page_shift, n_pages, max_pages;
-  int pieces, splits;      // of the key axis; of the rows
-  int units;
+  int pieces, splits;      // of a sequence's keys at most; of the rows
+  bool of_rows;            // sequences without queries have no units
+  const int *starts;       // more than 64 sequences: units before each, and in all (k_mass_plan); else null
   const float *mass_in;
   float *mass;
   float2 *part;            // [piece][kv head][token, head of the group]: reference, sum of weights
   float2 *stat;            // [kv head][token, head of the group]: reference, 1 / sum of weights
+  float *scores;           // [kv head][token, head of the group][position], where there are few rows; else null
 };
 
 struct Seq {
@@ -51,15 +53,16 @@ __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirst
 // One number for all lanes, by a scalar load
 __device__ __forceinline__ int uniform_at(const int32_t *p, int i) { return ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)p)[i]; }
 
-__device__ __forceinline__ Seq seq_at(const Call &a, int s) {
+__device__ __forceinline__ Seq seq_of_numbers(const Call &a, int off, int next, int kv_len) {
   Seq r;
-  const int len = max(uniform_at(a.kv_len, s), 0);
-  r.q0 = min(max(uniform_at(a.q_off, s), 0), a.n_q);
-  r.nq = min(max(uniform_at(a.q_off, s + 1), r.q0), a.n_q) - r.q0;
+  const int len = max(kv_len, 0);
+  r.q0 = min(max(off, 0), a.n_q);
+  r.nq = min(max(next, r.q0), a.n_q) - r.q0;
   r.nk = (int)min((int64_t)len, (int64_t)a.max_pages << a.page_shift);
   r.p0 = len - r.nq;
   return r;
 }
+__device__ __forceinline__ Seq seq_at(const Call &a, int s) { return seq_of_numbers(a, uniform_at(a.q_off, s), uniform_at(a.q_off, s + 1), uniform_at(a.kv_len, s)); }
 
 // Keys that query i sees (all up to this one); it does not fall from query to query
 __device__ __forceinline__ int limit_of(const Call &a, const Seq &s, int i) {
@@ -108,13 +111,21 @@ __device__ __forceinline__ int64_t row_of(const Call &a, int seq, int head, int 
   return held ? (((int64_t)id * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1)) : -1;
 }
 
+__device__ __forceinline__ int64_t row_number(const Call &a, int head, const Seq &s) { return ((int64_t)head * a.n_q + s.q0) * a.group; }
+
 template <int D>
 struct Query {
   bf16x8 f[D / 16];
   __device__ __forceinline__ void load(const Call &a, const Seq &s, int head, int row, int n_rows, int lane) {
     const int r = min(row, n_rows - 1);
-    const int i = (int)((uint32_t)r / (uint32_t)a.group), g = r - i * a.group;
-    const uint16_t *p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D + (lane >> 5) * (D / 2);
+    const uint16_t *p;
+    if (a.q_stride == 0) {
+      p = a.q + (row_number(a, head, s) + r) * D;
+    } else {
+      const int i = (int)((uint32_t)r / (uint32_t)a.group), g = r - i * a.group;
+      p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D;
+    }
+    p += (lane >> 5) * (D / 2);
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) f[j] = *(const bf16x8 *)(p + 8 * j);
   }
@@ -133,25 +144,109 @@ struct Work {
   int c0, c1;      // its chunks
 };
 
-// The wave's part of the call: chunks of kc keys, `pieces` runs of them as long as the sequence's length makes them
+__device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); }
+// A sequence's keys in chunks of kc, and these in pieces of so many: as many pieces as there may be, none of them empty
+__device__ __forceinline__ int chunks_of_piece(const Call &a, int nk, int kc) { return quotient_up(quotient_up(nk, kc), a.pieces); }
+__device__ __forceinline__ int pieces_of(const Call &a, const Seq &s, int kc) {
+  if (s.nk == 0 || (a.of_rows && s.nq == 0)) return 0;
+  return quotient_up(quotient_up(s.nk, kc), chunks_of_piece(a, s.nk, kc));
+}
+__device__ __forceinline__ int units_of(const Call &a, const Seq &s, int kc) { return pieces_of(a, s, kc) * a.kv_heads * a.splits; }
+
+// up to the lane (row_shr 1, 2, 4, 8 inside rows of 16 lanes; the rows' last lanes to the rows behind)
+__device__ __forceinline__ int wave_prefix(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
+// The wave's part of the call: the units of the sequences one after the other, those that are not there behind them all.  (Workgroups go to
+// the parts of an XCD in turn, whether these have room or not: where every pair had the same number of units, a third of them empty, the
+// parts that got the full ones held the others up, and 5 of 8 waves ran: four frames over 2748 to 41,220 positions 737 us
+// for the rows' sums and 896 for the keys'.)
 __device__ __forceinline__ bool find_work(const Call &a, int unit, int kc, Work &w, Seq &s) {
-  if (unit >= a.units) return false;
-  const int x = scalar((int)((uint32_t)unit / (uint32_t)a.splits));
-  w.split = scalar(unit - x * a.splits);
-  const int y = scalar((int)((uint32_t)x / (uint32_t)a.pieces));
-  w.piece = scalar(x - y * a.pieces);
-  w.seq = scalar((int)((uint32_t)y / (uint32_t)a.kv_heads));
-  w.head = scalar(y - w.seq * a.kv_heads);
-  s = seq_at(a, w.seq);
-  const int chunks = scalar((int)(((uint32_t)s.nk + kc - 1) / (uint32_t)kc)), per = scalar((int)((uint32_t)(chunks + a.pieces - 1) / (uint32_t)a.pieces));
-  w.c0 = min(w.piece * per, chunks);
-  w.c1 = min(w.c0 + per, chunks);
+  const int lane = threadIdx.x & 63;
+  int local;
+  if (a.starts) {
+    if (unit >= uniform_at(a.starts, a.n_seq)) return false;
+    w.seq = scalar(max(last_at_most(a.starts, a.n_seq, unit, lane), 0));
+    local = unit - uniform_at(a.starts, w.seq);
+    s = seq_at(a, w.seq);
+  } else {
+    const int i = min(lane, a.n_seq - 1);
+    const Seq mine = seq_of_numbers(a, a.q_off[i], a.q_off[i + 1], a.kv_len[i]);
+    const int units = lane < a.n_seq ? units_of(a, mine, kc) : 0, end = wave_prefix(units);
+    if (unit >= __builtin_amdgcn_readlane(end, 63)) return false;
+    w.seq = scalar(__popcll(__builtin_amdgcn_ballot_w64(end <= unit)));
+    local = unit - __builtin_amdgcn_readlane(end - units, w.seq);
+    s.q0 = __builtin_amdgcn_readlane(mine.q0, w.seq);
+    s.nq = __builtin_amdgcn_readlane(mine.nq, w.seq);
+    s.nk = __builtin_amdgcn_readlane(mine.nk, w.seq);
+    s.p0 = __builtin_amdgcn_readlane(mine.p0, w.seq);
+  }
+  const int pieces = scalar(pieces_of(a, s, kc)), per = scalar(chunks_of_piece(a, s.nk, kc));
+  if (pieces == 0) return false;      // (lengths that changed meanwhile)
+  const int x = scalar((int)((uint32_t)local / (uint32_t)pieces));
+  w.piece = scalar(local - x * pieces);
+  w.head = scalar((int)((uint32_t)x / (uint32_t)a.splits));
+  w.split = scalar(x - w.head * a.splits);
+  if (w.head >= a.kv_heads) return false;
+  w.c0 = w.piece * per;
+  w.c1 = min(w.c0 + per, quotient_up(s.nk, kc));
   return w.c0 < w.c1;
 }
 
-__device__ __forceinline__ int64_t row_number(const Call &a, int head, const Seq &s) { return ((int64_t)head * a.n_q + s.q0) * a.group; }
-
 }  // namespace
+
+// More than 64 sequences: the units before each, worked out once.  (Twice: for the rows' sums, then, with `b`, for the keys'.)
+__global__ __launch_bounds__(1024) void k_mass_plan(Call a, Call b, int kc_a, int kc_b, int *starts_a, int *starts_b) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
+  __shared__ int sums[2][16];
+  for (int which = 0; which < 2; ++which) {
+    const Call &c = which ? b : a;
+    int *const starts = which ? starts_b : starts_a;
+    int before = 0;
+    for (int i0 = 0; i0 < c.n_seq; i0 += 1024) {
+      const int i = i0 + tid, turn = i0 >> 10 & 1;
+      int units = 0;
+      if (i < c.n_seq) units = units_of(c, seq_of_numbers(c, c.q_off[i], c.q_off[i + 1], c.kv_len[i]), which ? kc_b : kc_a);
+      const int end = wave_prefix(units);
+      if (lane == 63) sums[turn][wave] = end;
+      __syncthreads();      // (the other of the two is read by nobody any more behind it)
+      int at = before + end - units;
+      for (int x = 0; x < 16; ++x) {
+        at += x < wave ? sums[turn][x] : 0;
+        before += sums[turn][x];
+      }
+      if (i < c.n_seq) starts[i] = at;
+    }
+    if (tid == 0) starts[c.n_seq] = before;
+    __syncthreads();
+  }
+}
+
+// Rows by kv head, normalised if they are to be: [kv head][token, head of the group][D].  As they come, the rows of one head lie the width of a
+// token apart, and many waves that walk the same head would all wait for the few channels of L2 that such lines are in.
+template <int D>
+__global__ __launch_bounds__(256) void k_mass_pack(const uint16_t *q, int64_t stride, int n_q, int kv_heads, int group, int qk_norm, uint16_t *out) {
+  constexpr int L = D / 8;
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L, rows = (int64_t)n_q * kv_heads * group;
+  const int p = threadIdx.x % L;
+  const uint32_t rr = (uint32_t)(r < rows ? r : rows - 1), heads = (uint32_t)(kv_heads * group);
+  const uint32_t tok = rr / heads, head = rr - tok * heads, kv = head / (uint32_t)group;
+  u32x4 w = *(const u32x4 *)(q + tok * stride + head * D + p * 8);
+  if (qk_norm) {
+    float ss = sumsq8(w);
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) ss += __shfl_xor(ss, o, 64);
+    w = scale8(w, 1.0f / sqrtf(ss * (1.0f / D) + kQkEps));
+  }
+  if (r < rows) *(u32x4 *)(out + (((int64_t)kv * n_q + tok) * group + (head - kv * group)) * D + p * 8) = w;
+}
 
 // ---------------------------------------------------------------------------------------
 // Rows' sums, many rows: S^T = K Q^T, a lane has one row and 16 of a tile's keys.  NT tiles of 32 keys stay in registers.  A row's sum over
@@ -186,10 +281,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     there = (uint32_t)scalar((int)there);
     if (there == 0 && !(fresh && ch == w.c1 - 1)) continue;
     const int from = first_query(a, s, fresh ? w.c0 * (32 * NT) : key0) * a.group / 32;
-    for (int b = max(from, w.split * per); b < b1; ++b) {
+    const int b0 = max(from, w.split * per);
+    Query<D> next;
+    if (b0 < b1) next.load(a, s, w.head, b0 * 32 + (lane & 31), n_rows, lane);
+    for (int b = b0; b < b1; ++b) {
       const int row = b * 32 + (lane & 31);
-      Query<D> q;
-      q.load(a, s, w.head, row, n_rows, lane);
+      const Query<D> q = next;
+      next.load(a, s, w.head, row + 32, n_rows, lane);
       const int lim = limit_of(a, s, min(row, n_rows - 1) / a.group);
       const int first = scalar(limit_of(a, s, b * 32 / a.group));      // keys that every row of the block sees
       float ref = kUnset, l = 0.f;
@@ -248,8 +346,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ---------------------------------------------------------------------------------------
-// Rows' sums, up to 32 rows: S = Q K^T, a lane has one key of a tile and 4 RG of the rows, and sums of its own until the piece's end.
-template <Kind K, int D, int RG>
+// Rows' sums, up to 32 rows: S = Q K^T, a lane has one key of a tile and 4 RG of the rows, and sums of its own until the piece's end.  The next
+// tile is on its way, and the page of the one behind it known, while one is computed with.  SCORES: they are kept, so that K is not
+// read again.
+template <Kind K, int D, int RG, bool SCORES>
 __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
   constexpr int R = 4 * RG;
   const int lane = threadIdx.x & 63, h = lane >> 5;
@@ -257,11 +357,16 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
   Seq s;
   if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32, w, s)) return;
   const int n_rows = s.nq * a.group;
-  if (n_rows == 0) return;
-  // blocks of 32 rows (8 RG of which are looked at; more than one block where sequences are of unlike lengths)
+  const int64_t room = (int64_t)a.max_pages << a.page_shift;
+  // 8 RG rows at a time (more than once where sequences are of unlike lengths)
   for (int row0 = 0; row0 < n_rows; row0 += 8 * RG) {
+    Half<K, D> coming;
+    int64_t at = row_of(a, w.seq, w.head, w.c0 * 32 + (lane & 31), s.nk);
+    int64_t at1 = row_of(a, w.seq, w.head, (w.c0 + 1) * 32 + (lane & 31), s.nk);
+    coming.load(a, max(at, (int64_t)0), lane);
     Query<D> q;
     q.load(a, s, w.head, row0 + (lane & 31), n_rows, lane);
+    const int64_t number = row_number(a, w.head, s) + row0;
     float l[R], ref[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -270,24 +375,29 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
     }
     for (int ch = w.c0; ch < w.c1; ++ch) {
       const int key = ch * 32 + (lane & 31);
-      const int64_t at = row_of(a, w.seq, w.head, key, s.nk);
-      if (__builtin_amdgcn_ballot_w64(at >= 0) == 0) continue;
-      Half<K, D> x;
-      x.load(a, max(at, (int64_t)0), lane);
+      const Half<K, D> x = coming;
+      const bool held = at >= 0;
+      at = at1;
+      coming.load(a, max(at, (int64_t)0), lane);
+      at1 = row_of(a, w.seq, w.head, key + 64, s.nk);
+      if (__builtin_amdgcn_ballot_w64(held) == 0) continue;
       bf16x8 kf[D / 16];
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) kf[j] = x.fragment(j);
       const f32x16 y = product<D>(q.f, kf);
       // the lane's key counts for rows from this one on
-      const int from = at >= 0 ? first_query(a, s, key) * a.group - row0 - 4 * h : kNoKey;
-      float v[R], top = 0.f;
+      const int from = held ? first_query(a, s, key) * a.group - row0 - 4 * h : kNoKey;
+      float v[R], p[R];
       bool high = false;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        v[r] = 8 * (r >> 2) + (r & 3) >= from ? y[r] : -INFINITY;
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[r], a.c, -ref[r]));
-        top = l[r] + p;
-        high = high || !(top <= kRaise);
+        const int row = 8 * (r >> 2) + (r & 3);
+        if constexpr (SCORES) {
+          if (key < s.nk && row0 + row + 4 * h < n_rows) a.scores[(number + row + 4 * h) * room + key] = y[r];
+        }
+        v[r] = row >= from ? y[r] : -INFINITY;
+        p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[r], a.c, -ref[r]));
+        high = high || !(l[r] + p[r] <= kRaise);
       }
       if (__builtin_amdgcn_ballot_w64(high) != 0) {
 #pragma unroll
@@ -295,12 +405,13 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
           const float to = fmaxf(ref[r], v[r] * a.c);
           l[r] *= __builtin_amdgcn_exp2f(ref[r] - to);
           ref[r] = to;
+          p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[r], a.c, -to));
         }
       }
 #pragma unroll
-      for (int r = 0; r < R; ++r) l[r] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[r], a.c, -ref[r]));
+      for (int r = 0; r < R; ++r) l[r] += p[r];
     }
-    float2 *part = a.part + (int64_t)w.piece * a.kv_heads * a.n_q * a.group + row_number(a, w.head, s) + row0;
+    float2 *part = a.part + (int64_t)w.piece * a.kv_heads * a.n_q * a.group + number;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float to = ref[r];
@@ -315,6 +426,45 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
   }
 }
 
+// Keys' sums from scores that were kept: four keys to a thread, a workgroup to a unit.
+__global__ __launch_bounds__(256) void k_mass_add(Call a) {
+  Work w;
+  Seq s;
+  if (!find_work(a, (int)blockIdx.x, 1024, w, s)) return;
+  const int n_rows = s.nq * a.group;
+  const int64_t room = (int64_t)a.max_pages << a.page_shift, base = ((int64_t)w.seq * a.kv_heads + w.head) * room, number = row_number(a, w.head, s);
+  for (int ch = w.c0; ch < w.c1; ++ch) {
+    const int64_t key = (int64_t)ch * 1024 + threadIdx.x * 4;
+    if (key >= s.nk) continue;
+    const int id = a.table[(int64_t)w.seq * a.max_pages + (key >> a.page_shift)];
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if ((uint32_t)id < (uint32_t)a.n_pages) {
+      if (a.mass_in) sum = *(const f32x4 *)(a.mass_in + base + key);
+      int from[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) from[e] = first_query(a, s, (int)key + e) * a.group;
+      f32x4 drawn = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int r = 0; r < n_rows; ++r) {
+        const f32x4 v = *(const f32x4 *)(a.scores + (number + r) * room + key);
+        const float2 o = a.stat[number + r];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) drawn[e] += r >= from[e] ? __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], a.c, -o.x)) * o.y : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += drawn[e];
+    }
+    float *p = a.mass + base + key;
+    if (key + 4 <= s.nk) {
+      *(f32x4 *)p = sum;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (key + e < s.nk) p[e] = sum[e];
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------
 // The sums of a row's pieces put together, always in the same order; LANES of them take every LANES-th piece.
 template <int LANES>
@@ -323,7 +473,7 @@ __global__ __launch_bounds__(256) void k_mass_join(Call a, int kc, int side) {
   const int seq = scalar((int)((uint32_t)pair / (uint32_t)a.kv_heads)), head = scalar(pair - seq * a.kv_heads);
   const Seq s = seq_at(a, seq);
   const int n_rows = s.nq * a.group, lane = threadIdx.x % LANES;
-  const int chunks = (int)(((uint32_t)s.nk + kc - 1) / (uint32_t)kc), per = (int)((uint32_t)(chunks + a.pieces - 1) / (uint32_t)a.pieces);
+  const int per = chunks_of_piece(a, s.nk, kc);
   const int64_t all = (int64_t)a.kv_heads * a.n_q * a.group, base = row_number(a, head, s);
   for (int row = turn * (256 / LANES) + threadIdx.x / LANES; row < n_rows; row += side * (256 / LANES)) {
     const int lim = limit_of(a, s, row / a.group);
@@ -347,10 +497,10 @@ __global__ __launch_bounds__(256) void k_mass_join(Call a, int kc, int side) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Keys' sums: S = Q K^T, a lane has one key of each of NT tiles and 4 RG of a block's rows, whose references and divisors are in its
+// Keys' sums, up to 32 rows whose scores are not kept: S = Q K^T, a lane has one key of each of NT tiles and 4 RG of a block's rows, whose references and divisors are in its
 // registers, the same for all lanes of a half.
 template <Kind K, int D, int NT, int RG>
-__global__ __launch_bounds__(256) void k_mass_keys(Call a) {
+__global__ __launch_bounds__(256) void k_mass_keys_few(Call a) {
   constexpr int R = 4 * RG;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   Work w;
@@ -380,10 +530,13 @@ __global__ __launch_bounds__(256) void k_mass_keys(Call a) {
     if (__builtin_amdgcn_ballot_w64(mine != 0) != 0) {
       // (a chunk's last key decides where blocks begin that all its keys are seen by)
       const int all_from = scalar(first_query(a, s, min(key0 + 32 * NT, s.nk) - 1)) * a.group;
-      for (int b = scalar(first_query(a, s, key0)) * a.group / (8 * RG); b * (8 * RG) < n_rows; ++b) {
+      const int b0 = scalar(first_query(a, s, key0)) * a.group / (8 * RG);
+      Query<D> next;
+      if (b0 * (8 * RG) < n_rows) next.load(a, s, w.head, b0 * (8 * RG) + (lane & 31), n_rows, lane);
+      for (int b = b0; b * (8 * RG) < n_rows; ++b) {
         const int row0 = b * (8 * RG);
-        Query<D> q;
-        q.load(a, s, w.head, row0 + (lane & 31), n_rows, lane);
+        const Query<D> q = next;
+        next.load(a, s, w.head, row0 + 8 * RG + (lane & 31), n_rows, lane);
         float ref[R], inv[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -391,23 +544,30 @@ __global__ __launch_bounds__(256) void k_mass_keys(Call a) {
           ref[r] = o.x;
           inv[r] = o.y;
         }
-        const bool cut = row0 < all_from || row0 + 8 * RG > n_rows;
+        if (row0 < all_from || row0 + 8 * RG > n_rows) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const f32x16 x = product<D>(q.f, kf[t]);
-          float p[R];
-#pragma unroll
-          for (int r = 0; r < R; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref[r])) * inv[r];
-          if (cut) {
+          for (int t = 0; t < NT; ++t) {
+            const f32x16 x = product<D>(q.f, kf[t]);
             const int lo = from[t] - row0 - 4 * h, hi = n_rows - row0 - 4 * h;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
               const int i = 8 * (r >> 2) + (r & 3);
-              p[r] = i >= lo && i < hi ? p[r] : 0.f;
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref[r])) * inv[r];
+              acc[t] += i >= lo && i < hi ? p : 0.f;
             }
           }
+        } else {
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[t] += p[r];
+          for (int t = 0; t < NT; ++t) {
+            const f32x16 x = product<D>(q.f, kf[t]);
+            float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; r += 2) {
+              a0 = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref[r])), inv[r], a0);
+              a1 = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[r + 1], a.c, -ref[r + 1])), inv[r + 1], a1);
+            }
+            acc[t] += a0 + a1;
+          }
         }
       }
     }
@@ -423,96 +583,215 @@ __global__ __launch_bounds__(256) void k_mass_keys(Call a) {
   }
 }
 
+// Keys' sums, many rows: S^T = K Q^T as in k_mass_rows, with the rows' references and divisors one to a lane and a sum for each of a lane's 16
+// keys, which the lanes of a half put together when the last row is done.
+template <Kind K, int D, int NT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mass_keys(Call a) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  Work w;
+  Seq s;
+  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32 * NT, w, s)) return;
+  const int n_rows = s.nq * a.group;
+  const float2 *stat = a.stat + row_number(a, w.head, s);
+  const int64_t base = (int64_t)(w.seq * a.kv_heads + w.head) * ((int64_t)a.max_pages << a.page_shift);
+  for (int ch = w.c0; ch < w.c1; ++ch) {
+    const int key0 = ch * (32 * NT);
+    bf16x8 kf[NT][D / 16];
+    f32x16 acc[NT];
+    uint64_t held[NT];      // by lanes, the first 32 of which have a key each
+    uint32_t any = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int64_t row = row_of(a, w.seq, w.head, key0 + t * 32 + (lane & 31), s.nk);
+      held[t] = __builtin_amdgcn_ballot_w64(row >= 0);
+      any |= held[t] ? 1u << t : 0u;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+      Half<K, D> x;
+      x.load(a, max(row, (int64_t)0), lane);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) kf[t][j] = x.fragment(j);
+    }
+    const int b0 = scalar(first_query(a, s, key0)) * a.group / 32;
+    if (any && b0 * 32 < n_rows) {
+      Query<D> next;
+      float2 next_stat = stat[min(b0 * 32 + (lane & 31), n_rows - 1)];
+      next.load(a, s, w.head, b0 * 32 + (lane & 31), n_rows, lane);
+      for (int b = b0; b * 32 < n_rows; ++b) {
+        const int row = b * 32 + (lane & 31);
+        const Query<D> q = next;
+        const float ref = next_stat.x, inv = next_stat.y;
+        next_stat = stat[min(row + 32, n_rows - 1)];
+        next.load(a, s, w.head, row + 32, n_rows, lane);
+        // keys that the lane's row sees, and that every row of the block sees
+        const int lim = row < n_rows ? limit_of(a, s, row / a.group) : 0;
+        const int first = b * 32 + 32 <= n_rows ? scalar(limit_of(a, s, b * 32 / a.group)) : 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (!(any >> t & 1)) continue;
+          const f32x16 x = product<D>(kf[t], q.f);
+          if (key0 + t * 32 + 32 <= first) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref)), inv, acc[t][r]);
+          } else {
+            const int t0 = lim - (key0 + t * 32) - 4 * h;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref)) * inv;
+              acc[t][r] += (r >> 2) * 8 + (r & 3) < t0 ? p : 0.f;
+            }
+          }
+        }
+      }
+    }
+    // over the 32 lanes of a half: at each step a lane gives one half of its sums away and adds the other lane's to the half it keeps, so that
+    // lane r of 16 ends with sum r
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] = acc[t][r];
+#pragma unroll
+      for (int bit = 8; bit > 0; bit >>= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int r = 0; r < bit; ++r) {
+          const float keep = up ? v[r + bit] : v[r], give = up ? v[r] : v[r + bit];
+          v[r] = keep + __shfl_xor(give, bit, 64);
+        }
+      }
+      const float sum = v[0] + __shfl_xor(v[0], 16, 64);
+      const int r = lane & 15, i = 16 * (r >> 3) + 8 * (r >> 2 & 1) + 4 * h + (r & 3), key = key0 + t * 32 + i;
+      if (!(lane & 16) && key < s.nk) {
+        const float had = a.mass_in ? a.mass_in[base + key] : 0.f;
+        a.mass[base + key] = held[t] >> i & 1 ? had + sum : 0.f;
+      }
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------
 namespace {
 
-constexpr int kAim = 4096;                             // waves to aim at: two rounds of eight a CU
-constexpr int64_t kMostParts = (int64_t)1 << 24;       // (row, piece) pairs in the workspace, where rows leave a choice
+constexpr int kAim = 4096;                             // waves of the few rows' kernels: two rounds of eight a CU
+constexpr int kAimMany = 16384;                        // of the many rows', whose chunks are longer work
+constexpr int64_t kMostParts = (int64_t)1 << 25;       // (row, piece) pairs in the workspace, where rows leave a choice
+constexpr int64_t kMostScores = (int64_t)1 << 27;      // scores there
 
 struct Form {
+  bool few, scores;
   int pieces, splits;      // k_mass_rows*
   int key_pieces;          // k_mass_keys
 };
-Form form_of(int n_q, int n_seq, int heads, int kv_heads, int64_t most_keys) {
+// Tokens up to which scores are kept: where writing and reading them is less than reading K again, and they fit.
+int64_t kept_tokens(int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
+  const int64_t row_bytes = dtype == LV_CACHE_BF16 ? 2 * head_dim : dtype == LV_CACHE_E4M3 ? head_dim : head_dim / 2;
+  return std::min(row_bytes / 8 * n_seq / (heads / kv_heads), kMostScores / (most_keys * heads));
+}
+Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   Form f;
   const int64_t pairs = (int64_t)n_seq * kv_heads, rows = std::max((int64_t)n_q, (int64_t)1) * heads;
   const int64_t most = (most_keys + 31) / 32;
-  const int64_t aim = std::max((int64_t)1, std::min((kAim + pairs - 1) / pairs, most));
+  f.few = (double)n_q * (heads / kv_heads) / n_seq <= 32.0;
+  f.scores = n_q <= kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys);
+  const int64_t whole = f.few ? kAim : kAimMany;
+  const int64_t aim = std::max((int64_t)1, std::min((whole + pairs - 1) / pairs, most));
   f.key_pieces = (int)aim;
   f.pieces = (int)std::max((int64_t)1, std::min(aim, kMostParts / rows));
-  f.splits = (int)std::max((int64_t)1, kAim / (pairs * f.pieces));
+  f.splits = (int)std::max((int64_t)1, std::min(whole / (pairs * f.pieces), (int64_t)64));
   return f;
 }
-size_t parts_bytes(int64_t rows, int64_t aim) { return (size_t)std::min(rows * aim, std::max(kMostParts, rows)) * sizeof(float2); }
 
 }  // namespace
 
-size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int64_t most_keys) {
-  const Form f = form_of(n_q, n_seq, heads, kv_heads, most_keys);
-  const int64_t rows = (int64_t)n_q * heads;
-  return align_up(parts_bytes(rows, f.key_pieces), 256) + align_up((size_t)rows * sizeof(float2), 256) + align_up((size_t)rows * head_dim * 2, 256);
+// Parts, divisors, normalised rows, scores: each as much as any call of up to n_q tokens takes, so that scratch for more serves fewer
+static size_t parts_bytes(int64_t rows, int64_t pairs, int64_t most_keys) {
+  const int64_t aim = std::max((int64_t)1, std::min((kAimMany + pairs - 1) / pairs, (most_keys + 31) / 32));
+  return align_up((size_t)std::min(rows * aim, std::max(kMostParts, rows)) * sizeof(float2), 256);
+}
+static size_t plan_bytes(int n_seq) { return n_seq > 64 ? 2 * align_up((size_t)(n_seq + 1) * sizeof(int), 256) : 0; }
+static size_t packed_bytes(int64_t rows, int head_dim) { return align_up((size_t)rows * head_dim * 2, 256); }
+static size_t stat_bytes(int64_t rows) { return align_up((size_t)rows * sizeof(float2), 256); }
+
+size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
+  const int64_t rows = (int64_t)n_q * heads, kept = std::min((int64_t)n_q, kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys));
+  return plan_bytes(n_seq) + parts_bytes(rows, (int64_t)n_seq * kv_heads, most_keys) + stat_bytes(rows) + packed_bytes(rows, head_dim) +
+         align_up((size_t)kept * heads * most_keys * sizeof(float), 256);
 }
 
 template <Kind K, int D>
-static int launch_kind(const MassArgs &x, Call c, const Form &f, hipStream_t st) {
+static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *plan, hipStream_t st) {
   const double rows = (double)x.n_q * c.group / c.n_seq;
   const int64_t pairs = (int64_t)c.n_seq * c.kv_heads;
-  auto grid = [&]() { return dim3((uint32_t)((c.units + 3) / 4)); };
   constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;
-  auto keys = [&]() -> int {
-    c.pieces = f.key_pieces;
-    c.splits = 1;
-    c.units = (int)(pairs * c.pieces);
-    if (rows <= 8.0) k_mass_keys<K, D, 2, 1><<<grid(), 256, 0, st>>>(c);
-    else k_mass_keys<K, D, NK, 4><<<grid(), 256, 0, st>>>(c);
-    LV_HIP_CHECK_LAUNCH();
-    return LV_OK;
-  };
-  c.pieces = f.pieces;
-  int kc = 32;
-  if (x.n_q == 0) return keys();
-  if (rows <= 32.0) {
-    c.splits = 1;
-    c.units = (int)(pairs * c.pieces);
-    if (rows <= 8.0) k_mass_rows_few<K, D, 1><<<grid(), 256, 0, st>>>(c);
-    else k_mass_rows_few<K, D, 4><<<grid(), 256, 0, st>>>(c);
-  } else {
-    kc = 32 * NR;
-    c.splits = f.splits;
-    c.units = (int)(pairs * c.pieces * c.splits);
-    k_mass_rows<K, D, NR><<<grid(), 256, 0, st>>>(c);
+  const bool keep = x.n_q > 0 && f.few && f.scores;
+  const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : 32 * NK;
+  Call by_rows = c, by_keys = c;
+  by_rows.pieces = f.pieces;
+  by_rows.splits = f.splits;
+  by_rows.of_rows = true;
+  by_keys.pieces = f.key_pieces;
+  by_keys.splits = 1;
+  if (c.n_seq > 64) {
+    int *const starts = plan, *const starts_keys = (int *)((char *)plan + plan_bytes(c.n_seq) / 2);
+    k_mass_plan<<<dim3(1), 1024, 0, st>>>(by_rows, by_keys, kc_rows, kc_keys, starts, starts_keys);
+    by_rows.starts = starts;
+    by_keys.starts = starts_keys;
   }
-  const int64_t per_pair = std::max((int64_t)1, kAim / pairs);
-  auto join = [&](auto kernel, int rows_at_once) {
-    const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + rows_at_once - 1) / rows_at_once);
-    kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(c, kc, side);
+  // a wave to a unit
+  auto walk = [&](auto kernel, const Call &y) {
+    kernel<<<dim3((uint32_t)((pairs * y.pieces * y.splits + 3) / 4)), 256, 0, st>>>(y);
   };
-  if (rows <= 64.0) join(k_mass_join<64>, 4);
-  else join(k_mass_join<1>, 256);
-  return keys();
+  const bool eight = rows <= 8.0;
+  if (x.n_q > 0) {
+    if (keep) eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
+    else if (f.few) eight ? walk(k_mass_rows_few<K, D, 1, false>, by_rows) : walk(k_mass_rows_few<K, D, 4, false>, by_rows);
+    else walk(k_mass_rows<K, D, NR>, by_rows);
+    const int64_t per_pair = std::max((int64_t)1, kAim / pairs);
+    auto join = [&](auto kernel, int at_once) {
+      const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
+      kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, kc_rows, side);
+    };
+    if (rows <= 64.0) join(k_mass_join<64>, 4);
+    else join(k_mass_join<1>, 256);
+  }
+  if (keep) k_mass_add<<<dim3((uint32_t)(pairs * by_keys.pieces)), 256, 0, st>>>(by_keys);
+  else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
+  else if (f.few) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
+  else walk(k_mass_keys<K, D, NK>, by_keys);
+  LV_HIP_CHECK_LAUNCH();
+  return LV_OK;
 }
 
 int launch_mass(const MassArgs &x, void *ws, hipStream_t st) {
   const int64_t most = (int64_t)x.cv.max_pages << x.cv.page_shift, rows = (int64_t)x.n_q * x.heads;
-  const Form f = form_of(x.n_q, x.cv.n_seq, x.heads, x.cv.kv_heads, most);
+  const Form f = form_of(x.n_q, x.cv.n_seq, x.heads, x.cv.kv_heads, x.cv.head_dim, x.cv.dtype, most);
   Call c = {};
-  c.part = (float2 *)ws;
-  c.stat = (float2 *)((char *)ws + align_up(parts_bytes(rows, f.key_pieces), 256));
+  char *at = (char *)ws;
+  int *const plan = (int *)at;
+  at += plan_bytes(x.cv.n_seq);
+  c.part = (float2 *)at;
+  at += parts_bytes(rows, (int64_t)x.cv.n_seq * x.cv.kv_heads, most);
+  c.stat = (float2 *)at;
+  at += stat_bytes(rows);
   c.q = x.q;
   c.q_stride = x.q_stride;
-  if (x.qk_norm) {
-    uint16_t *qn = (uint16_t *)((char *)c.stat + align_up((size_t)rows * sizeof(float2), 256));
-    const int rc = launch_norm_rows(x.q, x.q_stride, x.n_q, x.heads, x.cv.head_dim, qn, st);
-    if (rc) return rc;
-    c.q = qn;
-    c.q_stride = (int64_t)x.heads * x.cv.head_dim;
+  c.kv_heads = x.cv.kv_heads;
+  c.group = x.heads / x.cv.kv_heads;
+  if (x.n_q > 0 && (x.qk_norm || !f.few)) {
+    uint16_t *packed = (uint16_t *)at;
+    const uint32_t grid = (uint32_t)((rows * (x.cv.head_dim / 8) + 255) / 256);
+    if (x.cv.head_dim == 64) k_mass_pack<64><<<dim3(grid), 256, 0, st>>>(x.q, x.q_stride, x.n_q, c.kv_heads, c.group, x.qk_norm, packed);
+    else k_mass_pack<128><<<dim3(grid), 256, 0, st>>>(x.q, x.q_stride, x.n_q, c.kv_heads, c.group, x.qk_norm, packed);
+    c.q = packed;
+    c.q_stride = 0;
   }
+  at += packed_bytes(rows, x.cv.head_dim);
+  if (f.scores) c.scores = (float *)at;
   c.q_off = x.q_off;
   c.kv_len = x.kv_len;
   c.n_q = x.n_q;
   c.n_seq = x.cv.n_seq;
-  c.kv_heads = x.cv.kv_heads;
-  c.group = x.heads / x.cv.kv_heads;
   c.frame = x.frame;
   c.c = x.scale * 1.4426950408889634f;
   c.k = (const char *)x.k;
@@ -525,7 +804,7 @@ int launch_mass(const MassArgs &x, void *ws, hipStream_t st) {
   c.mass = x.mass;
   auto by_dim = [&](auto kind) {
     constexpr Kind K = decltype(kind)::value;
-    return x.cv.head_dim == 64 ? launch_kind<K, 64>(x, c, f, st) : launch_kind<K, 128>(x, c, f, st);
+    return x.cv.head_dim == 64 ? launch_kind<K, 64>(x, c, f, plan, st) : launch_kind<K, 128>(x, c, f, plan, st);
   };
   if (x.cv.dtype == LV_CACHE_BF16) return by_dim(std::integral_constant<Kind, Kind::BF16>{});
   if (x.cv.dtype == LV_CACHE_E4M3) return by_dim(std::integral_constant<Kind, Kind::E4M3>{});

@@ -162,3 +162,11 @@ def test_a_stream_in_a_bounded_pool(dtype):
         free += freed[0, :int(count)].tolist()
         assert (table >= 0).sum() <= budget and len(free) + (table >= 0).sum() == n_pages
     assert (table >= 0).sum() == budget and table[0, 0] >= 0 and table[0, -1] >= 0
+
+
+def test_more_columns_than_fit_beside_the_select():
+    rng = np.random.default_rng(10)
+    t = tables(rng, [17000, 20000], 20000, 40000)
+    mass = rng.random((2, 1, 320000)).astype(np.float32)
+    run(t, 40000, 16, [17000 * 16 - 5, 320000], mass, [9000, 19], 2, 2)
+    run(t, 40000, 16, [17000 * 16 - 5, 320000], np.floor(mass * 3), [9000, 1900], 2, 2)

@@ -146,3 +146,26 @@ def test_same_bits_again_in_a_graph_and_with_scratch_of_a_longer_call():
     length.copy_(i32([700, 333]))
     g.replay()
     assert torch.equal(out, outs[0])
+
+
+def test_many_sequences_some_of_them_empty():
+    """More than 64: the units before each are worked out by a kernel of their own."""
+    lens = [(37 * i) % 90 for i in range(300)]
+    new = [min(n, 1 + i % 3) if i % 7 else 0 for i, n in enumerate(lens)]
+    for dtype in ("bf16", "e2m1"):
+        c = Pool(31, lens, heads=2, kv_heads=2, dtype=dtype, frame=1)
+        c.draw(new)
+        c.draw([0] * 300)
+    lens = [(37 * i) % 90 for i in range(70)]
+    Pool(32, lens, heads=2, kv_heads=1, dtype="e4m3", frame=5).draw([min(n, 33 + i) for i, n in enumerate(lens)])
+
+
+def test_no_new_tokens_at_all_in_many_sequences():
+    c = Pool(33, [20] * 1100, heads=1, kv_heads=1, dtype="e2m1")
+    p = c.p
+    had = torch.rand(1100, 1, p.max_pages * 16, device="cuda")
+    out = torch.full_like(had, 5.0)
+    q = torch.empty(0, 1, 64, dtype=torch.bfloat16, device="cuda")
+    ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, 0)).fill_(255)
+    B.litevggt_cached_mass(p, c.d, q, i32([0] * 1101), i32([20] * 1100), had, out, ws)
+    assert torch.equal(out[:, :, :20], had[:, :, :20]) and (out[:, :, 20:] == 5).all()
