@@ -250,7 +250,8 @@ __global__ __launch_bounds__(256) void k_mass_pack(const uint16_t *q, int64_t st
 
 // ---------------------------------------------------------------------------------------
 // Rows' sums, many rows: S^T = K Q^T, a lane has one row and 16 of a tile's keys.  NT tiles of 32 keys stay in registers.  A row's sum over
-// the keys of a wave's piece is kept in `part`: chunks after the first add to it.
+// the keys of a wave's piece is kept in `part`: chunks after the first add to it.  Blocks of rows that do not all see the whole chunk come
+// first; the others look at no position.
 template <Kind K, int D, int NT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mass_rows(Call a) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
@@ -258,9 +259,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   Seq s;
   if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32 * NT, w, s)) return;
   const int n_rows = s.nq * a.group;
-  if (n_rows == 0) return;
   // rows of this split, in blocks of 32, from the first that sees the piece's first key
-  const int blocks = (n_rows + 31) / 32, per = scalar((int)((uint32_t)(blocks + a.splits - 1) / (uint32_t)a.splits));
+  const int blocks = (n_rows + 31) / 32, per = scalar(quotient_up(blocks, a.splits));
   const int b1 = min((w.split + 1) * per, blocks);
   float2 *part = a.part + (int64_t)w.piece * a.kv_heads * a.n_q * a.group + row_number(a, w.head, s);
   bool fresh = true;
@@ -280,34 +280,44 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     there = (uint32_t)scalar((int)there);
     if (there == 0 && !(fresh && ch == w.c1 - 1)) continue;
-    const int from = first_query(a, s, fresh ? w.c0 * (32 * NT) : key0) * a.group / 32;
-    const int b0 = max(from, w.split * per);
+    const int b0 = max(scalar(first_query(a, s, fresh ? w.c0 * (32 * NT) : key0)) * a.group / 32, w.split * per);
+    // the first block whose rows all see the chunk
+    const int end = min(key0 + 32 * NT, s.nk);
+    const int whole = (int)min((uint32_t)(scalar(first_query(a, s, end - 1)) * a.group + 31) / 32u, (uint32_t)blocks);
+    if (b0 >= b1) {
+      fresh = false;
+      continue;
+    }
     Query<D> next;
-    if (b0 < b1) next.load(a, s, w.head, b0 * 32 + (lane & 31), n_rows, lane);
-    for (int b = b0; b < b1; ++b) {
+    next.load(a, s, w.head, b0 * 32 + (lane & 31), n_rows, lane);
+    auto block = [&](auto cut, int b) __attribute__((always_inline)) {
+      constexpr bool kCut = decltype(cut)::value;
       const int row = b * 32 + (lane & 31);
       const Query<D> q = next;
       next.load(a, s, w.head, row + 32, n_rows, lane);
-      const int lim = limit_of(a, s, min(row, n_rows - 1) / a.group);
-      const int first = scalar(limit_of(a, s, b * 32 / a.group));      // keys that every row of the block sees
+      const int lim = kCut ? limit_of(a, s, min(row, n_rows - 1) / a.group) : end;
       float ref = kUnset, l = 0.f;
+
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const uint32_t held = there >> (2 * t) & 3u;
-        if (held == 0) continue;
         f32x16 x = product<D>(kf[t], q.f);
+
+        if (t > 0 && held == 0) continue;
         const int k0 = key0 + t * 32;
-        if (held != 3u || k0 + 32 > first) {
-          const int t0 = lim - (held & 1u ? k0 : kNoKey) - 4 * h, t1 = lim - (held & 2u ? k0 + 16 : kNoKey) - 4 * h;
+        if (kCut || held != 3u || k0 + 32 > end) {
+          int seen = lim;
+          asm volatile("" : "+v"(seen));      // (known ahead of the loop, 128 comparisons would be kept in scalar registers that are not there)
+          const int t0 = seen - (held & 1u ? k0 : kNoKey) - 4 * h, t1 = seen - (held & 2u ? k0 + 16 : kNoKey) - 4 * h;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if ((r >> 2 & 1) * 8 + (r & 3) >= (r < 8 ? t0 : t1)) x[r] = -INFINITY;
         }
         float sum;
         auto weights = [&]() __attribute__((always_inline)) {
-          float s0 = 0.f, s1 = 0.f;
+          float s0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[0], a.c, -ref)), s1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[1], a.c, -ref));
 #pragma unroll
-          for (int r = 0; r < 16; r += 2) {
+          for (int r = 2; r < 16; r += 2) {
             s0 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref));
             s1 += __builtin_amdgcn_exp2f(__builtin_fmaf(x[r + 1], a.c, -ref));
           }
@@ -340,7 +350,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         part[row] = float2{ref, l};
       }
-    }
+    };
+    int b = b0;
+    for (; b < min(whole, b1); ++b) block(std::true_type{}, b);
+    for (; b < b1; ++b) block(std::false_type{}, b);
     fresh = false;
   }
 }
@@ -466,33 +479,56 @@ __global__ __launch_bounds__(256) void k_mass_add(Call a) {
 }
 
 // ---------------------------------------------------------------------------------------
-// The sums of a row's pieces put together, always in the same order; LANES of them take every LANES-th piece.
-template <int LANES>
+// The sums of a row's pieces put together, always in the same order.  ROWS of them to a workgroup (64: a lane each, the pieces by turns to
+// the four waves; 4: a wave each, a lane's pieces 64 apart), four pieces' loads on the way together.
+template <int ROWS>
 __global__ __launch_bounds__(256) void k_mass_join(Call a, int kc, int side) {
+  constexpr int kSlices = 256 / ROWS;
   const int pair = scalar((int)(blockIdx.x / (uint32_t)side)), turn = scalar((int)(blockIdx.x - pair * (uint32_t)side));
   const int seq = scalar((int)((uint32_t)pair / (uint32_t)a.kv_heads)), head = scalar(pair - seq * a.kv_heads);
   const Seq s = seq_at(a, seq);
-  const int n_rows = s.nq * a.group, lane = threadIdx.x % LANES;
+  const int n_rows = s.nq * a.group, mine = ROWS == 64 ? threadIdx.x & 63 : threadIdx.x >> 6, slice = ROWS == 64 ? threadIdx.x >> 6 : threadIdx.x & 63;
   const int per = chunks_of_piece(a, s.nk, kc);
   const int64_t all = (int64_t)a.kv_heads * a.n_q * a.group, base = row_number(a, head, s);
-  for (int row = turn * (256 / LANES) + threadIdx.x / LANES; row < n_rows; row += side * (256 / LANES)) {
+  __shared__ float2 sums[4][64];
+  for (int row0 = turn * ROWS; row0 < n_rows; row0 += side * ROWS) {
+    const int row = min(row0 + mine, n_rows - 1);
     const int lim = limit_of(a, s, row / a.group);
-    const int seen = per ? (int)(((uint32_t)lim + (uint32_t)(per * kc) - 1) / (uint32_t)(per * kc)) : 0;      // pieces that it sees
+    const int seen = per ? quotient_up(lim, per * kc) : 0;      // pieces that it sees
     float ref = kUnset, l = 0.f;
-    for (int p = lane; p < seen; p += LANES) {
-      const float2 o = a.part[p * all + base + row];
-      const float to = fmaxf(ref, o.x);
-      l = l * __builtin_amdgcn_exp2f(ref - to) + o.y * __builtin_amdgcn_exp2f(o.x - to);
+    for (int p0 = slice; p0 < seen; p0 += 4 * kSlices) {
+      float2 o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = a.part[min(p0 + i * kSlices, seen - 1) * all + base + row];
+      float to = ref;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to = fmaxf(to, o[i].x);
+      l *= __builtin_amdgcn_exp2f(ref - to);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l += p0 + i * kSlices < seen ? o[i].y * __builtin_amdgcn_exp2f(o[i].x - to) : 0.f;
       ref = to;
     }
-    if constexpr (LANES == 64) {
+    if constexpr (ROWS == 64) {
+      sums[slice][mine] = float2{ref, l};
+      __syncthreads();
+      if (slice == 0) {
+        float to = ref;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) to = fmaxf(to, sums[i][mine].x);
+        l *= __builtin_amdgcn_exp2f(ref - to);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) l += sums[i][mine].y * __builtin_amdgcn_exp2f(sums[i][mine].x - to);
+        ref = to;
+      }
+      __syncthreads();
+    } else {
       float to = ref;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor(to, o, 64));
       l = wave_sum(l * __builtin_amdgcn_exp2f(ref - to));
       ref = to;
     }
-    if (lane == 0) a.stat[base + row] = float2{ref, l == 0.f ? 0.f : 1.0f / l};
+    if (slice == 0 && row0 + mine < n_rows) a.stat[base + row] = float2{ref, l == 0.f ? 0.f : 1.0f / l};
   }
 }
 
@@ -612,25 +648,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) kf[t][j] = x.fragment(j);
     }
-    const int b0 = scalar(first_query(a, s, key0)) * a.group / 32;
+    const int b0 = scalar(first_query(a, s, key0)) * a.group / 32, blocks = n_rows / 32;      // (whole ones)
     if (any && b0 * 32 < n_rows) {
+      const int whole = (int)min((uint32_t)(scalar(first_query(a, s, min(key0 + 32 * NT, s.nk) - 1)) * a.group + 31) / 32u, (uint32_t)blocks + 1u);
       Query<D> next;
       float2 next_stat = stat[min(b0 * 32 + (lane & 31), n_rows - 1)];
       next.load(a, s, w.head, b0 * 32 + (lane & 31), n_rows, lane);
-      for (int b = b0; b * 32 < n_rows; ++b) {
+      auto block = [&](auto cut, int b) __attribute__((always_inline)) {
         const int row = b * 32 + (lane & 31);
         const Query<D> q = next;
         const float ref = next_stat.x, inv = next_stat.y;
         next_stat = stat[min(row + 32, n_rows - 1)];
         next.load(a, s, w.head, row + 32, n_rows, lane);
-        // keys that the lane's row sees, and that every row of the block sees
-        const int lim = row < n_rows ? limit_of(a, s, row / a.group) : 0;
-        const int first = b * 32 + 32 <= n_rows ? scalar(limit_of(a, s, b * 32 / a.group)) : 0;
+        const int lim = decltype(cut)::value && row < n_rows ? limit_of(a, s, row / a.group) : 0;      // keys that the lane's row sees
+
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          if (!(any >> t & 1)) continue;
           const f32x16 x = product<D>(kf[t], q.f);
-          if (key0 + t * 32 + 32 <= first) {
+
+          if (!(any >> t & 1)) continue;
+          if constexpr (!decltype(cut)::value) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[t][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.c, -ref)), inv, acc[t][r]);
           } else {
@@ -642,24 +679,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
           }
         }
-      }
+      };
+      int b = b0;
+      for (; b < min(whole, blocks); ++b) block(std::true_type{}, b);
+      for (; b < blocks; ++b) block(std::false_type{}, b);
+      if (b * 32 < n_rows) block(std::true_type{}, b);      // (rows beyond the last see nothing)
     }
     // over the 32 lanes of a half: at each step a lane gives one half of its sums away and adds the other lane's to the half it keeps, so that
     // lane r of 16 ends with sum r
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      float v[16];
+      f32x16 v = acc[t];
+      auto halve = [&](auto step) __attribute__((always_inline)) {
+        constexpr int kBit = decltype(step)::value;
+        const bool up = lane & kBit;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) v[r] = acc[t][r];
-#pragma unroll
-      for (int bit = 8; bit > 0; bit >>= 1) {
-        const bool up = lane & bit;
-#pragma unroll
-        for (int r = 0; r < bit; ++r) {
-          const float keep = up ? v[r + bit] : v[r], give = up ? v[r] : v[r + bit];
-          v[r] = keep + __shfl_xor(give, bit, 64);
+        for (int r = 0; r < kBit; ++r) {
+          const float keep = up ? v[r + kBit] : v[r], give = up ? v[r] : v[r + kBit];
+          v[r] = keep + __shfl_xor(give, kBit, 64);
         }
-      }
+      };
+      halve(std::integral_constant<int, 8>{});
+      halve(std::integral_constant<int, 4>{});
+      halve(std::integral_constant<int, 2>{});
+      halve(std::integral_constant<int, 1>{});
       const float sum = v[0] + __shfl_xor(v[0], 16, 64);
       const int r = lane & 15, i = 16 * (r >> 3) + 8 * (r >> 2 & 1) + 4 * h + (r & 3), key = key0 + t * 32 + i;
       if (!(lane & 16) && key < s.nk) {
@@ -674,7 +717,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 namespace {
 
 constexpr int kAim = 4096;                             // waves of the few rows' kernels: two rounds of eight a CU
-constexpr int kAimMany = 16384;                        // of the many rows', whose chunks are longer work
+constexpr int kAimMany = 32768;                        // of the many rows', whose chunks are longer work
 constexpr int64_t kMostParts = (int64_t)1 << 25;       // (row, piece) pairs in the workspace, where rows leave a choice
 constexpr int64_t kMostScores = (int64_t)1 << 27;      // scores there
 
@@ -698,7 +741,9 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtyp
   const int64_t aim = std::max((int64_t)1, std::min((whole + pairs - 1) / pairs, most));
   f.key_pieces = (int)aim;
   f.pieces = (int)std::max((int64_t)1, std::min(aim, kMostParts / rows));
-  f.splits = (int)std::max((int64_t)1, std::min(whole / (pairs * f.pieces), (int64_t)64));
+  // (a unit of many rows: 24 blocks of 32 of them or more, so that what it takes to fetch a chunk is little beside them)
+  const int64_t most_blocks = ((int64_t)n_q * (heads / kv_heads) / n_seq + 31) / 32;
+  f.splits = (int)std::max((int64_t)1, f.few ? (int64_t)1 : std::min(most_blocks / 24, (int64_t)64));
   return f;
 }
 
@@ -752,8 +797,8 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
       const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
       kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, kc_rows, side);
     };
-    if (rows <= 64.0) join(k_mass_join<64>, 4);
-    else join(k_mass_join<1>, 256);
+    if (rows <= 64.0) join(k_mass_join<4>, 4);
+    else join(k_mass_join<64>, 64);
   }
   if (keep) k_mass_add<<<dim3((uint32_t)(pairs * by_keys.pieces)), 256, 0, st>>>(by_keys);
   else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
