@@ -522,8 +522,25 @@ struct Codes<Kv::E2M1, D> {
     using T = Tile<D>;
     const int row = lane / 4, p = kWords * (lane % 4), x = of_v ? T::v_xor(row) : T::k_xor(row);
     const float f = __uint_as_float(e << 23);
+    // In which order a lane writes its pieces: such that the eight lanes that write at once are in different banks
+    const int turn = D == 64 ? row & 1 : (row & 1) * 2 | (lane >> 1 & 1);
+    uint32_t w[kWords];
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) *(u32x4 *)(lds + row * T::kRow + (((p + i) ^ x) * 16)) = dequant8(c[i], f);
+    for (int i = 0; i < kWords; i += 2) {
+      const uint32_t even = c[i], odd = c[i + 1], mask = turn & 1 ? even ^ odd : 0u;
+      w[i] = even ^ mask;
+      w[i + 1] = odd ^ mask;
+    }
+    if constexpr (kWords == 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t mask = turn & 2 ? w[i] ^ w[i + 2] : 0u;
+        w[i] ^= mask;
+        w[i + 2] ^= mask;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) *(u32x4 *)(lds + row * T::kRow + (((p + (i ^ turn)) ^ x) * 16)) = dequant8(w[i], f);
   }
 };
 
