@@ -364,7 +364,8 @@ typedef struct {
 typedef struct {
   void *k, *v;                  /* [n_pages][kv_heads][page_tokens][head_dim] bf16 or E4M3 codes,
                                    [..][head_dim / 2] bytes of E2M1 codes                        */
-  uint8_t *k_scale, *v_scale;   /* E4M3: [n_pages][kv_heads][page_tokens]; E2M1: [..][page_tokens][head_dim / 32] */
+  uint8_t *k_scale, *v_scale;   /* E4M3: [n_pages][kv_heads][page_tokens]; E2M1: [..][page_tokens][head_dim / 32],
+                                   4-byte aligned (k and v: 16-byte aligned)                     */
   const int32_t *page_table;    /* [n_seq][max_pages]                                            */
 } litevggt_cache;
 

@@ -149,6 +149,7 @@ int check_cache_buffers(const litevggt_cache *c, CacheView *cv) {
   if (!c || !c->k || !c->v || !c->page_table) return LV_ERR_NULL;
   if (cv->dtype != LV_CACHE_BF16 && (!c->k_scale || !c->v_scale)) return LV_ERR_NULL;
   if (((uintptr_t)c->k | (uintptr_t)c->v) & 15u) return LV_ERR_SHAPE;
+  if (cv->dtype == LV_CACHE_E2M1 && (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3u)) return LV_ERR_SHAPE;      // (fetched by words)
   cv->table = c->page_table;
   return LV_OK;
 }
@@ -466,7 +467,7 @@ int litevggt_cache_read(const litevggt_cache_params *p, const litevggt_cache *ca
 size_t litevggt_cached_attn_ws_bytes(const litevggt_cache_params *p, int64_t n_tokens) {
   CacheView cv;
   if (check_cache(p, &cv) || n_tokens < 1 || !count_ok(n_tokens, p->heads)) return 0;
-  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.dtype != LV_CACHE_BF16, (int64_t)p->max_pages << cv.page_shift);
+  return kv_attn_ws_bytes((int)n_tokens, p->n_seq, p->heads, p->kv_heads, p->head_dim, cv.dtype, (int64_t)p->max_pages << cv.page_shift);
 }
 
 int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *cache, int64_t n_tokens,
@@ -511,7 +512,7 @@ static int check_cross(const litevggt_cross_params *p) {
 size_t litevggt_cross_attn_ws_bytes(const litevggt_cross_params *p, int64_t n_q, int64_t n_kv) {
   if (check_cross(p) || n_q < 1 || !count_ok(n_q, p->heads) || !count_ok(n_kv, p->kv_heads)) return 0;
   const size_t norm = p->qk_norm ? align_up((size_t)n_kv * p->kv_heads * p->head_dim * 2, 256) : 0;
-  return kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, false, n_kv) + norm;
+  return kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, LV_CACHE_BF16, n_kv) + norm;
 }
 
 int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void *q, int64_t q_stride,
@@ -532,7 +533,7 @@ int litevggt_cross_attn(const litevggt_cross_params *p, int64_t n_q, const void 
   a.k = k;
   a.k_stride = k_stride;
   if (p->qk_norm && n_kv > 0) {
-    uint16_t *kn = (uint16_t *)((char *)ws + kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, false, n_kv));
+    uint16_t *kn = (uint16_t *)((char *)ws + kv_attn_ws_bytes((int)n_q, p->n_seq, p->heads, p->kv_heads, p->head_dim, LV_CACHE_BF16, n_kv));
     if ((rc = launch_norm_rows((const uint16_t *)k, k_stride, (int)n_kv, p->kv_heads, p->head_dim, kn, st))) return rc;
     a.k = kn;
     a.k_stride = kw;

@@ -48,6 +48,8 @@ enum class Kv { ROWS, PAGES, E4M3, E2M1 };
 template <Kv KV> constexpr bool kCoded = KV == Kv::E4M3 || KV == Kv::E2M1;                // codes that become bf16 on their way into LDS
 template <Kv KV, int D> constexpr int kRowBytes = KV == Kv::E2M1 ? D / 2 : KV == Kv::E4M3 ? D : 2 * D;
 
+template <Kv KV, int D, int QB> constexpr int kFewWaves = KV == Kv::E2M1 && D == 64 && QB == 1 ? 3 : 2;      // waves of a SIMD, few rows
+
 // What a kernel needs of the call, by value
 struct Call {
   const uint16_t *q;
@@ -544,10 +546,35 @@ struct Codes<Kv::E2M1, D> {
   }
 };
 
+// E2M1, few rows: codes and scales lie in LDS as they are held, in a ring of kSlots tiles of 32 keys a wave, on their way straight from memory.
+// A slot: K's codes, V's, 256 bytes of K's scales, 256 of V's.
+template <int D>
+struct Ring {
+  static constexpr int kSlots = D == 64 ? 3 : 2, kCodes = 32 * (D / 2), kScales = 32 * (D / 32);      // bytes of a tile's K or V
+  static constexpr int kSlot = 2 * kCodes + 512, kBytes = kSlots * kSlot;
+  static constexpr int kWhole = 2 * (D / 64) + 2, kApart = 8;      // fetches of a tile that lies in one page, and in two
+};
+// fetch_lds of 4 bytes a lane
+__device__ __forceinline__ void fetch_lds4(u32x4 rsrc, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(off),
+               "s"(rsrc)
+               : "memory");
+}
+
 // ---------------------------------------------------------------------------------------
-// QB blocks of 32 rows of a wave
-template <int D, int QB>
-struct Rows {
+// A tile's K as E2M1 codes and scales: of the lane's key (lane % 32) half of the channels, (lane / 32) D / 2 on
+template <int D, bool RAW>
+struct RawKeys {};
+template <int D>
+struct RawKeys<D, true> {
+  u32x4 kw[D / 64];
+  uint32_t ke[D / 64];
+};
+
+// QB blocks of 32 rows of a wave.  RAW: K's fragments come from codes in registers, with the channels in the order in which a lane has them
+// (any order will do that q has as well).
+template <int D, int QB, bool RAW = false>
+struct Rows : RawKeys<D, RAW> {
   bf16x8 q[QB][D / 16];
   f32x16 o[QB][D / 32];     // O^T: a lane's row, channels 32 dt + 8 (r / 4) + 4 h + r % 4
   float l[QB], ref[QB];     // sum of this lane half's weights, the row's reference (both halves the same)
@@ -560,10 +587,10 @@ struct Rows {
     for (int b = 0; b < QB; ++b) {
       const int r = min(first + b * 32 + (lane & 31), n_rows - 1);
       const int i = (int)((uint32_t)r / (uint32_t)a.group), g = r - i * a.group;
-      const uint16_t *p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D + (lane >> 5) * 8;
+      const uint16_t *p = a.q + (int64_t)(s.q0 + i) * a.q_stride + (int64_t)(head * a.group + g) * D + (lane >> 5) * (RAW ? D / 2 : 8);
       u32x4 w[D / 16];
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) w[j] = *(const u32x4 *)(p + 16 * j);
+      for (int j = 0; j < D / 16; ++j) w[j] = *(const u32x4 *)(p + (RAW ? 8 : 16) * j);
       if (a.qk_norm) {
         float ss = 0.f;
 #pragma unroll
@@ -609,8 +636,10 @@ struct Rows {
     {
       bf16x8 kf[D / 16];
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-        kf[j] = __builtin_bit_cast(bf16x8, *(const u32x4 *)(k_lds + kr * T::kRow + (((2 * j + h) ^ T::k_xor(kr)) * 16)));
+      for (int j = 0; j < D / 16; ++j) {
+        if constexpr (RAW) kf[j] = __builtin_bit_cast(bf16x8, dequant8((uint32_t)this->kw[j / 4][j % 4], __uint_as_float(this->ke[j / 4] << 23)));
+        else kf[j] = __builtin_bit_cast(bf16x8, *(const u32x4 *)(k_lds + kr * T::kRow + (((2 * j + h) ^ T::k_xor(kr)) * 16)));
+      }
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
         f32x16 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -737,7 +766,7 @@ struct Rows {
 // join; 32 tokens over 301 to 30,011 keys, 16 heads on 4 of 128, E4M3: 97 us, 5.2 TB/s, and 5 to join.  (Eight waves to a
 // workgroup where there are few of them: 34.1 us against 32.0 for 24 rows over 30,000 keys, 17.2 against 14.4 for 48 over 2000.)
 template <Kv KV, int D, int QB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv_attn_few(Call a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kFewWaves<KV, D, QB>, kFewWaves<KV, D, QB>))) void k_kv_attn_few(Call a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   using T = Tile<D>;
   constexpr int kRows = 32 * QB;
@@ -787,38 +816,123 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
     }
   };
-  if (n > 0) {      // (on its way while the rows come)
-    look_up(0);
-    fetch(0);
-  }
-  Rows<D, QB> rows;
-  rows.load(a, s, w.head, row0, lane);
-  if (n > 0) {
-    uint64_t shut_now = holes;
-    for (int i = 0; i < n; ++i) {
-      char *kt = mine + (i % kStages) * (2 * kTile);
-      int shut = 0;
-      if (KV != Kv::ROWS && (shut_now >> (i & 63) & 1))
-        shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
-      if constexpr (kCoded<KV>) {
+  Rows<D, QB, KV == Kv::E2M1> rows;
+  if constexpr (KV == Kv::E2M1) {
+    using R = Ring<D>;
+    char *const ring = lds + wave * (R::kBytes + kTile), *const vt = ring + R::kBytes;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+    uint32_t there = 0;       // bits 2 slot + g: group g of the slot's tile is held
+    // What is not held arrives as zeros, and its keys are nobody's.  (Scales by words: with the last row's those of the row behind, in the same
+    // page.)  Pages of 32 positions and more: a tile lies in one; else a half of the lanes
+    // takes a group.
+    const bool whole = a.page_shift > 4;
+    auto fetch_raw = [&](int i) __attribute__((always_inline)) {
+      if (i % 64 == 0) look_up(i);
+      const int slot = i % R::kSlots, key = begin + i * 128;
+      const uint32_t to = ring_at + slot * R::kSlot;
+      int id[2], rows_of[2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          kc[g].store(kt + g * kGrp * T::kRow, false, lane);
-          vc[g].store(kt + kTile + g * kGrp * T::kRow, true, lane);
+      for (int g = 0; g < 2; ++g) {
+        id[g] = i < n ? __builtin_amdgcn_readlane(ids[g], i & 63) : -1;
+        rows_of[g] = id[g] < 0 ? 0 : min(end - key - g * kGrp, kGrp);
+      }
+      there = (there & ~(3u << 2 * slot)) | ((id[0] < 0 ? 0u : 1u) | (id[1] < 0 ? 0u : 2u)) << 2 * slot;
+      auto at = [&](int g) __attribute__((always_inline)) {
+        return (((int64_t)max(id[g], 0) * a.kv_heads + w.head) << a.page_shift) + ((key + g * kGrp) & ((1 << a.page_shift) - 1));
+      };
+      if (whole) {
+        const int64_t row = at(0);
+        const int rows = rows_of[0] + rows_of[1];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const u32x4 r = uniform_rsrc((v ? a.v : a.k) + row * (D / 2), rows * (D / 2));
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) fetch_lds(r, x * 1024 + lane * 16, to + v * R::kCodes + x * 1024);
+          fetch_lds4(uniform_rsrc((const char *)(v ? a.v_scale : a.k_scale) + row * (D / 32), (rows * (D / 32) + 3) & ~3), lane * 4, to + 2 * R::kCodes + v * 256);
         }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int64_t row = at(g);
+            const u32x4 r = uniform_rsrc((v ? a.v : a.k) + row * (D / 2), rows_of[g] * (D / 2));
+            const u32x4 rs = uniform_rsrc((const char *)(v ? a.v_scale : a.k_scale) + row * (D / 32), (rows_of[g] * (D / 32) + 3) & ~3);
+            if constexpr (D == 64) {
+              if (lane >> 5 == g) fetch_lds(r, (lane & 31) * 16, to + v * R::kCodes);
+            } else {
+              fetch_lds(r, lane * 16, to + v * R::kCodes + g * 1024);
+            }
+            if (lane / (D / 8) == g) fetch_lds4(rs, lane % (D / 8) * 4, to + 2 * R::kCodes + v * 256);
+          }
       }
-      if (i + 1 < n) {
-        if ((i + 1) % 64 == 0) look_up(i + 1);
-        fetch(i + 1);
-        if constexpr (!kCoded<KV>) wait_vm<4 * T::kFetches>();
-      } else if constexpr (!kCoded<KV>) {
-        wait_vm<0>();
+    };
+    if (n > 0) {
+#pragma unroll
+      for (int i = 0; i < R::kSlots; ++i) fetch_raw(i);
+    }
+    rows.load(a, s, w.head, row0, lane);
+    for (int i = 0; i < n; ++i) {
+      const int slot = i % R::kSlots, kr = lane & 31, h = lane >> 5;
+      const char *const at = ring + slot * R::kSlot, *const scales = at + 2 * R::kCodes;
+      if (whole) wait_vm<(R::kSlots - 1) * R::kWhole>();
+      else wait_vm<(R::kSlots - 1) * R::kApart>();
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) {
+        rows.kw[x] = *(const u32x4 *)(at + kr * (D / 2) + h * (D / 4) + x * 16);
+        rows.ke[x] = *(const uint8_t *)(scales + kr * (D / 32) + h * (D / 64) + x);
       }
+      Codes<KV, D> vc[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) vc[g].c[x] = *(const uint32_t *)(at + R::kCodes + g * (kGrp * D / 2) + lane * (D / 8) + x * 4);
+        vc[g].e = *(const uint8_t *)(scales + 256 + g * (R::kScales / 2) + (D == 64 ? lane / 2 : lane));
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const uint32_t open = there >> 2 * slot & 3u;
+      fetch_raw(i + R::kSlots);
+      if (open == 0) continue;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) vc[g].store(vt + g * kGrp * T::kRow, true, lane);
       const int key0 = begin + i * 128;
-      if (shut != 3)
-        rows.tile(kt, kt + kTile, a.c, shut & 1 ? kNoKey : key0, shut & 2 ? kNoKey : key0 + kGrp, shut || key0 + 32 > first, lane);
+      rows.tile(nullptr, vt, a.c, open & 1u ? key0 : kNoKey, open & 2u ? key0 + kGrp : kNoKey, open != 3u || key0 + 32 > first, lane);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile has been read: its place may be filled again
-      shut_now = holes;
+    }
+    wait_vm<0>();      // nothing may land where the sums will lie
+  } else {
+    if (n > 0) {      // (on its way while the rows come)
+      look_up(0);
+      fetch(0);
+    }
+    rows.load(a, s, w.head, row0, lane);
+    if (n > 0) {
+      uint64_t shut_now = holes;
+      for (int i = 0; i < n; ++i) {
+        char *kt = mine + (i % kStages) * (2 * kTile);
+        int shut = 0;
+        if (KV != Kv::ROWS && (shut_now >> (i & 63) & 1))
+          shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
+        if constexpr (kCoded<KV>) {
+  #pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            kc[g].store(kt + g * kGrp * T::kRow, false, lane);
+            vc[g].store(kt + kTile + g * kGrp * T::kRow, true, lane);
+          }
+        }
+        if (i + 1 < n) {
+          if ((i + 1) % 64 == 0) look_up(i + 1);
+          fetch(i + 1);
+          if constexpr (!kCoded<KV>) wait_vm<4 * T::kFetches>();
+        } else if constexpr (!kCoded<KV>) {
+          wait_vm<0>();
+        }
+        const int key0 = begin + i * 128;
+        if (shut != 3)
+          rows.tile(kt, kt + kTile, a.c, shut & 1 ? kNoKey : key0, shut & 2 ? kNoKey : key0 + kGrp, shut || key0 + 32 > first, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the tile has been read: its place may be filled again
+        shut_now = holes;
+      }
     }
   }
 
@@ -1492,14 +1606,14 @@ struct Form {
 // keys 29 us in blocks of 32 rows, 41 in those of 256; 48 rows 31 us in blocks of 64, 46 of 32, 41 of 256 (over 2000 keys 12.6, 12.1, 17);
 // 100 rows 51 of 64, 84 of 32, 49 of 256.  128 channels, 8 sequences over 4000 keys: 24 rows 54 us in blocks of 32, 61 of 256; 48 rows 90 and 63
 // (64 do not fit the registers).
-Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys) {
+Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   Form f;
   const int group = heads / kv_heads;
   const double rows = (double)n_q * group / n_seq;
   f.few = rows <= (head_dim == 64 ? 64.0 : 32.0);
   f.rows = f.few ? (rows <= 32.0 ? 32 : 64) : 256;
   f.tile = f.few ? 128 : 64;
-  f.resident = kCus * (head_dim == 64 || (f.few && coded) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
+  f.resident = kCus * (f.few && dtype == LV_CACHE_E2M1 ? (head_dim == 64 && f.rows == 32 ? kFewWaves<Kv::E2M1, 64, 1> : 2) : head_dim == 64 || (f.few && dtype != LV_CACHE_BF16) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (Blocks of several sequences that fill the chip four times over are not cut: 32 x 2000 queries over 4000 keys, 16 heads of 64
@@ -1516,14 +1630,14 @@ size_t plan_bytes(int n_seq) { return 256 + (n_seq > 64 ? 2 * align_up((size_t)n
 
 }  // namespace
 
-size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys) {
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   // What the call needs grows with n_q inside a form only.  The size is the largest up to n_q, so that scratch for a
   // longer call serves the shorter ones.
   const int group = heads / kv_heads;
   const int64_t cut = (4 * kCus * (head_dim == 64 ? 2 : 1) - 1) / kv_heads - n_seq;     // most blocks of many rows that are cut (form_of)
   size_t most = 0;
   for (int64_t n : {(int64_t)n_q, (int64_t)32 * n_seq / group, (int64_t)64 * n_seq / group, (256 * cut + 255) / group})
-    if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, coded, most_keys), head_dim));
+    if (n > 0 && n <= n_q) most = std::max(most, sums_bytes(form_of((int)n, n_seq, heads, kv_heads, head_dim, dtype, most_keys), head_dim));
   return most || n_seq > 64 ? plan_bytes(n_seq) + most : 0;
 }
 
@@ -1545,7 +1659,7 @@ static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t 
   constexpr size_t tile = 64 * D * 2 * 2;      // 64 keys of K and V as bf16
   static std::atomic<uint64_t> d0{0}, d1{0}, d2{0};
   // (the ring of four waves' tiles, and room for their sums at the end)
-  constexpr size_t ring = kCoded<KV> ? 2 * tile : 4 * tile, sums = 4 * 32 * D * sizeof(float);
+  constexpr size_t ring = KV == Kv::E2M1 ? 4 * (Ring<D>::kBytes + tile / 4) : kCoded<KV> ? 2 * tile : 4 * tile, sums = 4 * 32 * D * sizeof(float);
   if (f.few && f.rows == 32) return go(k_kv_attn_few<KV, D, 1>, d0, std::integral_constant<size_t, std::max(ring, sums)>{}, c, grid, 256, st);
   if constexpr (D == 64)
     if (f.few) return go(k_kv_attn_few<KV, D, 2>, d1, std::integral_constant<size_t, std::max(ring, 2 * sums)>{}, c, grid, 256, st);
@@ -1555,7 +1669,7 @@ static int launch_form(const Form &f, const Call &c, uint32_t grid, hipStream_t 
 
 int launch_kv_attn(const KvAttnArgs &x, void *ws, hipStream_t st) {
   const int64_t most = x.paged ? (int64_t)x.cv.max_pages << x.cv.page_shift : x.n_kv;
-  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, x.paged && x.cv.dtype != LV_CACHE_BF16, most);
+  const Form f = form_of(x.n_q, x.n_seq, x.heads, x.kv_heads, x.head_dim, x.paged ? x.cv.dtype : LV_CACHE_BF16, most);
   Call c;
   c.q = x.q;
   c.o = x.o;

@@ -156,7 +156,7 @@ struct KvAttnArgs {
   CacheView cv;
   const uint8_t *k_scale, *v_scale;
 };
-size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, bool coded, int64_t most_keys);
+size_t kv_attn_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys);
 int launch_kv_attn(const KvAttnArgs &a, void *ws, hipStream_t st);
 // k normalised per head (row stride in elements) into rows of kv_heads * head_dim
 int launch_norm_rows(const uint16_t *k, int64_t k_stride, int n, int kv_heads, int head_dim, uint16_t *out, hipStream_t st);

@@ -50,6 +50,9 @@ def test_e2m1_needs_scales():
         assert L.litevggt_cache_write(C.byref(p), C.byref(c), 5, P, 128, P, 128, P, P, None) == NULL
         assert L.litevggt_cache_read(C.byref(p), C.byref(c), P, P, 5, P, 128, P, 128, None) == NULL
         assert L.litevggt_cached_attn(C.byref(p), C.byref(c), 5, P, 256, P, P, P, 256, P, 1 << 40, None) == NULL
+    for name in ("k_scale", "v_scale"):
+        c = cache(**{name: P + 2})
+        assert L.litevggt_cached_attn(C.byref(p), C.byref(c), 5, P, 256, P, P, P, 256, P, 1 << 40, None) == SHAPE
     for bad in (2, 3, 5, -1):
         assert mass(params(cache_dtype=bad)) == evict(params(cache_dtype=bad)) == DTYPE
 
