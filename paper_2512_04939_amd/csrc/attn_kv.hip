@@ -48,7 +48,7 @@ enum class Kv { ROWS, PAGES, E4M3, E2M1 };
 template <Kv KV> constexpr bool kCoded = KV == Kv::E4M3 || KV == Kv::E2M1;                // codes that become bf16 on their way into LDS
 template <Kv KV, int D> constexpr int kRowBytes = KV == Kv::E2M1 ? D / 2 : KV == Kv::E4M3 ? D : 2 * D;
 
-template <Kv KV, int D, int QB> constexpr int kFewWaves = KV == Kv::E2M1 && D == 64 && QB == 1 ? 3 : 2;      // waves of a SIMD, few rows
+template <Kv KV, int D, int QB> constexpr int kFewWaves = KV == Kv::E2M1 && D == 64 && QB == 1 ? 4 : 2;      // waves of a SIMD, few rows
 
 // What a kernel needs of the call, by value
 struct Call {
@@ -550,7 +550,7 @@ struct Codes<Kv::E2M1, D> {
 // A slot: K's codes, V's, 256 bytes of K's scales, 256 of V's.
 template <int D>
 struct Ring {
-  static constexpr int kSlots = D == 64 ? 3 : 2, kCodes = 32 * (D / 2), kScales = 32 * (D / 32);      // bytes of a tile's K or V
+  static constexpr int kSlots = 2, kCodes = 32 * (D / 2), kScales = 32 * (D / 32);      // bytes of a tile's K or V
   static constexpr int kSlot = 2 * kCodes + 512, kBytes = kSlots * kSlot;
   static constexpr int kWhole = 2 * (D / 64) + 2, kApart = 8;      // fetches of a tile that lies in one page, and in two
 };

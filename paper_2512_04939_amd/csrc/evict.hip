@@ -14,7 +14,8 @@ namespace {
 
 constexpr int kSpan = 256;       // positions that a workgroup sums at a time
 constexpr int kBins = 2048;
-constexpr int kList = 512;       // keys that are compared one by one
+constexpr int kList = 128;       // keys that are compared one by one
+constexpr int kOwnSums = 128;    // masses of a page (heads times positions) up to which k_evict_select sums them by itself, a thread to a page
 constexpr int kLdsKeys = 16384;  // columns whose keys lie in LDS
 
 __device__ __forceinline__ int used_columns(const EvictArgs &a, int s) {
@@ -80,8 +81,8 @@ __device__ __forceinline__ uint64_t higher(uint64_t a, uint64_t b) { return a > 
 
 }  // namespace
 
-// LDS: the keys lie there and not in the workspace
-template <bool LDS>
+// LDS: the keys lie there and not in the workspace.  OWN: it sums the masses itself.
+template <bool LDS, bool OWN>
 __global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, const double *sums, uint64_t *room) {
   extern __shared__ uint64_t keys_lds[];
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -95,23 +96,51 @@ __global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, const double
   __shared__ uint64_t ends[16][2], list[kList], at_last;
   const int lo_col = min(a.first_pages, used), hi_col = max(used - min(a.last_pages, used), lo_col);
 
-  // keys of the pages that may leave (all bits set: may not), how many these are, how many are held, the least and the largest key
+  // keys of the pages that may leave (all bits set: may not), how many these are, how many are held, the least and the largest key.  Four
+  // columns' loads are on the way together.
   int held = 0, open = 0;
   uint64_t lo = ~(uint64_t)0, hi = 0;
-  for (int j = tid; j < used; j += 1024) {
-    const bool is_held = (uint32_t)table[j] < (uint32_t)a.n_pages, is_open = is_held && j >= lo_col && j < hi_col;
-    uint64_t k = ~(uint64_t)0;
-    held += is_held;
-    if (is_open) {
-      double sum = sums[(int64_t)j * per];
-      for (int i = 1; i < per; ++i)
-        if (((int64_t)j << a.page_shift) + i * kSpan < len) sum += sums[(int64_t)j * per + i];
-      k = key_of(sum);
-      lo = lower(lo, k);
-      hi = higher(hi, k);
-      ++open;
+  for (int j0 = tid; j0 < used; j0 += 4 * 1024) {
+    int ids[4];
+    double mass[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = min(j0 + i * 1024, used - 1);
+      ids[i] = table[j];
+      if constexpr (!OWN) mass[i] = sums[(int64_t)j * per];
     }
-    keys[j] = k;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = j0 + i * 1024;
+      if (j >= used) break;
+      const bool is_held = (uint32_t)ids[i] < (uint32_t)a.n_pages, is_open = is_held && j >= lo_col && j < hi_col;
+      uint64_t k = ~(uint64_t)0;
+      held += is_held;
+      if (is_open) {
+        double sum = 0.0;
+        if constexpr (OWN) {
+          const int64_t room = (int64_t)a.max_pages << a.page_shift, first = (int64_t)j << a.page_shift;
+          const int n = (int)min(len - first, (int64_t)1 << a.page_shift);
+          for (int h = 0; h < a.kv_heads; ++h) {
+            const float *p = a.mass + ((int64_t)s * a.kv_heads + h) * room + first;
+#pragma unroll 4
+            for (int x = 0; x < 1 << a.page_shift; x += 4) {
+              const f32x4 v = *(const f32x4 *)(p + x);
+              sum += ((x < n ? (double)v.x : 0.0) + (x + 1 < n ? (double)v.y : 0.0)) + ((x + 2 < n ? (double)v.z : 0.0) + (x + 3 < n ? (double)v.w : 0.0));
+            }
+          }
+        } else {
+          sum = mass[i];
+          for (int x = 1; x < per; ++x)
+            if (((int64_t)j << a.page_shift) + x * kSpan < len) sum += sums[(int64_t)j * per + x];
+        }
+        k = key_of(sum);
+        lo = lower(lo, k);
+        hi = higher(hi, k);
+        ++open;
+      }
+      keys[j] = k;
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -217,18 +246,22 @@ __global__ __launch_bounds__(1024) void k_evict_select(EvictArgs a, const double
       tied += counts[i][1];
     }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (int j = j0 + lane; j < j0 + run; j += 64) {
-      const uint64_t k = j < used ? keys[j] : ~(uint64_t)0;
-      const uint64_t equal = __builtin_amdgcn_ballot_w64(k == lo);
-      const bool leaves = k < lo || (k == lo && tied + __popcll(equal & below) < ties);
-      const uint64_t out = __builtin_amdgcn_ballot_w64(leaves);
-      if (j < used) {
-        const int id = from[j];
-        if (leaves) freed[gone + __popcll(out & below)] = id;
-        to[j] = leaves ? -1 : id;
+    for (int jj = j0 + lane; jj < j0 + run; jj += 4 * 64) {
+      int ids[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ids[i] = from[min(jj + i * 64, used - 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = jj + i * 64;
+        const uint64_t k = j < min(j0 + run, used) ? keys[j] : ~(uint64_t)0;
+        const uint64_t equal = __builtin_amdgcn_ballot_w64(k == lo);
+        const bool leaves = k < lo || (k == lo && tied + __popcll(equal & below) < ties);
+        const uint64_t out = __builtin_amdgcn_ballot_w64(leaves);
+        if (leaves) freed[gone + __popcll(out & below)] = ids[i];
+        if (j < min(j0 + run, used)) to[j] = leaves ? -1 : ids[i];
+        tied += __popcll(equal);
+        gone += __popcll(out);
       }
-      tied += __popcll(equal);
-      gone += __popcll(out);
     }
   }
   for (int j = (leave > 0 ? used : 0) + tid; j < a.max_pages; j += 1024) to[j] = from[j];
@@ -245,17 +278,22 @@ int launch_evict(const EvictArgs &a, void *ws, hipStream_t st) {
   const int per = std::max(1 << a.page_shift >> 8, 1);
   double *sums = (double *)ws;
   uint64_t *keys = (uint64_t *)((char *)ws + align_up((size_t)a.n_seq * a.max_pages * per * sizeof(double), 256));
-  const int64_t spans = (((int64_t)a.max_pages << a.page_shift) + kSpan - 1) / kSpan;
-  const int side = (int)std::max((int64_t)1, std::min(spans, (int64_t)(8192 / a.n_seq)));
-  k_evict_sums<<<dim3((uint32_t)(side * (int64_t)a.n_seq)), 256, 0, st>>>(a, sums, side);
-  if (a.max_pages <= kLdsKeys) {
+  const bool own = a.max_pages <= 1024 && (a.kv_heads << a.page_shift) <= kOwnSums;
+  if (!own) {
+    const int64_t spans = (((int64_t)a.max_pages << a.page_shift) + kSpan - 1) / kSpan;
+    const int side = (int)std::max((int64_t)1, std::min(spans, (int64_t)(8192 / a.n_seq)));
+    k_evict_sums<<<dim3((uint32_t)(side * (int64_t)a.n_seq)), 256, 0, st>>>(a, sums, side);
+  }
+  const size_t lds = (size_t)a.max_pages * sizeof(uint64_t);
+  if (own) {
+    k_evict_select<true, true><<<dim3((uint32_t)a.n_seq), 1024, lds, st>>>(a, sums, keys);
+  } else if (a.max_pages <= kLdsKeys) {
     static std::atomic<uint64_t> done{0};
-    const size_t lds = (size_t)a.max_pages * sizeof(uint64_t);
-    const int rc = allow_dynamic_lds<kLdsKeys * sizeof(uint64_t)>((const void *)k_evict_select<true>, done);
+    const int rc = allow_dynamic_lds<kLdsKeys * sizeof(uint64_t)>((const void *)k_evict_select<true, false>, done);
     if (rc) return rc;
-    k_evict_select<true><<<dim3((uint32_t)a.n_seq), 1024, lds, st>>>(a, sums, keys);
+    k_evict_select<true, false><<<dim3((uint32_t)a.n_seq), 1024, lds, st>>>(a, sums, keys);
   } else {
-    k_evict_select<false><<<dim3((uint32_t)a.n_seq), 1024, 0, st>>>(a, sums, keys);
+    k_evict_select<false, false><<<dim3((uint32_t)a.n_seq), 1024, 0, st>>>(a, sums, keys);
   }
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;

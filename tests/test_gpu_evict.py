@@ -170,3 +170,17 @@ def test_more_columns_than_fit_beside_the_select():
     mass = rng.random((2, 1, 320000)).astype(np.float32)
     run(t, 40000, 16, [17000 * 16 - 5, 320000], mass, [9000, 19], 2, 2)
     run(t, 40000, 16, [17000 * 16 - 5, 320000], np.floor(mass * 3), [9000, 1900], 2, 2)
+
+
+@pytest.mark.parametrize("heads,page", [(1, 16), (4, 16), (8, 16), (9, 16), (2, 64), (1, 128)])
+def test_short_caches(heads, page):
+    """Pages of few masses, which one kernel sums and selects, and the next sizes, which two do."""
+    rng = np.random.default_rng(heads * page)
+    for pages in ([1, 5, 0], [300, 1024], [1025]):
+        t = tables(rng, pages, max(pages), sum(pages))
+        lens = [max(0, c * page - int(rng.integers(0, page))) for c in pages]
+        mass = np.floor(rng.random((len(pages), heads, max(pages) * page)) * 3).astype(np.float32)
+        for s, n in enumerate(lens):
+            mass[s, :, n:] = np.nan
+        run(t, sum(pages), page, lens, mass, [c // 2 for c in pages], 0, 1)
+        run(t, sum(pages), page, lens, mass, [c // 2 for c in pages], 1, 0, in_place=True)
