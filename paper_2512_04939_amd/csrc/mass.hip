@@ -42,6 +42,7 @@ struct Call {
   float *mass;
   float2 *part;            // [piece][kv head][token, head of the group]: reference, sum of weights
   float2 *stat;            // [kv head][token, head of the group]: reference, 1 / sum of weights
+  int row_pieces;          // k_mass_add: `pieces` of the rows' sums
   float *scores;           // [kv head][token, head of the group][position], where there are few rows; else null
 };
 
@@ -439,34 +440,62 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
   }
 }
 
-// Keys' sums from scores that were kept: four keys to a thread, a workgroup to a unit.
+// Keys' sums from scores that were kept: four keys to a thread, a workgroup to a unit.  OWN: the pieces of 64 rows at a time are put together by
+// every workgroup for itself (a wave to a row, its lanes to the pieces), which is less than another launch where there are few of them
+// (5 rows over 137,405 positions, 2147 workgroups: 21 us so, 17 with the launch).
+template <bool OWN>
 __global__ __launch_bounds__(256) void k_mass_add(Call a) {
   Work w;
   Seq s;
   if (!find_work(a, (int)blockIdx.x, 1024, w, s)) return;
-  const int n_rows = s.nq * a.group;
+  const int n_rows = s.nq * a.group, lane = threadIdx.x & 63, wave = scalar((int)(threadIdx.x >> 6));
   const int64_t room = (int64_t)a.max_pages << a.page_shift, base = ((int64_t)w.seq * a.kv_heads + w.head) * room, number = row_number(a, w.head, s);
+  const int64_t all = (int64_t)a.kv_heads * a.n_q * a.group;
+  const int of_piece = quotient_up(quotient_up(s.nk, 32), a.row_pieces) * 32;      // keys
+  __shared__ float2 stat[64];
   for (int ch = w.c0; ch < w.c1; ++ch) {
     const int64_t key = (int64_t)ch * 1024 + threadIdx.x * 4;
-    if (key >= s.nk) continue;
-    const int id = a.table[(int64_t)w.seq * a.max_pages + (key >> a.page_shift)];
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if ((uint32_t)id < (uint32_t)a.n_pages) {
-      if (a.mass_in) sum = *(const f32x4 *)(a.mass_in + base + key);
-      int from[4];
+    const int id = key < s.nk ? a.table[(int64_t)w.seq * a.max_pages + (key >> a.page_shift)] : -1;
+    const bool held = (uint32_t)id < (uint32_t)a.n_pages;
+    int from[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) from[e] = first_query(a, s, (int)key + e) * a.group;
-      f32x4 drawn = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int r = 0; r < n_rows; ++r) {
-        const f32x4 v = *(const f32x4 *)(a.scores + (number + r) * room + key);
-        const float2 o = a.stat[number + r];
+    for (int e = 0; e < 4; ++e) from[e] = first_query(a, s, (int)min(key, (int64_t)s.nk) + e) * a.group;
+    f32x4 had = {0.f, 0.f, 0.f, 0.f}, drawn = {0.f, 0.f, 0.f, 0.f};
+    if (held && a.mass_in) had = *(const f32x4 *)(a.mass_in + base + key);
+    for (int r0 = 0; r0 < n_rows; r0 += 64) {
+      const int rows = min(n_rows - r0, 64);
+      if (OWN && (n_rows > 64 || ch == w.c0)) {      // (the same for all)
+        __syncthreads();
+        for (int r = wave; r < rows; r += 4) {
+          const int seen = quotient_up(limit_of(a, s, (r0 + r) / a.group), of_piece);
+          float ref = kUnset, l = 0.f;
+          for (int p = lane; p < seen; p += 64) {
+            const float2 o = a.part[p * all + number + r0 + r];
+            const float to = fmaxf(ref, o.x);
+            l = l * __builtin_amdgcn_exp2f(ref - to) + o.y * __builtin_amdgcn_exp2f(o.x - to);
+            ref = to;
+          }
+          float to = ref;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) drawn[e] += r >= from[e] ? __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], a.c, -o.x)) * o.y : 0.f;
+          for (int o = 32; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor(to, o, 64));
+          l = wave_sum(l * __builtin_amdgcn_exp2f(ref - to));
+          if (lane == 0) stat[r] = float2{to, l == 0.f ? 0.f : 1.0f / l};
+        }
+        __syncthreads();
       }
+      if (held) {
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+          const f32x4 v = *(const f32x4 *)(a.scores + (number + r0 + r) * room + key);
+          const float2 o = OWN ? stat[r] : a.stat[number + r0 + r];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += drawn[e];
+          for (int e = 0; e < 4; ++e) drawn[e] += r0 + r >= from[e] ? __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], a.c, -o.x)) * o.y : 0.f;
+        }
+      }
     }
+    f32x4 sum;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = had[e] + drawn[e];
     float *p = a.mass + base + key;
     if (key + 4 <= s.nk) {
       *(f32x4 *)p = sum;
@@ -771,6 +800,9 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
   constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;
   const bool keep = x.n_q > 0 && f.few && f.scores;
   const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : 32 * NK;
+  // keys' units at most, where a workgroup takes one; as many as there are CUs or fewer join their rows themselves
+  const int64_t most_blocks = (((int64_t)c.max_pages << c.page_shift) + 1023) / 1024;
+  const bool own = keep && pairs * most_blocks <= 256;
   Call by_rows = c, by_keys = c;
   by_rows.pieces = f.pieces;
   by_rows.splits = f.splits;
@@ -792,15 +824,17 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
     if (keep) eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
     else if (f.few) eight ? walk(k_mass_rows_few<K, D, 1, false>, by_rows) : walk(k_mass_rows_few<K, D, 4, false>, by_rows);
     else walk(k_mass_rows<K, D, NR>, by_rows);
+    by_keys.row_pieces = f.pieces;
     const int64_t per_pair = std::max((int64_t)1, kAim / pairs);
     auto join = [&](auto kernel, int at_once) {
       const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
       kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, kc_rows, side);
     };
-    if (rows <= 64.0) join(k_mass_join<4>, 4);
-    else join(k_mass_join<64>, 64);
+    if (!own) rows <= 64.0 ? join(k_mass_join<4>, 4) : join(k_mass_join<64>, 64);
   }
-  if (keep) k_mass_add<<<dim3((uint32_t)(pairs * by_keys.pieces)), 256, 0, st>>>(by_keys);
+  const dim3 blocks((uint32_t)(pairs * std::min((int64_t)by_keys.pieces, most_blocks)));
+  if (own) k_mass_add<true><<<blocks, 256, 0, st>>>(by_keys);
+  else if (keep) k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
   else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
   else if (f.few) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
   else walk(k_mass_keys<K, D, NK>, by_keys);

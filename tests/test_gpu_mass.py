@@ -169,3 +169,11 @@ def test_no_new_tokens_at_all_in_many_sequences():
     ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, 0)).fill_(255)
     B.litevggt_cached_mass(p, c.d, q, i32([0] * 1101), i32([20] * 1100), had, out, ws)
     assert torch.equal(out[:, :, :20], had[:, :, :20]) and (out[:, :, 20:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_one_sequence_with_many_rows_among_those_of_few(dtype):
+    """The average chooses the form: a sequence of 200 rows where the others have one."""
+    lens = [300] + [40] * 40
+    Pool(34, lens, heads=4, kv_heads=2, dtype=dtype, frame=1).draw([100] + [1] * 40)
+    Pool(35, lens, heads=2, kv_heads=2, dtype=dtype, holes=[(0, 5)]).draw([150] + [0, 1] * 20)
