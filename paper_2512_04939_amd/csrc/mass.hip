@@ -747,11 +747,12 @@ namespace {
 
 constexpr int kAim = 4096;                             // waves of the few rows' kernels: two rounds of eight a CU
 constexpr int kAimMany = 32768;                        // of the many rows', whose chunks are longer work
+constexpr int kUnits = 6144;                           // three rounds of two waves a SIMD
 constexpr int64_t kMostParts = (int64_t)1 << 25;       // (row, piece) pairs in the workspace, where rows leave a choice
 constexpr int64_t kMostScores = (int64_t)1 << 27;      // scores there
 
 struct Form {
-  bool few, scores;
+  bool few, scores, small_chunks;
   int pieces, splits;      // k_mass_rows*
   int key_pieces;          // k_mass_keys
 };
@@ -770,9 +771,12 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtyp
   const int64_t aim = std::max((int64_t)1, std::min((whole + pairs - 1) / pairs, most));
   f.key_pieces = (int)aim;
   f.pieces = (int)std::max((int64_t)1, std::min(aim, kMostParts / rows));
-  // (a unit of many rows: 24 blocks of 32 of them or more, so that what it takes to fetch a chunk is little beside them)
-  const int64_t most_blocks = ((int64_t)n_q * (heads / kv_heads) / n_seq + 31) / 32;
-  f.splits = (int)std::max((int64_t)1, f.few ? (int64_t)1 : std::min(most_blocks / 24, (int64_t)64));
+  // Many rows: where the chunks are too few to fill the chip a few times over, rows are split too, down to four blocks of 32.  (The sums by
+  // keys cannot be: they take chunks of 32 keys then.)
+  const int64_t blocks = ((int64_t)n_q * (heads / kv_heads) / n_seq + 31) / 32, chunk = head_dim == 64 ? 256 : 128;
+  const int64_t units = pairs * std::min((int64_t)f.pieces, (most_keys + chunk - 1) / chunk);
+  f.splits = f.few ? 1 : (int)std::max((int64_t)1, std::min(std::min((kUnits + units - 1) / units, blocks / 4), (int64_t)64));
+  f.small_chunks = pairs * ((most_keys + chunk / 2 - 1) / (chunk / 2)) < kUnits / 4;
   return f;
 }
 
@@ -799,7 +803,7 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
   const int64_t pairs = (int64_t)c.n_seq * c.kv_heads;
   constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;
   const bool keep = x.n_q > 0 && f.few && f.scores;
-  const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : 32 * NK;
+  const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : f.small_chunks ? 32 : 32 * NK;
   // keys' units at most, where a workgroup takes one; as many as there are CUs or fewer join their rows themselves
   const int64_t most_blocks = (((int64_t)c.max_pages << c.page_shift) + 1023) / 1024;
   const bool own = keep && pairs * most_blocks <= 256;
@@ -837,6 +841,7 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
   else if (keep) k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
   else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
   else if (f.few) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
+  else if (f.small_chunks) walk(k_mass_keys<K, D, 1>, by_keys);
   else walk(k_mass_keys<K, D, NK>, by_keys);
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
