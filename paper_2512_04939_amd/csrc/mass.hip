@@ -724,8 +724,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const bool up = lane & kBit;
 #pragma unroll
         for (int r = 0; r < kBit; ++r) {
-          const float keep = up ? v[r + kBit] : v[r], give = up ? v[r] : v[r + kBit];
-          v[r] = keep + __shfl_xor(give, kBit, 64);
+          float low = v[r], high = v[r + kBit];
+          asm("" : "+v"(low), "+v"(high));      // (else one is taken by an index that the lane chooses: sixteen selections)
+          v[r] = (up ? high : low) + __shfl_xor(up ? low : high, kBit, 64);
         }
       };
       halve(std::integral_constant<int, 8>{});
