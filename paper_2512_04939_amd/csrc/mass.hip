@@ -426,17 +426,42 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
       for (int r = 0; r < R; ++r) l[r] += p[r];
     }
     float2 *part = a.part + (int64_t)w.piece * a.kv_heads * a.n_q * a.group + number;
+    // over the 32 lanes of a half: at each step a lane gives half of its rows away and takes the other lane's share of the half it keeps, until
+    // lane r has row r of R; then the lanes that have the same row
+    auto join = [&](int r, float other, float sum) __attribute__((always_inline)) {
+      const float to = fmaxf(ref[r], other);
+      l[r] = l[r] * __builtin_amdgcn_exp2f(ref[r] - to) + sum * __builtin_amdgcn_exp2f(other - to);
+      ref[r] = to;
+    };
+    auto halve = [&](auto step) __attribute__((always_inline)) {
+      constexpr int kBit = decltype(step)::value;
+      const bool up = lane & kBit;
+      if constexpr (kBit < R) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float to = ref[r];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor(to, o, 64));
-      float sum = l[r] * __builtin_amdgcn_exp2f(ref[r] - to);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-      const int row = 8 * (r >> 2) + (r & 3) + 4 * h;
-      if ((lane & 31) == 0 && row0 + row < n_rows) part[row] = float2{to, sum};
+        for (int r = 0; r < kBit; ++r) {
+          float a0 = ref[r], a1 = ref[r + kBit], b0 = l[r], b1 = l[r + kBit];
+          asm("" : "+v"(a0), "+v"(a1), "+v"(b0), "+v"(b1));
+          ref[r] = up ? a1 : a0;
+          l[r] = up ? b1 : b0;
+          join(r, __shfl_xor(up ? a0 : a1, kBit, 64), __shfl_xor(up ? b0 : b1, kBit, 64));
+        }
+      } else {
+        join(0, __shfl_xor(ref[0], kBit, 64), __shfl_xor(l[0], kBit, 64));
+      }
+    };
+    if constexpr (R == 16) {
+      halve(std::integral_constant<int, 8>{});
+      halve(std::integral_constant<int, 4>{});
     }
+    halve(std::integral_constant<int, 2>{});
+    halve(std::integral_constant<int, 1>{});
+    if constexpr (R == 4) {
+      halve(std::integral_constant<int, 4>{});
+      halve(std::integral_constant<int, 8>{});
+    }
+    halve(std::integral_constant<int, 16>{});
+    const int r = lane & (R - 1), row = 8 * (r >> 2) + (r & 3) + 4 * h;
+    if ((lane & 31) < R && row0 + row < n_rows) part[row] = float2{ref[0], l[0]};
   }
 }
 
