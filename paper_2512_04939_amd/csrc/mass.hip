@@ -25,6 +25,16 @@ constexpr int kNoKey = 0x7fff0000;           // the position of a key that is no
 
 enum class Kind { BF16, E4M3, E2M1 };
 
+// How the keys of a call are cut: into chunks of so many, and these into pieces, about `aim` of them in all, so that pieces of sequences with
+// many rows are shorter and all take about as long
+struct Cut {
+  int chunk, aim;
+  int most;                // pieces of a sequence
+  int block;               // rows that a wave takes at a time
+  bool of_rows;            // sequences without queries have no pieces
+  const int *starts;       // more than 64 sequences: units before each, in all, and the work of a piece (k_mass_plan); else null
+};
+
 struct Call {
   const uint16_t *q;
   int64_t q_stride;        // 0: rows lie as their numbers count (k_mass_pack)
@@ -35,14 +45,13 @@ struct Call {
   const uint8_t *k_scale;
   const int32_t *table;
   int page_shift, n_pages, max_pages;
-  int pieces, splits;      // of a sequence's keys at most; of the rows
-  bool of_rows;            // sequences without queries have no units
-  const int *starts;       // more than 64 sequences: units before each, and in all (k_mass_plan); else null
+  Cut cut;
+  int splits;              // of the rows
   const float *mass_in;
   float *mass;
   float2 *part;            // [piece][kv head][token, head of the group]: reference, sum of weights
   float2 *stat;            // [kv head][token, head of the group]: reference, 1 / sum of weights
-  int row_pieces;          // k_mass_add: `pieces` of the rows' sums
+  Cut rows_cut;            // k_mass_add: that of the rows' sums
   float *scores;           // [kv head][token, head of the group][position], where there are few rows; else null
 };
 
@@ -146,13 +155,31 @@ struct Work {
 };
 
 __device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); }
-// A sequence's keys in chunks of kc, and these in pieces of so many: as many pieces as there may be, none of them empty
-__device__ __forceinline__ int chunks_of_piece(const Call &a, int nk, int kc) { return quotient_up(quotient_up(nk, kc), a.pieces); }
-__device__ __forceinline__ int pieces_of(const Call &a, const Seq &s, int kc) {
-  if (s.nk == 0 || (a.of_rows && s.nq == 0)) return 0;
-  return quotient_up(quotient_up(s.nk, kc), chunks_of_piece(a, s.nk, kc));
+__device__ __forceinline__ bool has_pieces(const Cut &c, const Seq &s) { return s.nk > 0 && (!c.of_rows || s.nq > 0); }
+// What a chunk of a sequence costs, what all of them do
+__device__ __forceinline__ float cost(const Call &a, const Cut &c, const Seq &s) { return (float)max(quotient_up(s.nq * a.group, c.block), 1); }
+__device__ __forceinline__ float cost_of_all(const Call &a, const Cut &c, const Seq &s) {
+  return has_pieces(c, s) ? cost(a, c, s) * (float)quotient_up(s.nk, c.chunk) : 0.f;
 }
-__device__ __forceinline__ int units_of(const Call &a, const Seq &s, int kc) { return pieces_of(a, s, kc) * a.kv_heads * a.splits; }
+// The work of a piece, from that of all sequences and heads (a hair more, so that there are not more pieces than were aimed at and one for each
+// sequence and head)
+__device__ __forceinline__ float piece_work(const Call &a, const Cut &c, float all) { return all * (float)a.kv_heads / (float)c.aim * 1.0001f; }
+__device__ __forceinline__ int chunks_of_piece(const Call &a, const Cut &c, const Seq &s, float work) {
+  const int chunks = quotient_up(s.nk, c.chunk);
+  return max(max((int)fminf(ceilf(work / cost(a, c, s)), (float)chunks), quotient_up(chunks, c.most)), 1);
+}
+__device__ __forceinline__ int units_of(const Call &a, const Cut &c, const Seq &s, float work) {
+  return has_pieces(c, s) ? quotient_up(quotient_up(s.nk, c.chunk), chunks_of_piece(a, c, s, work)) * a.kv_heads * a.splits : 0;
+}
+// The work of a piece, worked out by every wave (the same in all of them) or once
+__device__ __forceinline__ Seq lane_seq(const Call &a) {
+  const int i = min((int)(threadIdx.x & 63), a.n_seq - 1);
+  return seq_of_numbers(a, a.q_off[i], a.q_off[i + 1], a.kv_len[i]);
+}
+__device__ __forceinline__ float work_of(const Call &a, const Cut &c, const Seq &mine) {
+  if (c.starts) return __builtin_bit_cast(float, uniform_at(c.starts, a.n_seq + 1));
+  return piece_work(a, c, wave_sum_ordered((int)(threadIdx.x & 63) < a.n_seq ? cost_of_all(a, c, mine) : 0.f));
+}
 
 // up to the lane (row_shr 1, 2, 4, 8 inside rows of 16 lanes; the rows' last lanes to the rows behind)
 __device__ __forceinline__ int wave_prefix(int v) {
@@ -169,18 +196,21 @@ __device__ __forceinline__ int wave_prefix(int v) {
 // the parts of an XCD in turn, whether these have room or not: where every pair had the same number of units, a third of them empty, the
 // parts that got the full ones held the others up, and 5 of 8 waves ran: four frames over 2748 to 41,220 positions 737 us
 // for the rows' sums and 896 for the keys'.)
-__device__ __forceinline__ bool find_work(const Call &a, int unit, int kc, Work &w, Seq &s) {
+__device__ __forceinline__ bool find_work(const Call &a, int unit, Work &w, Seq &s) {
   const int lane = threadIdx.x & 63;
+  const Cut &c = a.cut;
   int local;
-  if (a.starts) {
-    if (unit >= uniform_at(a.starts, a.n_seq)) return false;
-    w.seq = scalar(max(last_at_most(a.starts, a.n_seq, unit, lane), 0));
-    local = unit - uniform_at(a.starts, w.seq);
+  float work;
+  if (c.starts) {
+    if (unit >= uniform_at(c.starts, a.n_seq)) return false;
+    w.seq = scalar(max(last_at_most(c.starts, a.n_seq, unit, lane), 0));
+    local = unit - uniform_at(c.starts, w.seq);
     s = seq_at(a, w.seq);
+    work = work_of(a, c, s);
   } else {
-    const int i = min(lane, a.n_seq - 1);
-    const Seq mine = seq_of_numbers(a, a.q_off[i], a.q_off[i + 1], a.kv_len[i]);
-    const int units = lane < a.n_seq ? units_of(a, mine, kc) : 0, end = wave_prefix(units);
+    const Seq mine = lane_seq(a);
+    work = work_of(a, c, mine);
+    const int units = lane < a.n_seq ? units_of(a, c, mine, work) : 0, end = wave_prefix(units);
     if (unit >= __builtin_amdgcn_readlane(end, 63)) return false;
     w.seq = scalar(__popcll(__builtin_amdgcn_ballot_w64(end <= unit)));
     local = unit - __builtin_amdgcn_readlane(end - units, w.seq);
@@ -189,33 +219,42 @@ __device__ __forceinline__ bool find_work(const Call &a, int unit, int kc, Work 
     s.nk = __builtin_amdgcn_readlane(mine.nk, w.seq);
     s.p0 = __builtin_amdgcn_readlane(mine.p0, w.seq);
   }
-  const int pieces = scalar(pieces_of(a, s, kc)), per = scalar(chunks_of_piece(a, s.nk, kc));
-  if (pieces == 0) return false;      // (lengths that changed meanwhile)
+  if (!has_pieces(c, s)) return false;      // (lengths that changed meanwhile)
+  const int chunks = quotient_up(s.nk, c.chunk), per = scalar(chunks_of_piece(a, c, s, work)), pieces = scalar(quotient_up(chunks, per));
   const int x = scalar((int)((uint32_t)local / (uint32_t)pieces));
   w.piece = scalar(local - x * pieces);
   w.head = scalar((int)((uint32_t)x / (uint32_t)a.splits));
   w.split = scalar(x - w.head * a.splits);
   if (w.head >= a.kv_heads) return false;
   w.c0 = w.piece * per;
-  w.c1 = min(w.c0 + per, quotient_up(s.nk, kc));
+  w.c1 = min(w.c0 + per, chunks);
   return w.c0 < w.c1;
 }
 
 }  // namespace
 
-// More than 64 sequences: the units before each, worked out once.  (Twice: for the rows' sums, then, with `b`, for the keys'.)
-__global__ __launch_bounds__(1024) void k_mass_plan(Call a, Call b, int kc_a, int kc_b, int *starts_a, int *starts_b) {
+// More than 64 sequences: the work of a piece and the units before each sequence, worked out once.  (Twice: for the rows' sums, then, with
+// `b`, for the keys'.)  Sums in a fixed order.
+__global__ __launch_bounds__(1024) void k_mass_plan(Call a, Call b, int *starts_a, int *starts_b) {
   const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6);
   __shared__ int sums[2][16];
+  __shared__ float works[16];
   for (int which = 0; which < 2; ++which) {
     const Call &c = which ? b : a;
     int *const starts = which ? starts_b : starts_a;
+    auto seq = [&](int i) { return seq_of_numbers(c, c.q_off[i], c.q_off[i + 1], c.kv_len[i]); };
+    float all = 0.f;
+    for (int i = tid; i < c.n_seq; i += 1024) all += cost_of_all(c, c.cut, seq(i));
+    all = wave_sum_ordered(all);
+    if (lane == 0) works[wave] = all;
+    __syncthreads();
+    all = 0.f;
+    for (int x = 0; x < 16; ++x) all += works[x];
+    const float work = piece_work(c, c.cut, all);
     int before = 0;
     for (int i0 = 0; i0 < c.n_seq; i0 += 1024) {
       const int i = i0 + tid, turn = i0 >> 10 & 1;
-      int units = 0;
-      if (i < c.n_seq) units = units_of(c, seq_of_numbers(c, c.q_off[i], c.q_off[i + 1], c.kv_len[i]), which ? kc_b : kc_a);
-      const int end = wave_prefix(units);
+      const int units = i < c.n_seq ? units_of(c, c.cut, seq(i), work) : 0, end = wave_prefix(units);
       if (lane == 63) sums[turn][wave] = end;
       __syncthreads();      // (the other of the two is read by nobody any more behind it)
       int at = before + end - units;
@@ -225,7 +264,10 @@ __global__ __launch_bounds__(1024) void k_mass_plan(Call a, Call b, int kc_a, in
       }
       if (i < c.n_seq) starts[i] = at;
     }
-    if (tid == 0) starts[c.n_seq] = before;
+    if (tid == 0) {
+      starts[c.n_seq] = before;
+      starts[c.n_seq + 1] = __builtin_bit_cast(int, work);
+    }
     __syncthreads();
   }
 }
@@ -258,7 +300,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int lane = threadIdx.x & 63, h = lane >> 5;
   Work w;
   Seq s;
-  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32 * NT, w, s)) return;
+  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), w, s)) return;
   const int n_rows = s.nq * a.group;
   // rows of this split, in blocks of 32, from the first that sees the piece's first key
   const int blocks = (n_rows + 31) / 32, per = scalar(quotient_up(blocks, a.splits));
@@ -369,7 +411,7 @@ __global__ __launch_bounds__(256) void k_mass_rows_few(Call a) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
   Work w;
   Seq s;
-  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32, w, s)) return;
+  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), w, s)) return;
   const int n_rows = s.nq * a.group;
   const int64_t room = (int64_t)a.max_pages << a.page_shift;
   // 8 RG rows at a time (more than once where sequences are of unlike lengths)
@@ -472,11 +514,11 @@ template <bool OWN>
 __global__ __launch_bounds__(256) void k_mass_add(Call a) {
   Work w;
   Seq s;
-  if (!find_work(a, (int)blockIdx.x, 1024, w, s)) return;
+  if (!find_work(a, (int)blockIdx.x, w, s)) return;
   const int n_rows = s.nq * a.group, lane = threadIdx.x & 63, wave = scalar((int)(threadIdx.x >> 6));
   const int64_t room = (int64_t)a.max_pages << a.page_shift, base = ((int64_t)w.seq * a.kv_heads + w.head) * room, number = row_number(a, w.head, s);
   const int64_t all = (int64_t)a.kv_heads * a.n_q * a.group;
-  const int of_piece = quotient_up(quotient_up(s.nk, 32), a.row_pieces) * 32;      // keys
+  const int of_piece = OWN ? chunks_of_piece(a, a.rows_cut, s, work_of(a, a.rows_cut, lane_seq(a))) * a.rows_cut.chunk : 1;      // keys
   __shared__ float2 stat[64];
   for (int ch = w.c0; ch < w.c1; ++ch) {
     const int64_t key = (int64_t)ch * 1024 + threadIdx.x * 4;
@@ -536,19 +578,19 @@ __global__ __launch_bounds__(256) void k_mass_add(Call a) {
 // The sums of a row's pieces put together, always in the same order.  ROWS of them to a workgroup (64: a lane each, the pieces by turns to
 // the four waves; 4: a wave each, a lane's pieces 64 apart), four pieces' loads on the way together.
 template <int ROWS>
-__global__ __launch_bounds__(256) void k_mass_join(Call a, int kc, int side) {
+__global__ __launch_bounds__(256) void k_mass_join(Call a, int side) {
   constexpr int kSlices = 256 / ROWS;
   const int pair = scalar((int)(blockIdx.x / (uint32_t)side)), turn = scalar((int)(blockIdx.x - pair * (uint32_t)side));
   const int seq = scalar((int)((uint32_t)pair / (uint32_t)a.kv_heads)), head = scalar(pair - seq * a.kv_heads);
   const Seq s = seq_at(a, seq);
   const int n_rows = s.nq * a.group, mine = ROWS == 64 ? threadIdx.x & 63 : threadIdx.x >> 6, slice = ROWS == 64 ? threadIdx.x >> 6 : threadIdx.x & 63;
-  const int per = chunks_of_piece(a, s.nk, kc);
+  const int of_piece = chunks_of_piece(a, a.cut, s, work_of(a, a.cut, lane_seq(a))) * a.cut.chunk;      // keys
   const int64_t all = (int64_t)a.kv_heads * a.n_q * a.group, base = row_number(a, head, s);
   __shared__ float2 sums[4][64];
   for (int row0 = turn * ROWS; row0 < n_rows; row0 += side * ROWS) {
     const int row = min(row0 + mine, n_rows - 1);
     const int lim = limit_of(a, s, row / a.group);
-    const int seen = per ? quotient_up(lim, per * kc) : 0;      // pieces that it sees
+    const int seen = quotient_up(lim, of_piece);      // pieces that it sees
     float ref = kUnset, l = 0.f;
     for (int p0 = slice; p0 < seen; p0 += 4 * kSlices) {
       float2 o[4];
@@ -595,7 +637,7 @@ __global__ __launch_bounds__(256) void k_mass_keys_few(Call a) {
   const int lane = threadIdx.x & 63, h = lane >> 5;
   Work w;
   Seq s;
-  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32 * NT, w, s)) return;
+  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), w, s)) return;
   const int n_rows = s.nq * a.group;
   const float2 *stat = a.stat + row_number(a, w.head, s);
   const int64_t base = (int64_t)(w.seq * a.kv_heads + w.head) * ((int64_t)a.max_pages << a.page_shift);
@@ -680,7 +722,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int lane = threadIdx.x & 63, h = lane >> 5;
   Work w;
   Seq s;
-  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), 32 * NT, w, s)) return;
+  if (!find_work(a, scalar((int)(blockIdx.x * 4 + (threadIdx.x >> 6))), w, s)) return;
   const int n_rows = s.nq * a.group;
   const float2 *stat = a.stat + row_number(a, w.head, s);
   const int64_t base = (int64_t)(w.seq * a.kv_heads + w.head) * ((int64_t)a.max_pages << a.page_shift);
@@ -779,9 +821,11 @@ constexpr int64_t kMostScores = (int64_t)1 << 27;      // scores there
 
 struct Form {
   bool few, scores, small_chunks;
-  int pieces, splits;      // k_mass_rows*
-  int key_pieces;          // k_mass_keys
+  int aim, splits;         // units; of the rows
+  int most;                // pieces of a sequence
 };
+// Pieces of the only sequence that has many keys, at most
+int64_t most_pieces(int kv_heads, int64_t most_keys) { return std::max((int64_t)1, std::min((int64_t)(kAimMany + kv_heads - 1) / kv_heads, (most_keys + 31) / 32)); }
 // Tokens up to which scores are kept: where writing and reading them is less than reading K again, and they fit.
 int64_t kept_tokens(int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   const int64_t row_bytes = dtype == LV_CACHE_BF16 ? 2 * head_dim : dtype == LV_CACHE_E4M3 ? head_dim : head_dim / 2;
@@ -790,17 +834,14 @@ int64_t kept_tokens(int n_seq, int heads, int kv_heads, int head_dim, int dtype,
 Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   Form f;
   const int64_t pairs = (int64_t)n_seq * kv_heads, rows = std::max((int64_t)n_q, (int64_t)1) * heads;
-  const int64_t most = (most_keys + 31) / 32;
   f.few = (double)n_q * (heads / kv_heads) / n_seq <= 32.0;
   f.scores = n_q <= kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys);
-  const int64_t whole = f.few ? kAim : kAimMany;
-  const int64_t aim = std::max((int64_t)1, std::min((whole + pairs - 1) / pairs, most));
-  f.key_pieces = (int)aim;
-  f.pieces = (int)std::max((int64_t)1, std::min(aim, kMostParts / rows));
+  f.aim = f.few ? kAim : kAimMany;
+  f.most = (int)std::max((int64_t)1, std::min(most_pieces(kv_heads, most_keys), kMostParts / rows));
   // Many rows: where the chunks are too few to fill the chip a few times over, rows are split too, down to four blocks of 32.  (The sums by
   // keys cannot be: they take chunks of 32 keys then.)
   const int64_t blocks = ((int64_t)n_q * (heads / kv_heads) / n_seq + 31) / 32, chunk = head_dim == 64 ? 256 : 128;
-  const int64_t units = pairs * std::min((int64_t)f.pieces, (most_keys + chunk - 1) / chunk);
+  const int64_t units = std::min(pairs * ((most_keys + chunk - 1) / chunk), (int64_t)f.aim);
   f.splits = f.few ? 1 : (int)std::max((int64_t)1, std::min(std::min((kUnits + units - 1) / units, blocks / 4), (int64_t)64));
   f.small_chunks = pairs * ((most_keys + chunk / 2 - 1) / (chunk / 2)) < kUnits / 4;
   return f;
@@ -809,17 +850,16 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtyp
 }  // namespace
 
 // Parts, divisors, normalised rows, scores: each as much as any call of up to n_q tokens takes, so that scratch for more serves fewer
-static size_t parts_bytes(int64_t rows, int64_t pairs, int64_t most_keys) {
-  const int64_t aim = std::max((int64_t)1, std::min((kAimMany + pairs - 1) / pairs, (most_keys + 31) / 32));
-  return align_up((size_t)std::min(rows * aim, std::max(kMostParts, rows)) * sizeof(float2), 256);
+static size_t parts_bytes(int64_t rows, int kv_heads, int64_t most_keys) {
+  return align_up((size_t)std::min(rows * most_pieces(kv_heads, most_keys), std::max(kMostParts, rows)) * sizeof(float2), 256);
 }
-static size_t plan_bytes(int n_seq) { return n_seq > 64 ? 2 * align_up((size_t)(n_seq + 1) * sizeof(int), 256) : 0; }
+static size_t plan_bytes(int n_seq) { return n_seq > 64 ? 2 * align_up((size_t)(n_seq + 2) * sizeof(int), 256) : 0; }
 static size_t packed_bytes(int64_t rows, int head_dim) { return align_up((size_t)rows * head_dim * 2, 256); }
 static size_t stat_bytes(int64_t rows) { return align_up((size_t)rows * sizeof(float2), 256); }
 
 size_t mass_ws_bytes(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   const int64_t rows = (int64_t)n_q * heads, kept = std::min((int64_t)n_q, kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys));
-  return plan_bytes(n_seq) + parts_bytes(rows, (int64_t)n_seq * kv_heads, most_keys) + stat_bytes(rows) + packed_bytes(rows, head_dim) +
+  return plan_bytes(n_seq) + parts_bytes(rows, kv_heads, most_keys) + stat_bytes(rows) + packed_bytes(rows, head_dim) +
          align_up((size_t)kept * heads * most_keys * sizeof(float), 256);
 }
 
@@ -830,39 +870,43 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
   constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;
   const bool keep = x.n_q > 0 && f.few && f.scores;
   const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : f.small_chunks ? 32 : 32 * NK;
-  // keys' units at most, where a workgroup takes one; as many as there are CUs or fewer join their rows themselves
-  const int64_t most_blocks = (((int64_t)c.max_pages << c.page_shift) + 1023) / 1024;
-  const bool own = keep && pairs * most_blocks <= 256;
+  // as many workgroups as there are CUs or fewer join their rows themselves
+  const int64_t most = (int64_t)c.max_pages << c.page_shift;
+  const bool own = keep && pairs * ((most + 1023) / 1024) <= 256;
+  const bool eight = rows <= 8.0;
+  const int block = f.few && eight ? 8 : 32;
   Call by_rows = c, by_keys = c;
-  by_rows.pieces = f.pieces;
+  by_rows.cut = Cut{kc_rows, f.aim, f.most, block, true, nullptr};
   by_rows.splits = f.splits;
-  by_rows.of_rows = true;
-  by_keys.pieces = f.key_pieces;
+  by_keys.cut = Cut{kc_keys, f.aim, 0x7fffffff, block, false, nullptr};
   by_keys.splits = 1;
   if (c.n_seq > 64) {
     int *const starts = plan, *const starts_keys = (int *)((char *)plan + plan_bytes(c.n_seq) / 2);
-    k_mass_plan<<<dim3(1), 1024, 0, st>>>(by_rows, by_keys, kc_rows, kc_keys, starts, starts_keys);
-    by_rows.starts = starts;
-    by_keys.starts = starts_keys;
+    k_mass_plan<<<dim3(1), 1024, 0, st>>>(by_rows, by_keys, starts, starts_keys);
+    by_rows.cut.starts = starts;
+    by_keys.cut.starts = starts_keys;
   }
+  by_keys.rows_cut = by_rows.cut;
+  // units at most: those aimed at and one for each sequence and head, and no more than there are chunks
+  auto units = [&](const Call &y) {
+    return std::min(y.cut.aim + pairs, pairs * ((most + y.cut.chunk - 1) / y.cut.chunk)) * y.splits;
+  };
   // a wave to a unit
   auto walk = [&](auto kernel, const Call &y) {
-    kernel<<<dim3((uint32_t)((pairs * y.pieces * y.splits + 3) / 4)), 256, 0, st>>>(y);
+    kernel<<<dim3((uint32_t)((units(y) + 3) / 4)), 256, 0, st>>>(y);
   };
-  const bool eight = rows <= 8.0;
   if (x.n_q > 0) {
     if (keep) eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
     else if (f.few) eight ? walk(k_mass_rows_few<K, D, 1, false>, by_rows) : walk(k_mass_rows_few<K, D, 4, false>, by_rows);
     else walk(k_mass_rows<K, D, NR>, by_rows);
-    by_keys.row_pieces = f.pieces;
     const int64_t per_pair = std::max((int64_t)1, kAim / pairs);
     auto join = [&](auto kernel, int at_once) {
       const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
-      kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, kc_rows, side);
+      kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, side);
     };
     if (!own) rows <= 64.0 ? join(k_mass_join<4>, 4) : join(k_mass_join<64>, 64);
   }
-  const dim3 blocks((uint32_t)(pairs * std::min((int64_t)by_keys.pieces, most_blocks)));
+  const dim3 blocks((uint32_t)units(by_keys));
   if (own) k_mass_add<true><<<blocks, 256, 0, st>>>(by_keys);
   else if (keep) k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
   else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
@@ -881,7 +925,7 @@ int launch_mass(const MassArgs &x, void *ws, hipStream_t st) {
   int *const plan = (int *)at;
   at += plan_bytes(x.cv.n_seq);
   c.part = (float2 *)at;
-  at += parts_bytes(rows, (int64_t)x.cv.n_seq * x.cv.kv_heads, most);
+  at += parts_bytes(rows, x.cv.kv_heads, most);
   c.stat = (float2 *)at;
   at += stat_bytes(rows);
   c.q = x.q;

@@ -177,3 +177,11 @@ def test_one_sequence_with_many_rows_among_those_of_few(dtype):
     lens = [300] + [40] * 40
     Pool(34, lens, heads=4, kv_heads=2, dtype=dtype, frame=1).draw([100] + [1] * 40)
     Pool(35, lens, heads=2, kv_heads=2, dtype=dtype, holes=[(0, 5)]).draw([150] + [0, 1] * 20)
+
+
+@pytest.mark.parametrize("n_seq", [3, 66, 300])
+def test_a_long_sequence_among_empty_ones(n_seq):
+    """All pieces belong to one of many sequences."""
+    for lens, new, kw in ((3000, 40, dict(frame=7)), (5000, 2, dict(head_dim=128)), (900, 300, dict(frame=1))):
+        at = n_seq // 2
+        Pool(36, [0] * at + [lens] + [3] * (n_seq - at - 1), heads=2, kv_heads=1, dtype="e2m1", **kw).draw([0] * at + [new] + [0] * (n_seq - at - 1))
