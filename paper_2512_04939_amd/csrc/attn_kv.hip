@@ -19,7 +19,7 @@
 // weights already lie as the B operand of O^T += V^T P^T.  K and V lie in LDS as rows; V's fragments come out by transposing reads.
 //
 // Rounded to bf16: the weights, for the second product (their sum is that of the unrounded ones), q after its normalisation
-// (as K was before it), and the result.  An E4M3 code times a power of two is a bf16 value: nothing is rounded there.  The scale is
+// (as K was before it), and the result.  An E4M3 or E2M1 code times a power of two is a bf16 value: nothing is rounded there.  The scale is
 // multiplied to the fp32 scores and not into q, where it would cost a rounding (7 % of the time at 64 channels).
 #include <algorithm>
 
@@ -44,11 +44,11 @@ constexpr int kRounds = 3;               // a call's pieces fill the chip's slot
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-enum class Kv { ROWS, PAGES, E4M3, E2M1 };
+enum class Kv { ROWS, PAGES, E4M3, E2M1 };     // rows of another set; pages of bf16, of codes
 template <Kv KV> constexpr bool kCoded = KV == Kv::E4M3 || KV == Kv::E2M1;                // codes that become bf16 on their way into LDS
 template <Kv KV, int D> constexpr int kRowBytes = KV == Kv::E2M1 ? D / 2 : KV == Kv::E4M3 ? D : 2 * D;
 
-template <Kv KV, int D, int QB> constexpr int kFewWaves = KV == Kv::E2M1 && D == 64 && QB == 1 ? 4 : 2;      // waves of a SIMD, few rows
+template <Kv KV, int D, int QB> constexpr int kFewWaves = KV == Kv::E2M1 && D == 64 && QB == 1 ? 4 : 2;      // waves of a SIMD, few rows (by registers)
 
 // What a kernel needs of the call, by value
 struct Call {
@@ -547,7 +547,9 @@ struct Codes<Kv::E2M1, D> {
 };
 
 // E2M1, few rows: codes and scales lie in LDS as they are held, in a ring of kSlots tiles of 32 keys a wave, on their way straight from memory.
-// A slot: K's codes, V's, 256 bytes of K's scales, 256 of V's.
+// A slot: K's codes, V's, 256 bytes of K's scales, 256 of V's.  (A tile's codes are a quarter of bf16's bytes and take as long to compute with: waves
+// count more than what each has on the way.  A token over 137,405 positions of 16 heads of 64: 61 us with the next tile's codes in registers and
+// two waves to a SIMD, 57 with the ring, 50 with three waves, 46.5 with four; 32 over 301 to 30,011, 16 heads on 4 of 128, two waves: 76 and 73.)
 template <int D>
 struct Ring {
   static constexpr int kSlots = 2, kCodes = 32 * (D / 2), kScales = 32 * (D / 32);      // bytes of a tile's K or V

@@ -8,6 +8,12 @@
 // no barrier, and nobody waits for another wave.  Which channels a lane holds is free as long as q and k agree: a half wave takes half a
 // row's channels in one piece, so its loads are 16 bytes wide in every kind of cache.
 //
+// Up to 32 rows: bound by reading K and writing the scores, from which the second walk is made (5 rows over 137,405 positions of 16 heads of 64,
+// bf16: 61 to 66 us for 281 MB and 44, 5 to join, 14 to add; K twice was 48 and 54).  More: by the VALU.  A tile of 32 x 32 scores takes 16
+// exponentials, 16 multiply-adds and 16 sums of a lane, twice, some 400 cycles each time with what goes around them, against 128 of MFMA at 64
+// channels: four frames of 1374 tokens over 2748 to 41,220 positions of an E2M1 cache 500 us for the rows' sums and 450 for the keys', 20 to join.
+// (Tried and level: a tile's products ahead of or among the weights of the one before, keys in chunks of 5 tiles: 926, for want of registers.)
+//
 // References, sums and masses are fp32; sums over rows and pieces have a fixed order.  q is rounded to bf16 after its normalisation, as
 // K was before it was stored; nothing else is rounded below fp32.
 #include <algorithm>
@@ -195,7 +201,7 @@ __device__ __forceinline__ int wave_prefix(int v) {
 // The wave's part of the call: the units of the sequences one after the other, those that are not there behind them all.  (Workgroups go to
 // the parts of an XCD in turn, whether these have room or not: where every pair had the same number of units, a third of them empty, the
 // parts that got the full ones held the others up, and 5 of 8 waves ran: four frames over 2748 to 41,220 positions 737 us
-// for the rows' sums and 896 for the keys'.)
+// for the rows' sums and 896 for the keys', 505 and 633 so.)
 __device__ __forceinline__ bool find_work(const Call &a, int unit, Work &w, Seq &s) {
   const int lane = threadIdx.x & 63;
   const Cut &c = a.cut;
@@ -826,16 +832,21 @@ struct Form {
 };
 // Pieces of the only sequence that has many keys, at most
 int64_t most_pieces(int kv_heads, int64_t most_keys) { return std::max((int64_t)1, std::min((int64_t)(kAimMany + kv_heads - 1) / kv_heads, (most_keys + 31) / 32)); }
-// Tokens up to which scores are kept: where writing and reading them is less than reading K again, and they fit.
+// Tokens up to which scores are kept: where writing and reading them costs less than reading K and taking the products again, and they fit.  Over
+// 60,000 positions, 16 heads of 64, kept and not: bf16 16 rows 67 us and 81, 24 77 and 82, 32 87 and 81; E4M3 12 57 and 61, 24 71 and 62; E2M1 12 53 and
+// 58, 16 60 and 58; of 128, bf16 32 115 and 144, E2M1 16 65 and 75.
 int64_t kept_tokens(int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   const int64_t row_bytes = dtype == LV_CACHE_BF16 ? 2 * head_dim : dtype == LV_CACHE_E4M3 ? head_dim : head_dim / 2;
-  return std::min(row_bytes / 8 * n_seq / (heads / kv_heads), kMostScores / (most_keys * heads));
+  const int64_t rows = std::min(row_bytes / 8 + 8, (int64_t)32);
+  return std::min(rows * n_seq / (heads / kv_heads), kMostScores / (most_keys * heads));
 }
 Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
   Form f;
   const int64_t pairs = (int64_t)n_seq * kv_heads, rows = std::max((int64_t)n_q, (int64_t)1) * heads;
-  f.few = (double)n_q * (heads / kv_heads) / n_seq <= 32.0;
+  const double mean = (double)n_q * (heads / kv_heads) / n_seq;
   f.scores = n_q <= kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys);
+  // (not kept, E2M1: 32 rows of 128 channels 75 us so, 86 in the other form; 16 of 64 64 and 58)
+  f.few = f.scores || mean <= (head_dim == 128 ? 32.0 : 8.0);
   f.aim = f.few ? kAim : kAimMany;
   f.most = (int)std::max((int64_t)1, std::min(most_pieces(kv_heads, most_keys), kMostParts / rows));
   // Many rows: where the chunks are too few to fill the chip a few times over, rows are split too, down to four blocks of 32.  (The sums by
@@ -897,8 +908,12 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
   };
   if (x.n_q > 0) {
     if (keep) eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
-    else if (f.few) eight ? walk(k_mass_rows_few<K, D, 1, false>, by_rows) : walk(k_mass_rows_few<K, D, 4, false>, by_rows);
-    else walk(k_mass_rows<K, D, NR>, by_rows);
+    else if (f.few && eight) walk(k_mass_rows_few<K, D, 1, false>, by_rows);
+    else if (f.few) {
+      if constexpr (D == 128) walk(k_mass_rows_few<K, D, 4, false>, by_rows);
+    } else {
+      walk(k_mass_rows<K, D, NR>, by_rows);
+    }
     const int64_t per_pair = std::max((int64_t)1, kAim / pairs);
     auto join = [&](auto kernel, int at_once) {
       const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
@@ -907,12 +922,19 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
     if (!own) rows <= 64.0 ? join(k_mass_join<4>, 4) : join(k_mass_join<64>, 64);
   }
   const dim3 blocks((uint32_t)units(by_keys));
-  if (own) k_mass_add<true><<<blocks, 256, 0, st>>>(by_keys);
-  else if (keep) k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
-  else if (eight) walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
-  else if (f.few) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
-  else if (f.small_chunks) walk(k_mass_keys<K, D, 1>, by_keys);
-  else walk(k_mass_keys<K, D, NK>, by_keys);
+  if (own) {
+    k_mass_add<true><<<blocks, 256, 0, st>>>(by_keys);
+  } else if (keep) {
+    k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
+  } else if (f.few && eight) {
+    walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
+  } else if (f.few) {
+    if constexpr (D == 128) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
+  } else if (f.small_chunks) {
+    walk(k_mass_keys<K, D, 1>, by_keys);
+  } else {
+    walk(k_mass_keys<K, D, NK>, by_keys);
+  }
   LV_HIP_CHECK_LAUNCH();
   return LV_OK;
 }

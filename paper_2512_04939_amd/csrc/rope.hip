@@ -4,6 +4,10 @@
 //
 // The gradient is the same with -t.  Angles are taken in 64 bits as turns (t / 2 pi), of which only the fraction goes on in 32: a product
 // of a position below 2^31 and a frequency of 1 is off by 2^-24 of a turn there at most, where 32 bits would lose everything from 2^24 on.
+//
+// Bound by HBM: every row is read and written once.  43,968 tokens of 16 + 16 heads of 64 in 63 us, 5.7 TB/s (a copy of 4 GB reaches 4.8 on the same
+// card); one head after the other behind the angles, as it was first, 97.  20,011 tokens of 16 + 4 heads of 128 in 38 us, 60 before.
+// A single token takes 3 us of the GPU.  Rounded to bf16: the result, once.
 #include "internal.h"
 #include "common.h"
 
@@ -150,7 +154,8 @@ int launch_rope(const RopePairs &pairs, const int32_t *pos, int n, int heads, in
   a.rotated = 2 * pairs.first[pairs.axes];
   a.sign = inverse ? -1.0f : 1.0f;
   const int per_group = 256 / (head_dim / 8);
-  // four heads to a lane, so that the angles are worked out once for all of them; one where the chip would not be full so
+  // four heads to a lane, so that the angles are worked out once for all of them; one where the chip would not be full so (32 heads of 64: 1 token
+  // 2.8 us with one and 3.3 with four, 256 3.8 and 4.6; 5496 tokens 12.8 and 10)
   const bool few = (int64_t)n * a.all <= 8192;
   const int per = few ? 1 : 4;
   a.parts = (a.all + per - 1) / per;
