@@ -415,7 +415,7 @@ int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *c
  * sequence s, as in litevggt_cached_attn: same masks, same normalisation)
  *   mass[s][h][t] = mass_in[s][h][t] + sum_r w_rt / sum_t' w_rt',   w_rt = exp(q_r . k_t * softmax_scale)
  * for the positions t below kv_len[s] that are held, 0 for those that are not; what lies from kv_len[s] on is left as it was.  A row that
- * sees no held position adds nothing; one with a score that is NaN makes all that it sees NaN.  Everything is fp32 (from bf16 q and K as
+ * sees no held position adds nothing; one with a score that is NaN or plus infinity makes all that it sees NaN.  Everything is fp32 (from bf16 q and K as
  * it is held); results do not depend on the order in which workgroups run.  The call needs neither v nor v_scale.
  *   mass_in  [device] [n_seq][kv_heads][max_pages * page_tokens] fp32, 16-byte aligned; NULL: zeros; may be the same buffer as mass
  *   mass     [device] the same, out
@@ -436,7 +436,8 @@ int litevggt_cached_mass(const litevggt_cache_params *p, const litevggt_cache *c
  *   freed      [device] [n_seq][max_pages] the pages that left, in the order of their columns, -1 behind them; another buffer
  *   n_freed    [device] [n_seq] how many
  *   ws         litevggt_cache_evict_ws_bytes(p) bytes
- * Positions keep their numbers: what stays is attended to as before.  Pages that serve several sequences: each gives back its own use of them.
+ * Positions keep their numbers: what stays is attended to as before.  Pages that serve several sequences, or stand in several columns: each gives
+ * back its own use of them.
  * Of p: n_seq, kv_heads, page_tokens, n_pages, max_pages; the rest has to be valid.
  */
 size_t litevggt_cache_evict_ws_bytes(const litevggt_cache_params *p);
