@@ -5,7 +5,7 @@ import torch
 
 from paper_2512_04939_amd import binding as B
 
-from stream_cases import DTYPES, Pool, dev, host, i32, rows
+from stream_cases import DTYPES, S, Pool, dev, host, i32, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -185,3 +185,34 @@ def test_a_long_sequence_among_empty_ones(n_seq):
     for lens, new, kw in ((3000, 40, dict(frame=7)), (5000, 2, dict(head_dim=128)), (900, 300, dict(frame=1))):
         at = n_seq // 2
         Pool(36, [0] * at + [lens] + [3] * (n_seq - at - 1), heads=2, kv_heads=1, dtype="e2m1", **kw).draw([0] * at + [new] + [0] * (n_seq - at - 1))
+
+
+@pytest.mark.parametrize("new", [1, 20, 200])
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+def test_a_score_that_is_not_finite(value, new):
+    """Plus infinity and NaN: all that the row sees is NaN, what it does not see is not.  Minus infinity: no weight."""
+    c = Pool(37, [500], heads=2, kv_heads=2, dtype="bf16", scale=1.0, frame=100 if new < 200 else 50)
+    q = np.zeros((new, 2, 64))
+    q[:, :, 0] = 1.0
+    k = np.zeros_like(c.o.k)
+    for t in range(500):
+        k[c.table[0, t // 16], :, t % 16, 0] = t % 5
+    at = 430
+    k[c.table[0, at // 16], 0, at % 16, 0] = value
+    c.o.k = k
+    c.d = c.device()
+    p = c.p
+    had = np.zeros((1, 2, p.max_pages * 16), np.float32)
+    out = torch.full(had.shape, 5.0, device="cuda")
+    ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, new)).fill_(255)
+    B.litevggt_cached_mass(p, c.d, dev(q), i32([0, new]), i32([500]), None, out, ws)
+    exact = S.mass(c.o, q, [0, new], [500], p.frame_tokens, None, np.full(had.shape, 5.0), False, 1.0)
+    got = host(out)
+    fine = np.isfinite(exact)
+    assert fine[0, 1].all() and fine[0, 0, :500].all() == (value == -np.inf)
+    assert np.array_equal(np.isnan(got), ~fine)
+    # scores are whole numbers up to 4, exact in fp32: Pool.draw's terms without the scores' error
+    rel = 2.0 ** -17 + (500 + new + 16) * 2.0 ** -24
+    assert (np.abs(got - exact)[fine] <= (rel * np.abs(exact) + 1e-30)[fine]).all()
+    if value == -np.inf:
+        assert got[0, 0, at] == 0
