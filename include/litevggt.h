@@ -452,7 +452,8 @@ int litevggt_cache_evict(const litevggt_cache_params *p, const int32_t *page_tab
  *   LV_ROPE_HEAD_HALVES  channels i and R + i
  *   LV_ROPE_ADJACENT     channels 2 i and 2 i + 1
  *   freq(i) = base^(-j / pairs[a]), with `joint` base^(-i / R), or p->freq[i] where that is given
- * Channels from 2 R on are copied.  Angles are exact to 2^-24 turns or so at any position.  `inverse`: by -t, which undoes it and is its gradient.
+ * Channels from 2 R on are copied.  An angle is off by 2^-24 + |t| 2^-54 turns or so: worked out in 64 bits, its fraction of a turn held in 32.
+ * `inverse`: by -t, which undoes it and is its gradient.
  *   pos    [device] [n_tokens][axes] int32, of any sign
  *   q, q_out [device] [n_tokens, heads, head_dim] bf16;  k, k_out [device] [n_tokens, kv_heads, head_dim] bf16, not read with
  *            kv_heads = 0; row strides in elements (multiples of 8); an output may be its input, with the same stride
@@ -467,7 +468,7 @@ typedef struct {
   int32_t pairing;         /* LV_ROPE_*                                                */
   int32_t joint;           /* != 0: the frequencies of all axes are one ladder         */
   int32_t inverse;
-  float   base;            /* > 0 (100 for patches, 10000); not read where freq is given */
+  float   base;            /* > 0 (100 for patches, 10000), no frequency above 1e6; not read where freq is given */
   const double *freq;      /* [host] [R] radians a position, at most 1e6 in magnitude, or NULL */
 } litevggt_rope_params;
 int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t *pos, const void *q, int64_t q_stride, const void *k,

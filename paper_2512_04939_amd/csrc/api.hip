@@ -586,7 +586,10 @@ int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t
       const int of = p->joint ? r.first[p->axes] : p->pairs[a];
       const long double step = expl(-logl((long double)p->base) / of);
       long double f = a == 0 || !p->joint ? 1.0L : powl(step, r.first[a]);
-      for (int i = r.first[a]; i < r.first[a + 1]; ++i, f *= step) r.turns[i] = (double)(f * (long double)kTurn);
+      for (int i = r.first[a]; i < r.first[a + 1]; ++i, f *= step) {
+        if (!(f <= 1e6L)) return LV_ERR_PARAM;      // (a base far below 1)
+        r.turns[i] = (double)(f * (long double)kTurn);
+      }
     }
   }
   if (n_tokens > 0 && (!pos || !q || !q_out || (p->kv_heads > 0 && (!k || !k_out)))) return LV_ERR_NULL;

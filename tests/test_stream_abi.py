@@ -143,3 +143,10 @@ def test_binding_refuses_what_does_not_fit():
     for bad in (t.long(), t[:1], t[:, :3]):
         with pytest.raises(B.LiteVGGTError):
             B.litevggt_cache_evict(p, bad, lens, m, lens, 0, 0, t, t.clone(), lens, None)
+
+
+def test_a_base_may_not_give_frequencies_that_are_refused_by_themselves():
+    """At most 1e6 radians a position, as for the caller's own: the last pair of 16 has base^(-15/16)."""
+    for base, rc in ((1e-30, PARAM), (1e-7, PARAM), (1e-6, OK), (0.5, OK), (100.0, OK)):
+        assert rope(rope_params(base=base), n=0) == rc, base
+        assert rope(rope_params(base=base, joint=1), n=0) == rc, base
