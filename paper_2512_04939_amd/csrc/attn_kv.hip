@@ -916,7 +916,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kFewWaves<K
         if (KV != Kv::ROWS && (shut_now >> (i & 63) & 1))
           shut = (__builtin_amdgcn_readlane(ids[0], i & 63) < 0 ? 1 : 0) | (__builtin_amdgcn_readlane(ids[1], i & 63) < 0 ? 2 : 0);
         if constexpr (kCoded<KV>) {
-  #pragma unroll
+#pragma unroll
           for (int g = 0; g < 2; ++g) {
             kc[g].store(kt + g * kGrp * T::kRow, false, lane);
             vc[g].store(kt + kTile + g * kGrp * T::kRow, true, lane);
@@ -1615,7 +1615,9 @@ Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtyp
   f.few = rows <= (head_dim == 64 ? 64.0 : 32.0);
   f.rows = f.few ? (rows <= 32.0 ? 32 : 64) : 256;
   f.tile = f.few ? 128 : 64;
-  f.resident = kCus * (f.few && dtype == LV_CACHE_E2M1 ? (head_dim == 64 && f.rows == 32 ? kFewWaves<Kv::E2M1, 64, 1> : 2) : head_dim == 64 || (f.few && dtype != LV_CACHE_BF16) ? 2 : 1);     // (by LDS; 128 channels, many rows: 8 waves each)
+  // (by LDS; 128 channels, many rows: 8 waves each)
+  f.resident = kCus * (head_dim == 64 || (f.few && dtype != LV_CACHE_BF16) ? 2 : 1);
+  if (f.few && dtype == LV_CACHE_E2M1 && head_dim == 64 && f.rows == 32) f.resident = kCus * kFewWaves<Kv::E2M1, 64, 1>;
   f.units = ((int64_t)n_q * group / f.rows + n_seq) * kv_heads;
   const int64_t tiles = (most_keys + f.tile - 1) / f.tile;
   // (Blocks of several sequences that fill the chip four times over are not cut: 32 x 2000 queries over 4000 keys, 16 heads of 64

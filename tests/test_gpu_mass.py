@@ -216,3 +216,25 @@ def test_a_score_that_is_not_finite(value, new):
     assert (np.abs(got - exact)[fine] <= (rel * np.abs(exact) + 1e-30)[fine]).all()
     if value == -np.inf:
         assert got[0, 0, at] == 0
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [1, 20, 200])
+def test_scores_that_are_all_minus_infinity(new, dim):
+    """Such rows add nothing; those of the other kv head do."""
+    c = Pool(38, [500], heads=2, kv_heads=2, dtype="bf16", scale=1.0, head_dim=dim, frame=50)
+    q = np.zeros((new, 2, dim))
+    q[:, :, 0] = 1.0
+    k = np.zeros_like(c.o.k)
+    k[:, 0, :, 0] = -np.inf
+    c.o.k = k
+    c.d = c.device()
+    p = c.p
+    had = torch.rand(1, 2, p.max_pages * 16, device="cuda")
+    out = torch.empty_like(had)
+    ws = B.alloc_ws(B.litevggt_cached_mass_ws_bytes(p, new)).fill_(255)
+    B.litevggt_cached_mass(p, c.d, dev(q), i32([0, new]), i32([500]), had, out, ws)
+    assert torch.equal(out[0, 0, :500], had[0, 0, :500])
+    drawn = host(out - had)[0, 1, :500]
+    # what the other head draws: each row's weights sum to 1; 500 differences of values below 2, and sums of up to 200 rows (2^-17 a weight)
+    assert abs(drawn.sum() - new) <= 500 * 2.0 ** -23 * max(2.0, new) + new * 2.0 ** -16
