@@ -457,7 +457,8 @@ int litevggt_cache_evict(const litevggt_cache_params *p, const int32_t *page_tab
  * `inverse`: by -t, which undoes it and is its gradient.
  *   pos    [device] [n_tokens][axes] int32, of any sign
  *   q, q_out [device] [n_tokens, heads, head_dim] bf16;  k, k_out [device] [n_tokens, kv_heads, head_dim] bf16, not read with
- *            kv_heads = 0; row strides in elements (multiples of 8); an output may be its input, with the same stride
+ *            kv_heads = 0; row strides in elements (multiples of 8); an output may be its input, with the same stride; no row of an
+ *            output may meet another row of the call (LV_ERR_SHAPE)
  */
 enum { LV_ROPE_AXIS_HALVES = 0, LV_ROPE_HEAD_HALVES = 1, LV_ROPE_ADJACENT = 2 };
 typedef struct {

@@ -552,7 +552,7 @@ def litevggt_cache_evict(p: CacheParams, page_table, kv_len, mass, keep, first_p
 
 
 def litevggt_rope(p: RopeParams, pos, q, k, q_out, k_out) -> None:
-    """``k``, ``k_out``: None with ``kv_heads=0``.  An output may be its input."""
+    """``k``, ``k_out``: None with ``kv_heads=0``.  An output may be its input, row for row."""
     n, qp, qs = _rows(q, p.heads, p.head_dim, "q")
     m, op, os_ = _rows(q_out, p.heads, p.head_dim, "q_out")
     _same(n, m, "q and q_out")

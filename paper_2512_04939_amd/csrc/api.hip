@@ -157,6 +157,27 @@ int check_cache_buffers(const litevggt_cache *c, CacheView *cv) {
 bool rows_ok(const void *p, int64_t stride, int64_t n, int64_t width) {
   return ((uintptr_t)p & 15u) == 0 && stride % 8 == 0 && stride >= width && stride <= kMostStride && n >= 0;
 }
+// n rows of one call: where they begin, how far apart, how long (elements of 2 bytes)
+struct RowSet {
+  const void *p;
+  int64_t stride, width;
+};
+// Whether a row of one set has bytes in common with a row of the other.  Of the same stride it is enough to look at the first rows, as slices
+// of one projection's output come with every call; others are walked by their ends.
+bool rows_meet(const RowSet &x, const RowSet &y, int64_t n) {
+  const bool swap = (uintptr_t)y.p < (uintptr_t)x.p;
+  const RowSet &a = swap ? y : x, &b = swap ? x : y;
+  const int64_t off = (int64_t)(((uintptr_t)b.p - (uintptr_t)a.p) / 2);
+  if (off >= (n - 1) * a.stride + a.width) return false;
+  if (a.stride == b.stride && n > 1) return off % a.stride < a.width || off % a.stride + b.width > a.stride;
+  for (int64_t i = 0, j = 0; i < n && j < n;) {
+    const int64_t a0 = i * a.stride, b0 = off + j * b.stride;
+    if (a0 < b0 + b.width && b0 < a0 + a.width) return true;
+    a0 < b0 ? ++i : ++j;
+  }
+  return false;
+}
+
 // tokens of a call, and of these times heads (grids of 256 threads stay below 2^32 of them in x)
 bool count_ok(int64_t n, int64_t heads) { return n >= 0 && n < ((int64_t)1 << 24) && n * heads < ((int64_t)1 << 26); }
 
@@ -598,6 +619,15 @@ int litevggt_rope(const litevggt_rope_params *p, int64_t n_tokens, const int32_t
   const int64_t width = (int64_t)p->heads * p->head_dim, kw = (int64_t)p->kv_heads * p->head_dim;
   if (!rows_ok(q, q_stride, n_tokens, width) || !rows_ok(q_out, q_out_stride, n_tokens, width)) return LV_ERR_SHAPE;
   if (p->kv_heads > 0 && (!rows_ok(k, k_stride, n_tokens, kw) || !rows_ok(k_out, k_out_stride, n_tokens, kw))) return LV_ERR_SHAPE;
+  // (the kernel reads a token's rows and writes them, in no order among tokens)
+  const RowSet in[2] = {{q, q_stride, width}, {k, k_stride, kw}}, out[2] = {{q_out, q_out_stride, width}, {k_out, k_out_stride, kw}};
+  const int sets = p->kv_heads > 0 ? 2 : 1;
+  for (int o = 0; o < sets; ++o)
+    for (int i = 0; i < sets; ++i) {
+      const bool in_place = i == o && in[i].p == out[o].p && (in[i].stride == out[o].stride || n_tokens == 1);
+      if (!in_place && rows_meet(in[i], out[o], n_tokens)) return LV_ERR_SHAPE;
+    }
+  if (sets == 2 && rows_meet(out[0], out[1], n_tokens)) return LV_ERR_SHAPE;
   return launch_rope(r, pos, (int)n_tokens, p->heads, p->kv_heads, p->head_dim, p->inverse != 0, (const uint16_t *)q, q_stride,
                      (const uint16_t *)k, k_stride, (uint16_t *)q_out, q_out_stride, (uint16_t *)k_out, k_out_stride, (hipStream_t)stream);
 }
