@@ -20,8 +20,11 @@
 
 #include "internal.h"
 #include "common.h"
+#include "mass_plan.h"
 
 namespace lv {
+
+using namespace mass;
 
 namespace {
 
@@ -30,16 +33,6 @@ constexpr float kRaise = 1.0995116e12f;      // 2^40: a sum beyond it raises the
 constexpr int kNoKey = 0x7fff0000;           // the position of a key that is not there: beyond all that rows see
 
 enum class Kind { BF16, E4M3, E2M1 };
-
-// How the keys of a call are cut: into chunks of so many, and these into pieces, about `aim` of them in all, so that pieces of sequences with
-// many rows are shorter and all take about as long
-struct Cut {
-  int chunk, aim;
-  int most;                // pieces of a sequence
-  int block;               // rows that a wave takes at a time
-  bool of_rows;            // sequences without queries have no pieces
-  const int *starts;       // more than 64 sequences: units before each, in all, and the work of a piece (k_mass_plan); else null
-};
 
 struct Call {
   const uint16_t *q;
@@ -160,22 +153,13 @@ struct Work {
   int c0, c1;      // its chunks
 };
 
-__device__ __forceinline__ int quotient_up(int a, int b) { return (int)(((uint32_t)a + (uint32_t)b - 1u) / (uint32_t)b); }
-__device__ __forceinline__ bool has_pieces(const Cut &c, const Seq &s) { return s.nk > 0 && (!c.of_rows || s.nq > 0); }
-// What a chunk of a sequence costs, what all of them do
-__device__ __forceinline__ float cost(const Call &a, const Cut &c, const Seq &s) { return (float)max(quotient_up(s.nq * a.group, c.block), 1); }
+// What all chunks of a sequence cost
 __device__ __forceinline__ float cost_of_all(const Call &a, const Cut &c, const Seq &s) {
-  return has_pieces(c, s) ? cost(a, c, s) * (float)quotient_up(s.nk, c.chunk) : 0.f;
+  return has_pieces(c, s.nq, s.nk) ? chunk_cost(c, s.nq * a.group) * (float)quotient_up(s.nk, c.chunk) : 0.f;
 }
-// The work of a piece, from that of all sequences and heads (a hair more, so that there are not more pieces than were aimed at and one for each
-// sequence and head)
-__device__ __forceinline__ float piece_work(const Call &a, const Cut &c, float all) { return all * (float)a.kv_heads / (float)c.aim * 1.0001f; }
-__device__ __forceinline__ int chunks_of_piece(const Call &a, const Cut &c, const Seq &s, float work) {
-  const int chunks = quotient_up(s.nk, c.chunk);
-  return max(max((int)fminf(ceilf(work / cost(a, c, s)), (float)chunks), quotient_up(chunks, c.most)), 1);
-}
+__device__ __forceinline__ int chunks_of_piece(const Call &a, const Cut &c, const Seq &s, float work) { return mass::chunks_of_piece(c, s.nq * a.group, s.nk, work); }
 __device__ __forceinline__ int units_of(const Call &a, const Cut &c, const Seq &s, float work) {
-  return has_pieces(c, s) ? quotient_up(quotient_up(s.nk, c.chunk), chunks_of_piece(a, c, s, work)) * a.kv_heads * a.splits : 0;
+  return has_pieces(c, s.nq, s.nk) ? quotient_up(quotient_up(s.nk, c.chunk), chunks_of_piece(a, c, s, work)) * a.kv_heads * a.splits : 0;
 }
 // The work of a piece, worked out by every wave (the same in all of them) or once
 __device__ __forceinline__ Seq lane_seq(const Call &a) {
@@ -184,7 +168,7 @@ __device__ __forceinline__ Seq lane_seq(const Call &a) {
 }
 __device__ __forceinline__ float work_of(const Call &a, const Cut &c, const Seq &mine) {
   if (c.starts) return __builtin_bit_cast(float, uniform_at(c.starts, a.n_seq + 1));
-  return piece_work(a, c, wave_sum_ordered((int)(threadIdx.x & 63) < a.n_seq ? cost_of_all(a, c, mine) : 0.f));
+  return piece_work(c, a.kv_heads, wave_sum_ordered((int)(threadIdx.x & 63) < a.n_seq ? cost_of_all(a, c, mine) : 0.f));
 }
 
 // up to the lane (row_shr 1, 2, 4, 8 inside rows of 16 lanes; the rows' last lanes to the rows behind)
@@ -225,7 +209,7 @@ __device__ __forceinline__ bool find_work(const Call &a, int unit, Work &w, Seq 
     s.nk = __builtin_amdgcn_readlane(mine.nk, w.seq);
     s.p0 = __builtin_amdgcn_readlane(mine.p0, w.seq);
   }
-  if (!has_pieces(c, s)) return false;      // (lengths that changed meanwhile)
+  if (!has_pieces(c, s.nq, s.nk)) return false;      // (lengths that changed meanwhile)
   const int chunks = quotient_up(s.nk, c.chunk), per = scalar(chunks_of_piece(a, c, s, work)), pieces = scalar(quotient_up(chunks, per));
   const int x = scalar((int)((uint32_t)local / (uint32_t)pieces));
   w.piece = scalar(local - x * pieces);
@@ -256,7 +240,7 @@ __global__ __launch_bounds__(1024) void k_mass_plan(Call a, Call b, int *starts_
     __syncthreads();
     all = 0.f;
     for (int x = 0; x < 16; ++x) all += works[x];
-    const float work = piece_work(c, c.cut, all);
+    const float work = piece_work(c.cut, c.kv_heads, all);
     int before = 0;
     for (int i0 = 0; i0 < c.n_seq; i0 += 1024) {
       const int i = i0 + tid, turn = i0 >> 10 & 1;
@@ -817,49 +801,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ---------------------------------------------------------------------------------------
-namespace {
-
-constexpr int kAim = 4096;                             // waves of the few rows' kernels: two rounds of eight a CU
-constexpr int kAimMany = 32768;                        // of the many rows', whose chunks are longer work
-constexpr int kUnits = 6144;                           // three rounds of two waves a SIMD
-constexpr int64_t kMostParts = (int64_t)1 << 25;       // (row, piece) pairs in the workspace, where rows leave a choice
-constexpr int64_t kMostScores = (int64_t)1 << 27;      // scores there
-
-struct Form {
-  bool few, scores, small_chunks;
-  int aim, splits;         // units; of the rows
-  int most;                // pieces of a sequence
-};
-// Pieces of the only sequence that has many keys, at most
-int64_t most_pieces(int kv_heads, int64_t most_keys) { return std::max((int64_t)1, std::min((int64_t)(kAimMany + kv_heads - 1) / kv_heads, (most_keys + 31) / 32)); }
-// Tokens up to which scores are kept: where writing and reading them costs less than reading K and taking the products again, and they fit.  Over
-// 60,000 positions, 16 heads of 64, kept and not: bf16 16 rows 67 us and 81, 24 77 and 82, 32 87 and 81; E4M3 12 57 and 61, 24 71 and 62; E2M1 12 53 and
-// 58, 16 60 and 58; of 128, bf16 32 115 and 144, E2M1 16 65 and 75.
-int64_t kept_tokens(int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
-  const int64_t row_bytes = dtype == LV_CACHE_BF16 ? 2 * head_dim : dtype == LV_CACHE_E4M3 ? head_dim : head_dim / 2;
-  const int64_t rows = std::min(row_bytes / 8 + 8, (int64_t)32);
-  return std::min(rows * n_seq / (heads / kv_heads), kMostScores / (most_keys * heads));
-}
-Form form_of(int n_q, int n_seq, int heads, int kv_heads, int head_dim, int dtype, int64_t most_keys) {
-  Form f;
-  const int64_t pairs = (int64_t)n_seq * kv_heads, rows = std::max((int64_t)n_q, (int64_t)1) * heads;
-  const double mean = (double)n_q * (heads / kv_heads) / n_seq;
-  f.scores = n_q <= kept_tokens(n_seq, heads, kv_heads, head_dim, dtype, most_keys);
-  // (not kept, E2M1: 32 rows of 128 channels 75 us so, 86 in the other form; 16 of 64 64 and 58)
-  f.few = f.scores || mean <= (head_dim == 128 ? 32.0 : 8.0);
-  f.aim = f.few ? kAim : kAimMany;
-  f.most = (int)std::max((int64_t)1, std::min(most_pieces(kv_heads, most_keys), kMostParts / rows));
-  // Many rows: where the chunks are too few to fill the chip a few times over, rows are split too, down to four blocks of 32.  (The sums by
-  // keys cannot be: they take chunks of 32 keys then.)
-  const int64_t blocks = ((int64_t)n_q * (heads / kv_heads) / n_seq + 31) / 32, chunk = head_dim == 64 ? 256 : 128;
-  const int64_t units = std::min(pairs * ((most_keys + chunk - 1) / chunk), (int64_t)f.aim);
-  f.splits = f.few ? 1 : (int)std::max((int64_t)1, std::min(std::min((kUnits + units - 1) / units, blocks / 4), (int64_t)64));
-  f.small_chunks = pairs * ((most_keys + chunk / 2 - 1) / (chunk / 2)) < kUnits / 4;
-  return f;
-}
-
-}  // namespace
-
 // Parts, divisors, normalised rows, scores: each as much as any call of up to n_q tokens takes, so that scratch for more serves fewer
 static size_t parts_bytes(int64_t rows, int kv_heads, int64_t most_keys) {
   return align_up((size_t)std::min(rows * most_pieces(kv_heads, most_keys), std::max(kMostParts, rows)) * sizeof(float2), 256);
@@ -878,18 +819,12 @@ template <Kind K, int D>
 static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *plan, hipStream_t st) {
   const double rows = (double)x.n_q * c.group / c.n_seq;
   const int64_t pairs = (int64_t)c.n_seq * c.kv_heads;
-  constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;
-  const bool keep = x.n_q > 0 && f.few && f.scores;
-  const int kc_rows = f.few ? 32 : 32 * NR, kc_keys = keep ? 1024 : f.few ? 64 : f.small_chunks ? 32 : 32 * NK;
-  // as many workgroups as there are CUs or fewer join their rows themselves
+  constexpr int NR = D == 64 ? 8 : 4, NK = D == 64 ? 4 : 2;      // tiles of a chunk of the many rows' kernels (Form's cuts)
   const int64_t most = (int64_t)c.max_pages << c.page_shift;
-  const bool own = keep && pairs * ((most + 1023) / 1024) <= 256;
-  const bool eight = rows <= 8.0;
-  const int block = f.few && eight ? 8 : 32;
   Call by_rows = c, by_keys = c;
-  by_rows.cut = Cut{kc_rows, f.aim, f.most, block, true, nullptr};
+  by_rows.cut = f.rows;
   by_rows.splits = f.splits;
-  by_keys.cut = Cut{kc_keys, f.aim, 0x7fffffff, block, false, nullptr};
+  by_keys.cut = f.keys;
   by_keys.splits = 1;
   if (c.n_seq > 64) {
     int *const starts = plan, *const starts_keys = (int *)((char *)plan + plan_bytes(c.n_seq) / 2);
@@ -907,8 +842,8 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
     kernel<<<dim3((uint32_t)((units(y) + 3) / 4)), 256, 0, st>>>(y);
   };
   if (x.n_q > 0) {
-    if (keep) eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
-    else if (f.few && eight) walk(k_mass_rows_few<K, D, 1, false>, by_rows);
+    if (f.keep) f.eight ? walk(k_mass_rows_few<K, D, 1, true>, by_rows) : walk(k_mass_rows_few<K, D, 4, true>, by_rows);
+    else if (f.few && f.eight) walk(k_mass_rows_few<K, D, 1, false>, by_rows);
     else if (f.few) {
       if constexpr (D == 128) walk(k_mass_rows_few<K, D, 4, false>, by_rows);
     } else {
@@ -919,14 +854,14 @@ static int launch_kind(const MassArgs &x, const Call &c, const Form &f, int *pla
       const int side = (int)std::min(per_pair, ((int64_t)x.n_q * c.group + at_once - 1) / at_once);
       kernel<<<dim3((uint32_t)(pairs * side)), 256, 0, st>>>(by_rows, side);
     };
-    if (!own) rows <= 64.0 ? join(k_mass_join<4>, 4) : join(k_mass_join<64>, 64);
+    if (!f.own) rows <= 64.0 ? join(k_mass_join<4>, 4) : join(k_mass_join<64>, 64);
   }
   const dim3 blocks((uint32_t)units(by_keys));
-  if (own) {
+  if (f.own) {
     k_mass_add<true><<<blocks, 256, 0, st>>>(by_keys);
-  } else if (keep) {
+  } else if (f.keep) {
     k_mass_add<false><<<blocks, 256, 0, st>>>(by_keys);
-  } else if (f.few && eight) {
+  } else if (f.few && f.eight) {
     walk(k_mass_keys_few<K, D, 2, 1>, by_keys);
   } else if (f.few) {
     if constexpr (D == 128) walk(k_mass_keys_few<K, D, 2, 4>, by_keys);
