@@ -416,8 +416,9 @@ int litevggt_cached_attn(const litevggt_cache_params *p, const litevggt_cache *c
  *   mass[s][h][t] = mass_in[s][h][t] + sum_r w_rt / sum_t' w_rt',   w_rt = exp(q_r . k_t * softmax_scale)
  * for the positions t below kv_len[s] that are held, 0 for those that are not; what lies from kv_len[s] on is left as it was.  A row that
  * sees no held position adds nothing, nor does one whose scores are all minus infinity; one with a score that is NaN or plus infinity
- * makes all that it sees NaN.  Everything is fp32 (from bf16 q and K as it is held); results do not depend on the order in which
- * workgroups run.  The call needs neither v nor v_scale.
+ * makes all that it sees NaN.  Scores, times softmax_scale, are to lie below 2^28 in magnitude, as in litevggt_cached_attn: far beyond it
+ * a row may come out as NaN or as if it saw no key.  Everything is fp32 (from bf16 q and K as it is held); results do not depend on the
+ * order in which workgroups run.  The call needs neither v nor v_scale.
  *   mass_in  [device] [n_seq][kv_heads][max_pages * page_tokens] fp32, 16-byte aligned; NULL: zeros; may be the same buffer as mass
  *   mass     [device] the same, out
  *   ws       litevggt_cached_mass_ws_bytes(p, n_tokens) bytes

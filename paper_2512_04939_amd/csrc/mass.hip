@@ -28,6 +28,8 @@ using namespace mass;
 
 namespace {
 
+// (A reference is c times the largest score, rounded: by 16 at most where scores, times the scale, stay below 2^28, so that all of a row's
+// weights are 2^16 times too large or too small at most, which the division takes out.  From 2^31 on they would leave fp32's range.)
 constexpr float kUnset = -1e30f;             // reference of a row that has seen no key
 constexpr float kRaise = 1.0995116e12f;      // 2^40: a sum beyond it raises the reference
 constexpr int kNoKey = 0x7fff0000;           // the position of a key that is not there: beyond all that rows see
