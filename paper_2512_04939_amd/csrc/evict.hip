@@ -3,7 +3,7 @@
 // Two kernels.  k_evict_sums reads the masses once, which bounds it (4 bytes per kv head and position), and sums them by page in 64 bits, so
 // that no order of the sums makes two pages change places that are not equal to 2^-50.  k_evict_select finds, with one workgroup to
 // a sequence, the page up to which they leave: by the bits of their sums, eleven at a time, until few are left.  32 sequences of up to 8588 pages of
-// 16, 16 heads: 24 us for the sums (156 MB), 19 to select, where each step waits for the one before; 46 with all bits by turns.
+// 16, 16 heads: 24 us for the sums (156 MB), 18 to select, where each step waits for the one before; 46 with all bits by turns.
 #include <algorithm>
 
 #include "internal.h"

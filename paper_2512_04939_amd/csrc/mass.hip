@@ -8,10 +8,12 @@
 // no barrier, and nobody waits for another wave.  Which channels a lane holds is free as long as q and k agree: a half wave takes half a
 // row's channels in one piece, so its loads are 16 bytes wide in every kind of cache.
 //
-// Up to 32 rows: bound by reading K and writing the scores, from which the second walk is made (5 rows over 137,405 positions of 16 heads of 64,
-// bf16: 61 to 66 us for 281 MB and 44, 5 to join, 14 to add; K twice was 48 and 54).  More: by the VALU.  A tile of 32 x 32 scores takes 16
+// Up to 32 rows: bound by reading K and writing the scores, from which the second walk is made, in bf16 (5 rows over 137,405 positions of 16 heads
+// of 64: 61 to 68 us for 281 MB and 44, 5 to join, 14 to add; K twice was 48 and 54); over codes by chains of dependent loads and three launches (5
+// rows over 60,000: 48 us in bf16, 34 in E4M3, 29 in E2M1, whose bytes take 27, 15 and 8).  More: a tile of 32 x 32 scores takes 16
 // exponentials, 16 multiply-adds and 16 sums of a lane, twice, some 400 cycles each time with what goes around them, against 128 of MFMA at 64
-// channels: four frames of 1374 tokens over 2748 to 41,220 positions of an E2M1 cache 500 us for the rows' sums and 450 for the keys', 20 to join.
+// channels: four frames of 1374 tokens over 2748 to 41,220 positions of an E2M1 cache 441 us for the rows' sums and 395 for the keys', 20 to join
+// (VALU 62 and 71 % busy, 1.5 and 1.6 of two waves resident to a SIMD, CUs busy 84 and 89 %).
 // (Tried and level: a tile's products ahead of or among the weights of the one before, keys in chunks of 5 tiles: 926, for want of registers.)
 //
 // References, sums and masses are fp32; sums over rows and pieces have a fixed order.  q is rounded to bf16 after its normalisation, as

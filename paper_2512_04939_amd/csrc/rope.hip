@@ -7,7 +7,8 @@
 //
 // Bound by HBM: every row is read and written once.  43,968 tokens of 16 + 16 heads of 64 in 63 us, 5.7 TB/s (a copy of 4 GB reaches 4.8 on the same
 // card); one head after the other behind the angles, as it was first, 97.  20,011 tokens of 16 + 4 heads of 128 in 38 us, 60 before.
-// A single token takes 3 us of the GPU.  Rounded to bf16: the result, once.
+// Axes whose pairs are no multiple of 8 fetch partners by two bytes: the former 177 us with halves of an axis paired (10, 11, 11 pairs), 126 with a
+// head's, 67 with neighbours.  A single token takes 3 us of the GPU.  Rounded to bf16: the result, once.
 #include "internal.h"
 #include "common.h"
 
