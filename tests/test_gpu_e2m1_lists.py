@@ -16,8 +16,8 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("page", [16, 32, 128])
 @pytest.mark.parametrize("n_seq,kv,group,dim,new,length", [
-    (16, 128, 1, 64, 1, 20000),      # 2048 units of 157 tiles for 3072 places: 104 tiles to a piece
-    (16, 64, 2, 128, 1, 20000),      # 1024 units, 1536 places
+    (16, 128, 1, 64, 1, 20000),      # 2048 units of 157 tiles in three rounds of 1024 places: 104 tiles to a piece
+    (16, 64, 2, 128, 1, 20000),      # 1024 units, three rounds of 512 places
     (16, 64, 1, 64, 40, 17000),      # rows in blocks of 64
     (130, 16, 1, 64, 65, 9000),      # many rows, not cut: 141 stages
     (130, 16, 1, 128, 40, 9000),
